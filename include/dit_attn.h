@@ -411,6 +411,107 @@ dit_status dit_qkv_proj_forward(const void *x, const void *w, const void *bias, 
                                 const dit_linear_params *lp, const dit_self_attn_params *ap,
                                 void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * ---- The projections of a transformer block in 8 bits ----
+ * The Diffusion stage runs the projections either side of attention, and those of the feed-forward layer, at every
+ * denoising step on the same weights (Sec. 2.4).  In 8 bits they read half the bytes and run at twice the matrix rate:
+ *   dit_quant_rows_forward        rows of numbers -> 8-bit rows (weights once; attention's output; GELU activations)
+ *   dit_rms_norm_quant_forward    residual addition, RMS normalisation and 8-bit rows in one pass
+ *   dit_linear_quant_forward      the product of 8-bit rows and 8-bit weights
+ *   dit_dequant_rows_forward      8-bit rows read back as numbers
+ *
+ * A QUANTISED ROW is N signed 8-bit integers q and one fp32 scale, and stands for the numbers q[n] * scale.  The
+ * quantisation is symmetric, one scale a row: with amax the largest magnitude of the row's numbers t,
+ *     scale = amax / 127,   q[n] = round to nearest even (t[n] * (127 / amax)),   in [-127, 127],
+ * so the largest number is kept, and every other is off by at most half a scale.  All of it is computed in fp32.
+ *   - A row whose amax is below 2^-120 (a row of zeros) gets scale 0 and q 0.
+ *   - A row with a NaN or an infinity gets scale NaN and q 0: whatever reads the row yields NaN, and no other row is touched.
+ * 8-bit rows start on multiples of 16 bytes, like every row; exactly N bytes of a row are written.  Scales are dense:
+ * one for each row.
+ */
+
+/*
+ * t = act(x) to 8-bit rows.  x: [M, N] bf16 or fp32, row stride ldx.  q: [M, N] int8, row stride ldq (bytes).
+ * scale: [M] fp32.  The weights w [N, K] of a projection are quantised by this call too: a scale for each output channel.
+ * act: DIT_ACT_NONE, or DIT_ACT_GELU_TANH: t = x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))), in fp32.
+ * No workspace.  q may not overlap x.
+ * Errors: NULL x/q/scale/p, M or N < 1, a stride shorter than its row, a bad dtype or act, nonzero flags ->
+ * DIT_ERR_INVALID_ARG; N above DIT_QUANT_MAX_COLUMNS -> DIT_ERR_UNSUPPORTED; a base pointer or row stride that breaks
+ * 16-byte row alignment (4 bytes for scale) -> DIT_ERR_ALIGNMENT.
+ */
+#define DIT_QUANT_MAX_COLUMNS 65536
+
+typedef enum { DIT_ACT_NONE = 0, DIT_ACT_GELU_TANH = 1 } dit_act;
+
+typedef struct {
+    int32_t M, N;
+    int64_t ldx, ldq;
+    int32_t x_dtype; /* dit_dtype of x */
+    int32_t act;     /* dit_act */
+    uint32_t flags;  /* reserved, must be 0 */
+} dit_quant_rows_params;
+
+dit_status dit_quant_rows_forward(const void *x, int8_t *q, float *scale, const dit_quant_rows_params *p, void *stream);
+
+/*
+ * The step between two sublayers of a block: the sublayer's output x is added to the residual stream, and the sum is
+ * normalised and quantised for the next projection, in one pass over the rows:
+ *     h = x + residual,   y = h * gamma / sqrt(mean over the N columns of h^2 + eps),   q, scale = 8-bit rows of y.
+ * The sum h is used unrounded (fp32); h_out gets it rounded once to r_dtype.  Since 1 / sqrt(...) is common to a row, q is
+ * computed from h * gamma, and the factor goes into the scale alone: q does not depend on how the squares are summed.
+ *   x         [M, N] bf16 or fp32 (x_dtype, ldx)
+ *   residual  [M, N] of r_dtype (ldr), or NULL: h = x
+ *   gamma     [N] fp32, 16-byte aligned, or NULL: all 1
+ *   h_out     [M, N] of r_dtype (ldh); NULL if the sum is not wanted.  Without residual it must be NULL.  It may be the
+ *             residual itself, or x, if type and strides are the same too (the sum replaces it); else it may not overlap
+ *             either.
+ *   q, scale  as above.  A row whose sum of squares overflows fp32 counts as one with an infinity.
+ * No workspace.  Errors: as dit_quant_rows_forward; eps negative or not finite, h_out without residual -> DIT_ERR_INVALID_ARG.
+ */
+typedef struct {
+    int32_t M, N;
+    int64_t ldx, ldr, ldh, ldq; /* ldr, ldh are ignored where the pointer is NULL */
+    float eps;
+    int32_t x_dtype; /* dit_dtype of x */
+    int32_t r_dtype; /* dit_dtype of residual and h_out */
+    uint32_t flags;  /* reserved, must be 0 */
+} dit_norm_quant_params;
+
+dit_status dit_rms_norm_quant_forward(const void *x, const void *residual, const float *gamma, void *h_out, int8_t *q,
+                                      float *scale, const dit_norm_quant_params *p, void *stream);
+
+/*
+ * 8-bit rows read back: y[m, n] = q[m, n] * scale[m], rounded once to out_dtype.  q: [M, N] int8 (ldq), scale: [M] fp32,
+ * y: [M, N] bf16 or fp32 (ldy).  No workspace, no limit on N.  Errors: as dit_quant_rows_forward.
+ */
+typedef struct {
+    int32_t M, N;
+    int64_t ldq, ldy;
+    int32_t out_dtype;
+    uint32_t flags; /* reserved, must be 0 */
+} dit_dequant_rows_params;
+
+dit_status dit_dequant_rows_forward(const int8_t *q, const float *scale, void *y, const dit_dequant_rows_params *p,
+                                    void *stream);
+
+/*
+ * The projection of dit_linear_forward on 8-bit rows, a scale for each token and one for each output channel:
+ *     y[m, n] = (sum_k x[m, k] w[n, k]) * (x_scale[m] * w_scale[n]) + bias[n].
+ * x: [M, K] int8, x_scale: [M] fp32; w: [N, K] int8, w_scale: [N] fp32; bias: [N] bf16 or NULL; y: [M, N] bf16 or fp32
+ * (out_dtype).  Strides in ELEMENTS.  The sum is an exact 32-bit integer, so results do not depend on the order of the
+ * sum nor on the tiles: a row of y depends on its own x row alone, bit for bit.  It is rounded to fp32 (a relative 2^-24),
+ * scaled and biased in fp32, and rounded once if y is bf16.  M, N and K need not be multiples of anything (K a
+ * multiple of 128 is fastest); M = 1 is a pass over the weights.  Every 8-bit value counts, -128 too.
+ * x and w are read in whole 16-byte pieces: the bytes between the end of a row and the next multiple of 16 are read
+ * (also behind the last row) and not used.  x and w may not overlap y.  No workspace.
+ * Errors: NULL x, x_scale, w, w_scale, y or p, M, N or K < 1, a stride shorter than its row, bad out_dtype or nonzero
+ * flags -> DIT_ERR_INVALID_ARG; K above 131071 (the sum could pass 31 bits), ldx or ldw above 2^23 -> DIT_ERR_UNSUPPORTED;
+ * a base pointer or row stride that breaks 16-byte row alignment (w_scale too; 8 bytes for bias, 4 for x_scale) ->
+ * DIT_ERR_ALIGNMENT.
+ */
+dit_status dit_linear_quant_forward(const int8_t *x, const float *x_scale, const int8_t *w, const float *w_scale,
+                                    const void *bias, void *y, const dit_linear_params *p, void *stream);
+
 /* Static strings; never NULL. */
 const char *dit_strerror(dit_status s);
 /* Text of the last HIP error seen by the calling thread ("" if none). */

@@ -60,6 +60,10 @@ EXPORTS = (
     "dit_attn_varlen_forward",
     "dit_linear_forward",
     "dit_qkv_proj_forward",
+    "dit_quant_rows_forward",
+    "dit_rms_norm_quant_forward",
+    "dit_dequant_rows_forward",
+    "dit_linear_quant_forward",
     "dit_mfma_probe",
     "dit_attn_set_timing_events",
     "dit_strerror",
@@ -137,6 +141,33 @@ class dit_linear_params(ctypes.Structure):
     ]
 
 
+DIT_QUANT_MAX_COLUMNS = 65536
+DIT_ACT_NONE = 0
+DIT_ACT_GELU_TANH = 1
+
+
+class dit_quant_rows_params(ctypes.Structure):
+    _fields_ = [
+        ("M", ctypes.c_int32), ("N", ctypes.c_int32), ("ldx", ctypes.c_int64), ("ldq", ctypes.c_int64),
+        ("x_dtype", ctypes.c_int32), ("act", ctypes.c_int32), ("flags", ctypes.c_uint32),
+    ]
+
+
+class dit_norm_quant_params(ctypes.Structure):
+    _fields_ = [
+        ("M", ctypes.c_int32), ("N", ctypes.c_int32),
+        ("ldx", ctypes.c_int64), ("ldr", ctypes.c_int64), ("ldh", ctypes.c_int64), ("ldq", ctypes.c_int64),
+        ("eps", ctypes.c_float), ("x_dtype", ctypes.c_int32), ("r_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+    ]
+
+
+class dit_dequant_rows_params(ctypes.Structure):
+    _fields_ = [
+        ("M", ctypes.c_int32), ("N", ctypes.c_int32), ("ldq", ctypes.c_int64), ("ldy", ctypes.c_int64),
+        ("out_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+    ]
+
+
 class DitError(RuntimeError):
     def __init__(self, status, what):
         self.status = int(status)
@@ -183,6 +214,14 @@ def lib():
         L.dit_qkv_proj_forward.restype = ctypes.c_int
         L.dit_qkv_proj_forward.argtypes = [vp, vp, vp, vp, ctypes.POINTER(dit_linear_params),
                                            ctypes.POINTER(dit_self_attn_params), vp, ctypes.c_size_t, vp]
+        L.dit_quant_rows_forward.restype = ctypes.c_int
+        L.dit_quant_rows_forward.argtypes = [vp, vp, vp, ctypes.POINTER(dit_quant_rows_params), vp]
+        L.dit_rms_norm_quant_forward.restype = ctypes.c_int
+        L.dit_rms_norm_quant_forward.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(dit_norm_quant_params), vp]
+        L.dit_dequant_rows_forward.restype = ctypes.c_int
+        L.dit_dequant_rows_forward.argtypes = [vp, vp, vp, ctypes.POINTER(dit_dequant_rows_params), vp]
+        L.dit_linear_quant_forward.restype = ctypes.c_int
+        L.dit_linear_quant_forward.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(dit_linear_params), vp]
         L.dit_mfma_probe.restype = ctypes.c_int
         L.dit_mfma_probe.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, vp, ctypes.c_size_t,
                                      ctypes.POINTER(ctypes.c_double), vp]
@@ -583,6 +622,147 @@ def dit_qkv_proj_forward(x, w, bias, grid, split, H, q_out=None, origin=(0, 0, 0
     if st != DIT_OK:
         raise DitError(st, "dit_qkv_proj_forward")
     return q_out, workspace
+
+
+def _empty_rows(M, N, dtype, device):
+    """An [M, N] tensor whose rows start on multiples of 16 bytes."""
+    per = 16 // dtype.itemsize
+    return torch.empty((M, (N + per - 1) // per * per), dtype=dtype, device=device)[:, :N]
+
+
+def _check_rows(what, name, t, shape, dtype, device):
+    """t: a [M, N] tensor of that type on that device, contiguous along its rows.  dtype None: bf16 or float32."""
+    if t.shape != shape or t.stride(1) != 1 and shape[1] != 1:
+        raise ValueError("%s: %s must be a %s tensor with contiguous rows" % (what, name, tuple(shape)))
+    if dtype is None:
+        _dtype_code(t)
+    elif t.dtype != dtype:
+        raise TypeError("%s: %s must be %s, got %s" % (what, name, dtype, t.dtype))
+    if not t.is_cuda or t.device != device:
+        raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+
+
+def _check_vector(what, name, t, n, dtype, device):
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s: %s must be a dense tensor of %d elements" % (what, name, n))
+    if t.dtype != dtype:
+        raise TypeError("%s: %s must be %s, got %s" % (what, name, dtype, t.dtype))
+    if t.device != device:
+        raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+
+
+def _quant_outputs(what, x, q, scale):
+    """q and scale of x's rows: allocated, or checked."""
+    if x.dim() != 2:
+        raise ValueError("%s: x must be [M, N]" % what)
+    M, N = x.shape
+    if q is None:
+        q = _empty_rows(M, N, torch.int8, x.device)
+    else:
+        _check_rows(what, "q", q, x.shape, torch.int8, x.device)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=x.device)
+    else:
+        _check_vector(what, "scale", scale, M, torch.float32, x.device)
+    return q, scale
+
+
+_ACT_CODES = {"none": DIT_ACT_NONE, "gelu": DIT_ACT_GELU_TANH}
+
+
+def dit_quant_rows_forward(x, act="none", q=None, scale=None, stream=None):
+    """Rows of x [M, N] (bf16 or float32), through act ("none" or "gelu"), to 8-bit rows: returns q [M, N] int8 and
+    scale [M] float32; the rows stand for q * scale[:, None]."""
+    if act not in _ACT_CODES:
+        raise ValueError("dit_quant_rows_forward: act must be one of %s" % ", ".join(sorted(_ACT_CODES)))
+    q, scale = _quant_outputs("dit_quant_rows_forward", x, q, scale)
+    _check_rows("dit_quant_rows_forward", "x", x, x.shape, None, x.device)
+    p = dit_quant_rows_params(x.shape[0], x.shape[1], x.stride(0), q.stride(0), _dtype_code(x), _ACT_CODES[act], 0)
+    st = lib().dit_quant_rows_forward(x.data_ptr(), q.data_ptr(), scale.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
+    if st != DIT_OK:
+        raise DitError(st, "dit_quant_rows_forward")
+    return q, scale
+
+
+def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=None, q=None, scale=None, stream=None):
+    """h = x + residual, y = h * gamma / sqrt(mean(h^2) + eps) and y's 8-bit rows: x [M, N] bf16 or float32, gamma [N]
+    float32 or None, residual [M, N] bf16 or float32 or None.  Returns (q, scale), and with a residual (q, scale, h): h in
+    residual's type, in h_out if given (residual itself: the sum replaces it)."""
+    what = "dit_rms_norm_quant_forward"
+    q, scale = _quant_outputs(what, x, q, scale)
+    _check_rows(what, "x", x, x.shape, None, x.device)
+    if gamma is not None:
+        _check_vector(what, "gamma", gamma, x.shape[1], torch.float32, x.device)
+    ldr = ldh = r_code = 0
+    if residual is not None:
+        _check_rows(what, "residual", residual, x.shape, None, x.device)
+        if h_out is None:
+            h_out = _empty_rows(x.shape[0], x.shape[1], residual.dtype, x.device)
+        else:
+            _check_rows(what, "h_out", h_out, x.shape, residual.dtype, x.device)
+        ldr, ldh, r_code = residual.stride(0), h_out.stride(0), _dtype_code(residual)
+    elif h_out is not None:
+        raise ValueError("%s: h_out needs a residual" % what)
+    p = dit_norm_quant_params(x.shape[0], x.shape[1], x.stride(0), ldr, ldh, q.stride(0), eps, _dtype_code(x), r_code, 0)
+    st = lib().dit_rms_norm_quant_forward(x.data_ptr(), residual.data_ptr() if residual is not None else None,
+                                          gamma.data_ptr() if gamma is not None else None,
+                                          h_out.data_ptr() if h_out is not None else None, q.data_ptr(),
+                                          scale.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
+    if st != DIT_OK:
+        raise DitError(st, what)
+    return (q, scale) if residual is None else (q, scale, h_out)
+
+
+def dit_dequant_rows_forward(q, scale, out=None, out_dtype=None, stream=None):
+    """8-bit rows read back: q [M, N] int8 times scale [M] float32, as bf16 (default) or float32 rows."""
+    what = "dit_dequant_rows_forward"
+    if q.dim() != 2:
+        raise ValueError("%s: q must be [M, N]" % what)
+    _check_rows(what, "q", q, q.shape, torch.int8, q.device)
+    _check_vector(what, "scale", scale, q.shape[0], torch.float32, q.device)
+    if out is None:
+        out = _empty_rows(q.shape[0], q.shape[1], out_dtype or torch.bfloat16, q.device)
+    _check_rows(what, "out", out, q.shape, None, q.device)
+    p = dit_dequant_rows_params(q.shape[0], q.shape[1], q.stride(0), out.stride(0), _dtype_code(out), 0)
+    st = lib().dit_dequant_rows_forward(q.data_ptr(), scale.data_ptr(), out.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
+    if st != DIT_OK:
+        raise DitError(st, what)
+    return out
+
+
+def _check_pieces(what, name, t):
+    """The projection reads 8-bit rows in whole 16-byte pieces, the last row too: its storage has to hold the last piece."""
+    end = t.storage_offset() + (t.shape[0] - 1) * t.stride(0) + (t.shape[1] + 15) // 16 * 16
+    if t.shape[1] % 16 and t.shape[0] and end > t.untyped_storage().nbytes():
+        raise ValueError("%s: the storage of %s ends inside the last 16-byte piece of its last row" % (what, name))
+
+
+def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dtype=None, stream=None):
+    """y = (x w^T) * x_scale[:, None] * w_scale[None, :] + bias on 8-bit rows: x [M, K] and w [N, K] int8, x_scale [M] and
+    w_scale [N] float32, bias [N] bf16 or None; y [M, N] bf16 (default) or float32."""
+    what = "dit_linear_quant_forward"
+    if x.dim() != 2 or w.dim() != 2 or w.shape[1] != x.shape[1]:
+        raise ValueError("%s: shapes do not fit y[M, N] = x[M, K] w[N, K]^T" % what)
+    M, K = x.shape
+    N = w.shape[0]
+    _check_rows(what, "x", x, x.shape, torch.int8, x.device)
+    _check_rows(what, "w", w, w.shape, torch.int8, x.device)
+    _check_pieces(what, "x", x)
+    _check_pieces(what, "w", w)
+    _check_vector(what, "x_scale", x_scale, M, torch.float32, x.device)
+    _check_vector(what, "w_scale", w_scale, N, torch.float32, x.device)
+    if bias is not None:
+        _check_vector(what, "bias", bias, N, torch.bfloat16, x.device)
+    if out is None:
+        out = _empty_rows(M, N, out_dtype or torch.bfloat16, x.device)
+    _check_rows(what, "out", out, (M, N), None, x.device)
+    p = dit_linear_params(M, N, K, x.stride(0), w.stride(0), out.stride(0), _dtype_code(out), 0)
+    st = lib().dit_linear_quant_forward(x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
+                                        bias.data_ptr() if bias is not None else None, out.data_ptr(), ctypes.byref(p),
+                                        _stream_ptr(stream))
+    if st != DIT_OK:
+        raise DitError(st, what)
+    return out
 
 
 DIT_PROBE_BF16 = 0

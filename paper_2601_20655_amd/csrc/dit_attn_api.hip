@@ -834,6 +834,26 @@ int dit::packed_layout(const void* params, size_t workspace_bytes, int* split_ti
     return pl.fl.nw;
 }
 
+namespace {
+
+// A launch between the caller's timing events.
+template <class F>
+dit_status timed_launch(const char* name, hipStream_t s, F&& launch) {
+    const bool timed = g_ev_before && g_ev_after;
+    hipError_t e;
+    if (timed && (e = hipEventRecord(g_ev_before, s)) != hipSuccess) return hip_fail(e, "hipEventRecord");
+    e = launch();
+    if (e != hipSuccess) return hip_fail(e, name);
+    if (timed && (e = hipEventRecord(g_ev_after, s)) != hipSuccess) return hip_fail(e, "hipEventRecord");
+    return DIT_OK;
+}
+
+size_t dtype_bytes(int32_t t) { return t == DIT_F32 ? 4 : 2; }
+bool bad_dtype(int32_t t) { return t != DIT_BF16 && t != DIT_F32; }
+bool off16(const void* p, int64_t ld, size_t bytes) { return (uintptr_t)p % 16 || ((uint64_t)ld * bytes) % 16; }
+
+}  // namespace
+
 extern "C" {
 
 size_t dit_attn_workspace_bytes(const dit_self_attn_params* p) {
@@ -1287,6 +1307,106 @@ dit_status dit_qkv_proj_forward(const void* x, const void* w, const void* bias, 
         if (e != hipSuccess) return hip_fail(e, "k_rescale_kernel");
     }
     return DIT_OK;
+}
+
+dit_status dit_quant_rows_forward(const void* x, int8_t* q, float* scale, const dit_quant_rows_params* p, void* stream) {
+    if (!x || !q || !scale || !p) return DIT_ERR_INVALID_ARG;
+    if (p->M < 1 || p->N < 1 || p->ldx < p->N || p->ldq < p->N || p->flags != 0) return DIT_ERR_INVALID_ARG;
+    if (bad_dtype(p->x_dtype) || (p->act != DIT_ACT_NONE && p->act != DIT_ACT_GELU_TANH)) return DIT_ERR_INVALID_ARG;
+    if (p->N > DIT_QUANT_MAX_COLUMNS) return DIT_ERR_UNSUPPORTED;
+    if (off16(x, p->ldx, dtype_bytes(p->x_dtype)) || off16(q, p->ldq, 1) || (uintptr_t)scale % 4) return DIT_ERR_ALIGNMENT;
+    dit::QuantArgs a{};
+    a.x = x;
+    a.q = q;
+    a.scale = scale;
+    a.M = p->M;
+    a.N = p->N;
+    a.ldx = p->ldx;
+    a.ldq = p->ldq;
+    a.x_f32 = p->x_dtype == DIT_F32;
+    a.gelu = p->act == DIT_ACT_GELU_TANH;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("quant_rows_kernel", s, [&] { return dit::launch_quant_rows(a, s); });
+}
+
+dit_status dit_rms_norm_quant_forward(const void* x, const void* residual, const float* gamma, void* h_out, int8_t* q,
+                                      float* scale, const dit_norm_quant_params* p, void* stream) {
+    if (!x || !q || !scale || !p) return DIT_ERR_INVALID_ARG;
+    if (p->M < 1 || p->N < 1 || p->ldx < p->N || p->ldq < p->N || p->flags != 0) return DIT_ERR_INVALID_ARG;
+    if (bad_dtype(p->x_dtype) || !(p->eps >= 0.0f) || isinf(p->eps)) return DIT_ERR_INVALID_ARG;
+    if (residual && (bad_dtype(p->r_dtype) || p->ldr < p->N)) return DIT_ERR_INVALID_ARG;
+    if (h_out && (!residual || p->ldh < p->N)) return DIT_ERR_INVALID_ARG;
+    if (p->N > DIT_QUANT_MAX_COLUMNS) return DIT_ERR_UNSUPPORTED;
+    const size_t re = dtype_bytes(p->r_dtype);
+    if (off16(x, p->ldx, dtype_bytes(p->x_dtype)) || off16(q, p->ldq, 1) || (uintptr_t)gamma % 16 ||
+        (uintptr_t)scale % 4 || (residual && off16(residual, p->ldr, re)) || (h_out && off16(h_out, p->ldh, re)))
+        return DIT_ERR_ALIGNMENT;
+    dit::QuantArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.gamma = gamma;
+    a.h_out = h_out;
+    a.q = q;
+    a.scale = scale;
+    a.M = p->M;
+    a.N = p->N;
+    a.ldx = p->ldx;
+    a.ldr = p->ldr;
+    a.ldh = p->ldh;
+    a.ldq = p->ldq;
+    a.eps = p->eps;
+    a.x_f32 = p->x_dtype == DIT_F32;
+    a.r_f32 = residual && p->r_dtype == DIT_F32;
+    a.norm = 1;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("quant_rows_kernel", s, [&] { return dit::launch_quant_rows(a, s); });
+}
+
+dit_status dit_dequant_rows_forward(const int8_t* q, const float* scale, void* y, const dit_dequant_rows_params* p,
+                                    void* stream) {
+    if (!q || !scale || !y || !p) return DIT_ERR_INVALID_ARG;
+    if (p->M < 1 || p->N < 1 || p->ldq < p->N || p->ldy < p->N || p->flags != 0) return DIT_ERR_INVALID_ARG;
+    if (bad_dtype(p->out_dtype)) return DIT_ERR_INVALID_ARG;
+    if (off16(q, p->ldq, 1) || off16(y, p->ldy, dtype_bytes(p->out_dtype)) || (uintptr_t)scale % 4) return DIT_ERR_ALIGNMENT;
+    dit::DequantArgs a{};
+    a.q = q;
+    a.scale = scale;
+    a.y = y;
+    a.M = p->M;
+    a.N = p->N;
+    a.ldq = p->ldq;
+    a.ldy = p->ldy;
+    a.out_f32 = p->out_dtype == DIT_F32;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("dequant_rows_kernel", s, [&] { return dit::launch_dequant_rows(a, s); });
+}
+
+dit_status dit_linear_quant_forward(const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale,
+                                    const void* bias, void* y, const dit_linear_params* p, void* stream) {
+    if (!x || !x_scale || !w || !w_scale || !y || !p) return DIT_ERR_INVALID_ARG;
+    if (p->M < 1 || p->N < 1 || p->K < 1 || p->flags != 0) return DIT_ERR_INVALID_ARG;
+    if (p->ldx < p->K || p->ldw < p->K || p->ldy < p->N || bad_dtype(p->out_dtype)) return DIT_ERR_INVALID_ARG;
+    // (the kernels address the rows of one tile with 32-bit byte offsets)
+    if (p->K > dit::kQuantMaxK || p->ldx > (int64_t)1 << 23 || p->ldw > (int64_t)1 << 23) return DIT_ERR_UNSUPPORTED;
+    if (off16(x, p->ldx, 1) || off16(w, p->ldw, 1) || off16(y, p->ldy, dtype_bytes(p->out_dtype)) ||
+        (uintptr_t)w_scale % 16 || (uintptr_t)x_scale % 4 || (uintptr_t)bias % 8)
+        return DIT_ERR_ALIGNMENT;
+    dit::LinearQuantArgs a{};
+    a.x = x;
+    a.w = w;
+    a.x_scale = x_scale;
+    a.w_scale = w_scale;
+    a.bias = static_cast<const uint16_t*>(bias);
+    a.y = y;
+    a.M = p->M;
+    a.N = p->N;
+    a.K = p->K;
+    a.ldx = p->ldx;
+    a.ldw = p->ldw;
+    a.ldy = p->ldy;
+    a.out_f32 = p->out_dtype == DIT_F32;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("linear_quant_kernel", s, [&] { return dit::launch_linear_quant(a, s); });
 }
 
 void dit_attn_set_timing_events(void* before, void* after) {

@@ -292,4 +292,48 @@ struct KRescaleArgs {
 };
 hipError_t launch_k_rescale(const KRescaleArgs& a, hipStream_t s);
 
+// ---- 8-bit rows: N signed 8-bit integers and one fp32 scale a row (dit_rows_quant.hip) ----
+constexpr float kQuantTop = 127.0f;            // the largest magnitude of a row becomes this integer
+constexpr float kQuantZero = 0x1p-120f;        // rows whose largest magnitude is below count as zero (127 / amax stays finite)
+constexpr int kQuantMaxColumns = 65536;
+struct QuantArgs {
+    const void* x;         // [M, N] bf16 or fp32
+    const void* residual;  // nullable [M, N]
+    const float* gamma;    // nullable [N]
+    void* h_out;           // nullable [M, N], type of residual
+    int8_t* q;             // [M, N]
+    float* scale;          // [M]
+    int M, N;
+    int64_t ldx, ldr, ldh, ldq;
+    float eps;
+    int x_f32, r_f32;
+    int norm;  // RMS normalisation (else rows as they are, or through act)
+    int gelu;
+};
+hipError_t launch_quant_rows(const QuantArgs& a, hipStream_t s);
+struct DequantArgs {
+    const int8_t* q;
+    const float* scale;
+    void* y;
+    int M, N;
+    int64_t ldq, ldy;
+    int out_f32;
+};
+hipError_t launch_dequant_rows(const DequantArgs& a, hipStream_t s);
+
+// ---- projection of 8-bit rows, y = (x w^T) x_scale w_scale + bias ----
+constexpr int kQuantMaxK = 131071;  // 128 * 128 * K < 2^31
+struct LinearQuantArgs {
+    const int8_t* x;       // [M, K]
+    const int8_t* w;       // [N, K]
+    const float* x_scale;  // [M]
+    const float* w_scale;  // [N]
+    const uint16_t* bias;  // [N] bf16, nullable
+    void* y;               // [M, N] bf16 or fp32
+    int M, N, K;
+    int64_t ldx, ldw, ldy;
+    int out_f32;
+};
+hipError_t launch_linear_quant(const LinearQuantArgs& a, hipStream_t s);
+
 }  // namespace dit
