@@ -309,6 +309,7 @@ struct QuantArgs {
     int x_f32, r_f32;
     int norm;  // RMS normalisation (else rows as they are, or through act)
     int gelu;
+    int past_caches;  // set by launch_quant_rows
 };
 hipError_t launch_quant_rows(const QuantArgs& a, hipStream_t s);
 struct DequantArgs {
@@ -318,6 +319,7 @@ struct DequantArgs {
     int M, N;
     int64_t ldq, ldy;
     int out_f32;
+    int past_caches;  // set by launch_dequant_rows
 };
 hipError_t launch_dequant_rows(const DequantArgs& a, hipStream_t s);
 

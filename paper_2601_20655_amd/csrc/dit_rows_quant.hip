@@ -1,5 +1,18 @@
 // Rows of numbers to 8-bit rows (N signed integers and one fp32 scale a row) and back: plainly, through a GELU, or behind
 // the addition to the residual stream and an RMS normalisation.
+//
+// A row has to be seen whole before its first integer is known, and is read once: W wavefronts hold it in registers, C
+// chunks of eight columns a lane, exchange its largest magnitude (and sum of squares) and write its integers.  The
+// normalisation's factor 1 / sqrt(mean + eps) is common to the row, so it cancels in the integers
+// q = rint(t * 127 / max|t|), t = h * gamma, and appears in the scale alone: the integers do not wait for the sum.
+//
+// What bounds it: memory.  32,760 x 5,120, new rows at every call: norm with 16-bit residual 201 us (5.8 TB/s of reads and
+// writes), with a 32-bit one 333 (5.5), 16-bit rows to 8 bits 85 (5.9), back to 16 bits 88 (5.7) and 32 bits 134 (6.2);
+// GELU, 32,760 x 20,480, 350 (5.7).  (Copying 2 GiB by torch: 4.9 TB/s.)  Tried without gain: workgroups that walk several
+// rows with the weights in registers (201 -> 219 to 249 us; 105 -> 98 without a residual), weights asked for ahead of their
+// use (121 us against 105 without a residual: the registers cost a wavefront a SIMD).
+#include <type_traits>
+
 #include "dit_attn_device.h"
 #include "dit_attn_internal.h"
 
@@ -7,90 +20,352 @@ namespace dit {
 
 namespace {
 
-constexpr int kRowThreads = 256;
+constexpr int kMostChunks = 8;  // of a lane: 16 wavefronts of 64 lanes hold rows of 65,536 columns
+static_assert(kMostChunks * 8 * 64 * 16 == kQuantMaxColumns, "the longest row fits one workgroup");
 
-__device__ __forceinline__ float load_number(const void* base, int64_t i, int f32) {
-    return f32 ? static_cast<const float*>(base)[i]
-               : __uint_as_float((uint32_t)static_cast<const uint16_t*>(base)[i] << 16);
-}
+enum RowMode { ROW_PLAIN = 0, ROW_GELU = 1, ROW_NORM = 2 };
+enum RowType { ROW_NONE = 0, ROW_BF16 = 1, ROW_F32 = 2 };  // of the residual
 
-__device__ __forceinline__ void store_number(void* base, int64_t i, int f32, float v) {
-    if (f32) static_cast<float*>(base)[i] = v;
-    else static_cast<uint16_t*>(base)[i] = (uint16_t)pack2<OP_BF16>(v, 0.f);
-}
-
+// x/2 (1 + tanh(u)) = x / (1 + exp(-2u)), u = sqrt(2/pi) (x + 0.044715 x^3)
 __device__ __forceinline__ float gelu_tanh(float x) {
-    const float u = 0.7978845608028654f * (x + 0.044715f * x * x * x);
-    return 0.5f * x * (1.0f + tanhf(u));
+    constexpr float c1 = -2.0f * 0.7978845608028654f * kLog2e, c3 = c1 * 0.044715f;
+    const float e = __builtin_amdgcn_exp2f(x * fmaf(c3, x * x, c1));
+    return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
-// one workgroup a row, which is read twice: for its largest magnitude and sum of squares, and to quantise it
-__global__ void __launch_bounds__(kRowThreads) quant_rows_kernel(const QuantArgs a) {
-    __shared__ uint32_t s_top[kRowThreads];
-    __shared__ float s_sum[kRowThreads];
-    const int64_t m = blockIdx.x;
-    const int tid = threadIdx.x;
-    auto sum_of = [&](int n) {
-        float h = load_number(a.x, m * a.ldx + n, a.x_f32);
-        if (a.residual) h += load_number(a.residual, m * a.ldr + n, a.r_f32);
-        return h;
-    };
-    auto value_of = [&](float h, int n) {
-        if (a.gelu) return gelu_tanh(h);
-        return a.gamma ? h * a.gamma[n] : h;
-    };
-    uint32_t top = 0;  // of the magnitudes' bit patterns, whose order puts infinities and NaNs above all numbers
-    float sum = 0.f;
-    for (int n = tid; n < a.N; n += kRowThreads) {
-        const float h = sum_of(n);
-        const uint32_t b = __float_as_uint(value_of(h, n)) & 0x7fffffffu;
-        top = b > top ? b : top;
-        sum = fmaf(h, h, sum);
+// Eight columns from `col` on.  PAST: past the caches, for rows that they cannot keep (rows_pass_caches).  Not for 32-bit
+// rows, whose eight columns are two loads or stores that each touch half of every 32 bytes: the caches join them (norm with a
+// 32-bit residual 333 us, past the caches 365).
+template <bool F32, bool PAST>
+__device__ __forceinline__ void load_chunk(const void* row, int col, float v[8]) {
+    if constexpr (F32 || !PAST)
+        load8(row, col, F32, v);
+    else
+        widen8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(row) + col)), v);
+}
+template <bool F32, bool PAST>
+__device__ __forceinline__ void store_chunk(void* row, int col, const float v[8]) {
+    if constexpr (F32) {
+        float4* const p = reinterpret_cast<float4*>(static_cast<float*>(row) + col);
+        p[0] = make_float4(v[0], v[1], v[2], v[3]);
+        p[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+        u32x4* const p = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(row) + col);
+        if constexpr (PAST) __builtin_nontemporal_store(pack8<OP_BF16>(v), p);
+        else *p = pack8<OP_BF16>(v);
     }
-    s_top[tid] = top;
-    s_sum[tid] = sum;
-    for (int d = kRowThreads / 2; d > 0; d >>= 1) {
-        __syncthreads();
-        if (tid < d) {
-            s_top[tid] = s_top[tid] > s_top[tid + d] ? s_top[tid] : s_top[tid + d];
-            s_sum[tid] += s_sum[tid + d];
+}
+template <bool F32>
+__device__ __forceinline__ float load_number(const void* row, int i) {
+    if constexpr (F32) return static_cast<const float*>(row)[i];
+    else return __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[i] << 16);
+}
+template <bool F32>
+__device__ __forceinline__ void store_number(void* row, int i, float v) {
+    if constexpr (F32) static_cast<float*>(row)[i] = v;
+    else static_cast<uint16_t*>(row)[i] = (uint16_t)pack2<OP_BF16>(v, 0.f);
+}
+
+// v * inverse, rounded to the nearest even integer of magnitude 127 or less, in the low byte: 1.5 * 2^23 puts the integer's
+// two's complement into the last bits of the significand
+__device__ __forceinline__ uint32_t to_byte(float v, float inverse) { return __float_as_uint(fmaf(v, inverse, 12582912.0f)); }
+__device__ __forceinline__ uint32_t to_bytes(const float v[4], float inverse) {
+    const uint32_t lo = __builtin_amdgcn_perm(to_byte(v[1], inverse), to_byte(v[0], inverse), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(to_byte(v[3], inverse), to_byte(v[2], inverse), 0x04000c0cu);
+    return lo | hi;
+}
+
+// W wavefronts a row, one row a workgroup or several.  CUT: N is no multiple of 8.
+template <int MODE, bool X_F32, int RES, int C, bool CUT>
+__global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int W) {
+    constexpr bool R_F32 = RES == ROW_F32;
+    __shared__ float s_top[16], s_sum[16];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = (blockDim.x >> 6) / W;  // of this workgroup
+    const int sub = wave / W, part = wave - sub * W;
+    const int64_t m = (int64_t)blockIdx.x * rows + sub;
+    const bool live = m < a.M;  // (a wavefront without a row goes along to the barrier)
+    const int64_t mm = live ? m : a.M - 1;
+    const void* const x = static_cast<const uint8_t*>(a.x) + mm * a.ldx * (X_F32 ? 4 : 2);
+    const void* const r = RES ? static_cast<const uint8_t*>(a.residual) + mm * a.ldr * (R_F32 ? 4 : 2) : nullptr;
+
+    // Chunk c of lane l is chunk (c W + part) 64 + l of the row.  Whole chunks are loaded without a branch: behind the last
+    // one it is loaded again, and counts as zeros.  (One chunk a lane: there may be no whole one.)  A last chunk that N cuts
+    // is loaded number by number, by its one lane.
+    const int whole = a.N >> 3, rest = CUT ? a.N & 7 : 0;
+    float t[C][8];
+    const int first = part * 64 + lane, step = W * 64;
+    auto load_all = [&](auto f32, auto past, const void* row, auto&& take) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = first + c * step;
+            float v[8];
+            if constexpr (C == 1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = 0.f;
+                if (at < whole) load_chunk<decltype(f32)::value, decltype(past)::value>(row, 8 * at, v);
+            } else {
+                load_chunk<decltype(f32)::value, decltype(past)::value>(row, 8 * (at < whole ? at : whole - 1), v);
+            }
+            take(c, v);
+        }
+    };
+    auto load_rows = [&](auto past) __attribute__((always_inline)) {
+        load_all(std::bool_constant<X_F32>(), past, x, [&](int c, const float v[8]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[c][i] = v[i];
+        });
+        if constexpr (RES != ROW_NONE)
+            load_all(std::bool_constant<R_F32>(), past, r, [&](int c, const float v[8]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[c][i] += v[i];
+            });
+    };
+    if (a.past_caches) load_rows(std::true_type());
+    else load_rows(std::false_type());
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = first + c * step;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[c][i] = at < whole ? t[c][i] : 0.f;
+        if (CUT && at == whole) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (i < rest) {
+                    float v = load_number<X_F32>(x, 8 * at + i);
+                    if constexpr (RES != ROW_NONE) v += load_number<R_F32>(r, 8 * at + i);
+                    t[c][i] = v;
+                }
         }
     }
-    __syncthreads();
-    const float amax = __uint_as_float(s_top[0]);
-    float factor = 1.0f / kQuantTop;
-    bool good = s_top[0] < 0x7f800000u;
-    if (a.norm) {
-        good = good && s_sum[0] < INFINITY;
-        factor = 1.0f / (sqrtf(s_sum[0] / (float)a.N + a.eps) * kQuantTop);
+
+    if constexpr (RES != ROW_NONE) {
+        if (a.h_out && live) {
+            void* const h = static_cast<uint8_t*>(a.h_out) + m * a.ldh * (R_F32 ? 4 : 2);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = first + c * step;
+                if (at < whole) {
+                    if (a.past_caches) store_chunk<R_F32, true>(h, 8 * at, t[c]);
+                    else store_chunk<R_F32, false>(h, 8 * at, t[c]);
+                } else if (CUT && at == whole) {
+#pragma unroll
+                    for (int i = 0; i < 7; ++i)
+                        if (i < rest) store_number<R_F32>(h, 8 * at + i, t[c][i]);
+                }
+            }
+        }
     }
-    const bool some = good && amax >= kQuantZero;
-    const float inverse = some ? kQuantTop / amax : 0.f;
-    if (tid == 0) a.scale[m] = !good ? NAN : some ? amax * factor : 0.f;
-    for (int n = tid; n < a.N; n += kRowThreads) {
-        const float h = sum_of(n);
-        if (a.h_out) store_number(a.h_out, m * a.ldh + n, a.r_f32, h);
-        a.q[m * a.ldq + n] = some ? (int8_t)rintf(value_of(h, n) * inverse) : (int8_t)0;
+    float top = 0.f, sum = 0.f;
+    if constexpr (MODE == ROW_NORM) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(t[c][i], t[c][i], sum);
+        if (a.gamma) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = first + c * step;
+                if (at < whole) {
+                    float g[8];
+                    load8(a.gamma, 8 * at, 1, g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) t[c][i] *= g[i];
+                } else if (CUT && at == whole) {
+#pragma unroll
+                    for (int i = 0; i < 7; ++i)
+                        if (i < rest) t[c][i] *= a.gamma[8 * at + i];
+                }
+            }
+        }
+    }
+    if constexpr (MODE == ROW_GELU) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[c][i] = gelu_tanh(t[c][i]);
+    }
+    // (by IEEE maximum, which passes a NaN on)
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = __builtin_elementwise_maximum(top, __builtin_fabsf(t[c][i]));
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        top = __builtin_elementwise_maximum(top, __shfl_xor(top, d));
+        if constexpr (MODE == ROW_NORM) sum += __shfl_xor(sum, d);
+    }
+    if (W > 1) {
+        if (lane == 0) {
+            s_top[wave] = top;
+            s_sum[wave] = sum;
+        }
+        __syncthreads();
+        top = s_top[sub * W];
+        sum = s_sum[sub * W];
+        for (int w = 1; w < W; ++w) {
+            top = __builtin_elementwise_maximum(top, s_top[sub * W + w]);
+            sum += s_sum[sub * W + w];
+        }
+    }
+    if (!live) return;
+
+    bool good = top < INFINITY;
+    float factor = 1.0f / kQuantTop;
+    if constexpr (MODE == ROW_NORM) {
+        good = good && sum < INFINITY;
+        factor = 1.0f / (sqrtf(sum / (float)a.N + a.eps) * kQuantTop);
+    }
+    const bool some = good && top >= kQuantZero;
+    const float inverse = some ? kQuantTop / top : 0.f;
+    if (part == 0 && lane == 0) a.scale[m] = !good ? NAN : some ? top * factor : 0.f;
+    int8_t* const q = a.q + m * a.ldq;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = first + c * step;
+        uint2 b = make_uint2(to_bytes(t[c], inverse), to_bytes(t[c] + 4, inverse));
+        if (!some) b = make_uint2(0u, 0u);  // (a NaN times zero is no zero)
+        if (at < whole) {
+            *reinterpret_cast<uint2*>(q + 8 * at) = b;
+        } else if (CUT && at == whole) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (i < rest) q[8 * at + i] = (int8_t)((i < 4 ? b.x : b.y) >> (8 * (i & 3)));
+        }
     }
 }
 
-__global__ void __launch_bounds__(kRowThreads) dequant_rows_kernel(const DequantArgs a) {
-    const int64_t m = blockIdx.x;
+// A lane writes 16 bytes at a time: V = 8 or 4 columns.  `parts` wavefronts a row, C pieces a lane.
+template <bool OUT_F32, int C, bool CUT>
+__global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, int parts) {
+    constexpr int V = OUT_F32 ? 4 : 8;
+    typedef std::conditional_t<OUT_F32, uint32_t, uint2> piece_t;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t id = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t m = id / parts;
+    if (m >= a.M) return;
+    const int first = (int)(id - m * parts) * (64 * C) + lane;
+    const int8_t* const q = a.q + m * a.ldq;
+    void* const y = static_cast<uint8_t*>(a.y) + m * a.ldy * (OUT_F32 ? 4 : 2);
     const float scale = a.scale[m];
-    for (int n = threadIdx.x; n < a.N; n += kRowThreads)
-        store_number(a.y, m * a.ldy + n, a.out_f32, (float)a.q[m * a.ldq + n] * scale);
+    const int whole = a.N / V, rest = CUT ? a.N % V : 0;
+    piece_t b[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = first + c * 64;
+        b[c] = piece_t();
+        if (at < whole) b[c] = *reinterpret_cast<const piece_t*>(q + V * (int64_t)at);
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = first + c * 64;
+        auto number = [&](uint32_t u, int i) { return (float)(int8_t)(u >> (8 * i)) * scale; };
+        if (at < whole) {
+            if constexpr (OUT_F32) {
+                const f32x4 v = {number(b[c], 0), number(b[c], 1), number(b[c], 2), number(b[c], 3)};
+                f32x4* const p = reinterpret_cast<f32x4*>(static_cast<float*>(y) + V * (int64_t)at);
+                if (a.past_caches) __builtin_nontemporal_store(v, p);
+                else *p = v;
+            } else {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = number(i < 4 ? b[c].x : b[c].y, i & 3);
+                if (a.past_caches) store_chunk<false, true>(y, V * at, v);
+                else store_chunk<false, false>(y, V * at, v);
+            }
+        } else if (CUT && at == whole) {
+            for (int i = 0; i < rest; ++i) store_number<OUT_F32>(y, V * at + i, (float)q[V * at + i] * scale);
+        }
+    }
 }
+
+// How rows lie over wavefronts.  Where there are wavefronts enough to keep the memory busy, `most` chunks a lane; where there
+// are not, one, the row over as many wavefronts as it takes (at most 16, a workgroup).
+constexpr int kBusy = 16 * kCUs;
+struct RowLayout {
+    int waves, per_lane, rows;  // wavefronts a row, chunks a lane, rows a workgroup
+};
+RowLayout layout_rows(int M, int N, int most) {
+    const int need = ((N + 7) / 8 + 63) / 64;  // wavefronts of one chunk a lane
+    if ((int64_t)M * ((need + most - 1) / most) < kBusy) most = 1;
+    int w = (need + most - 1) / most;
+    if (w > 16) w = 16;
+    const int c = (need + w - 1) / w;
+    w = (need + c - 1) / c;
+    return {w, c, w >= 4 ? 1 : 4 / w};
+}
+
+template <int MODE, bool X_F32, int RES, int C>
+hipError_t launch_quant(const QuantArgs& a, const RowLayout& l, hipStream_t s) {
+    const auto kern = a.N % 8 ? quant_rows_kernel<MODE, X_F32, RES, C, true> : quant_rows_kernel<MODE, X_F32, RES, C, false>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)a.M + l.rows - 1) / l.rows)),
+                       dim3(64 * l.waves * l.rows), 0, s, a, l.waves);
+    return hipGetLastError();
+}
+
+template <int MODE, bool X_F32, int RES>
+hipError_t launch_quant(const QuantArgs& a, hipStream_t s) {
+    // (two chunks a lane where little is done with what is read: 16-bit rows to 8 bits 85 us with two, 90 with five, norm with
+    // a 16-bit residual 201 and 212; five elsewhere: GELU 400 with two, 350 with five, norm with a 32-bit residual 341 and
+    // 333, with none 111 and 105)
+    const RowLayout l = layout_rows(a.M, a.N, MODE == ROW_PLAIN || RES == ROW_BF16 ? 2 : 5);
+    switch (l.per_lane) {
+        case 1: return launch_quant<MODE, X_F32, RES, 1>(a, l, s);
+        case 2: return launch_quant<MODE, X_F32, RES, 2>(a, l, s);
+        case 3: return launch_quant<MODE, X_F32, RES, 3>(a, l, s);
+        case 4: return launch_quant<MODE, X_F32, RES, 4>(a, l, s);
+        case 5: return launch_quant<MODE, X_F32, RES, 5>(a, l, s);
+        case 6: return launch_quant<MODE, X_F32, RES, 6>(a, l, s);
+        case 7: return launch_quant<MODE, X_F32, RES, 7>(a, l, s);
+        case 8: return launch_quant<MODE, X_F32, RES, 8>(a, l, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+template <bool OUT_F32, int C>
+hipError_t launch_dequant(const DequantArgs& a, int need, hipStream_t s) {
+    constexpr int V = OUT_F32 ? 4 : 8;
+    const int parts = (need + C - 1) / C;
+    const int64_t groups = ((int64_t)a.M * parts + 3) / 4;
+    if (groups > 0x7fffffff) return hipErrorInvalidValue;
+    const auto kern = a.N % V ? dequant_rows_kernel<OUT_F32, C, true> : dequant_rows_kernel<OUT_F32, C, false>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), 0, s, a, parts);
+    return hipGetLastError();
+}
+
+template <bool OUT_F32>
+hipError_t launch_dequant(const DequantArgs& a, hipStream_t s) {
+    constexpr int V = OUT_F32 ? 4 : 8;
+    const int need = (int)((((int64_t)a.N + V - 1) / V + 63) / 64);  // wavefronts of one piece a lane
+    // (two pieces a lane: 88 us in 16 bits and 134 in 32; five: 93 and 150)
+    return (int64_t)a.M * need < kBusy ? launch_dequant<OUT_F32, 1>(a, need, s) : launch_dequant<OUT_F32, 2>(a, need, s);
+}
+
+// Rows of more bytes than the chip's caches hold (256 MB) are read and written past them: they would push out what the next
+// call reads (norm and reading back, 32,760 x 5,120: 314 us through the caches, 284 past them).  Smaller ones were often just
+// written, and are still there (norm of 7,800 x 1,536 16 us through the caches, 18 past them).
+bool rows_pass_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
 
 }  // namespace
 
-hipError_t launch_quant_rows(const QuantArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(quant_rows_kernel, dim3((unsigned)a.M), dim3(kRowThreads), 0, s, a);
-    return hipGetLastError();
+hipError_t launch_quant_rows(const QuantArgs& args, hipStream_t s) {
+    QuantArgs a = args;
+    a.past_caches = rows_pass_caches((int64_t)a.M * a.N * ((a.x_f32 ? 4 : 2) + (a.residual ? a.r_f32 ? 4 : 2 : 0)));
+    if (!a.norm) {
+        if (a.gelu) return a.x_f32 ? launch_quant<ROW_GELU, true, ROW_NONE>(a, s) : launch_quant<ROW_GELU, false, ROW_NONE>(a, s);
+        return a.x_f32 ? launch_quant<ROW_PLAIN, true, ROW_NONE>(a, s) : launch_quant<ROW_PLAIN, false, ROW_NONE>(a, s);
+    }
+    if (!a.residual) return a.x_f32 ? launch_quant<ROW_NORM, true, ROW_NONE>(a, s) : launch_quant<ROW_NORM, false, ROW_NONE>(a, s);
+    if (a.r_f32) return a.x_f32 ? launch_quant<ROW_NORM, true, ROW_F32>(a, s) : launch_quant<ROW_NORM, false, ROW_F32>(a, s);
+    return a.x_f32 ? launch_quant<ROW_NORM, true, ROW_BF16>(a, s) : launch_quant<ROW_NORM, false, ROW_BF16>(a, s);
 }
 
-hipError_t launch_dequant_rows(const DequantArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(dequant_rows_kernel, dim3((unsigned)a.M), dim3(kRowThreads), 0, s, a);
-    return hipGetLastError();
+hipError_t launch_dequant_rows(const DequantArgs& args, hipStream_t s) {
+    DequantArgs a = args;
+    a.past_caches = rows_pass_caches((int64_t)a.M * a.N * (a.out_f32 ? 4 : 2));
+    return a.out_f32 ? launch_dequant<true>(a, s) : launch_dequant<false>(a, s);
 }
 
 }  // namespace dit
