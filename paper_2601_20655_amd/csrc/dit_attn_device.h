@@ -117,6 +117,54 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
     }
 }
 
+// The same shape on signed 8-bit integers, sixteen contraction indices a lane (16g .. 16g+15), 32-bit integer sums.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 mfma16_i8(u32x4 a, u32x4 b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
+
+// Accumulators of a projection's 16 x 16 block and one step of them.
+template <int OP>
+struct LinAcc {
+    typedef f32x4 type;
+    static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) { return mfma16<OP>(a, b, c); }
+};
+template <>
+struct LinAcc<OP_I8> {
+    typedef i32x4 type;
+    static __device__ __forceinline__ i32x4 mfma(u32x4 a, u32x4 b, i32x4 c) { return mfma16_i8(a, b, c); }
+};
+
+// Four features n .. n+3 (n a multiple of 4) of a projection's bias and of its weights' scales.  Those from N on are never
+// stored: unless N is CUT by four, the last four stand in for them; else they are zeros.
+template <bool CUT>
+__device__ __forceinline__ uint2 bias_of_4(const uint16_t* bias, int n, int N) {
+    if (!bias) return make_uint2(0u, 0u);
+    if (!CUT || n + 4 <= N) return *reinterpret_cast<const uint2*>(bias + (CUT || n < N ? n : N - 4));
+    uint32_t b[3];
+    for (int i = 0; i < 3; ++i) b[i] = n + i < N ? bias[n + i] : 0u;
+    return make_uint2(b[0] | (b[1] << 16), b[2]);
+}
+template <bool CUT>
+__device__ __forceinline__ f32x4 scales_of_4(const float* scale, int n, int N) {
+    if (!CUT || n + 4 <= N) return *reinterpret_cast<const f32x4*>(scale + (CUT || n < N ? n : N - 4));
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 3; ++i)
+        if (n + i < N) v[i] = scale[n + i];
+    return v;
+}
+
+// A 16-byte piece of an output row, columns n on, of which those from N on are not stored.
+template <bool F32>
+__device__ __forceinline__ void store_cut_piece(void* row, int n, int N, u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < (F32 ? 4 : 8); ++i) {
+        if (n + i >= N) return;
+        if constexpr (F32) static_cast<uint32_t*>(row)[n + i] = v[i];
+        else static_cast<uint16_t*>(row)[n + i] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
 // D(32x32, fp32) += 2^(sa-127) A(32x64, e4m3) * 2^(sb-127) B(64x32, e4m3).  Lane l supplies 32
 // contraction indices of row (l % 32) of A and of column (l % 32) of B, the same 32 indices on
 // both sides (group l / 32); sa and sb are the lane's own 8-bit scale codes for that row resp.

@@ -11,7 +11,7 @@ constexpr int kBK = 64;         // keys per K/V tile
 constexpr int kThreads = 256;   // four wavefronts per workgroup
 constexpr float kLog2e = 1.4426950408889634f;
 
-enum OperandType { OP_BF16 = 0, OP_F16 = 1, OP_FP8 = 2 };  // OP_FP8 (e4m3): score operands only
+enum OperandType { OP_BF16 = 0, OP_F16 = 1, OP_FP8 = 2, OP_I8 = 3 };  // OP_FP8 (e4m3): score operands only; OP_I8: projections only
 
 // One K/V tile as it sits in LDS (and, pre-packed, in workspace): 64 rows of K' followed by
 // D rows of V^T.  Rows carry 16 bytes of padding so that the 16-byte operand reads of 16
@@ -274,11 +274,19 @@ struct LinearArgs {
                                  // 2: over all heads of the token -- the weights here, the factor in k_rescale_kernel
     float qkv_eps;
     const float* qkv_kgamma;     // nullable [H*128]
+    // 8-bit operands: x and w hold pairs of signed 8-bit integers (K, ldx and ldw count pairs; K the whole steps only), the
+    // sums are integers, and y = sum * (x_scale * w_scale) + bias
+    const float* x_scale;  // [M]
+    const float* w_scale;  // [N]
+    int tail;              // 8-bit integers of a row behind the whole steps, 0 .. 127 (tiles of dit_linear_small.hip only)
 };
 hipError_t launch_linear(const LinearArgs& a, hipStream_t s);
+hipError_t launch_linear_i8(const LinearArgs& a, hipStream_t s);  // 256 x 256 tiles, 8-bit operands
 // plain projections that 256 x 256 tiles would leave most of the chip idle for (dit_linear_small.hip): which tile, 0 = none
 int choose_linear_form(int M, int N, int K, int cus);
 hipError_t launch_linear_small(const LinearArgs& a, int form, hipStream_t s);
+int choose_linear_form_i8(int M, int N, int K, bool big_too, int cus);  // 0 only with big_too
+hipError_t launch_linear_small_i8(const LinearArgs& a, int form, hipStream_t s);
 
 // Second half of the per-token normalisation of the fused q/k/v projection: the projection's epilogue left, in the
 // spare bytes behind the K' rows of every tile image, one float per key slot = the sum of squares of that token's k

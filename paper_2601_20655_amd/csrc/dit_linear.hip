@@ -59,10 +59,11 @@ __device__ __forceinline__ void static_for(F&& f) {
     }
 }
 
-template <bool OUT_F32, int QKV>
+template <int OP, bool OUT_F32, int QKV>
 __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearArgs a) {
     // QKV: 0 plain rows; 1 the fused q/k/v form; 2 the same with the k rows RMS-normalised per head; 3 with the
     // per-token normalisation's first half (weights applied, sums of squares left for k_rescale_kernel)
+    static_assert(OP == OP_BF16 || (OP == OP_I8 && !QKV), "operand types");
     static_assert(!(OUT_F32 && QKV), "the fused q/k/v form writes 16-bit rows and tiles");
     static_assert(kLinBM == 256 && kLinBN == 256 && kLinBK == 64, "tile shape");
     constexpr int SX = kLinSX;
@@ -184,13 +185,13 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     int lane_read = lr * ROWB + (lg ^ sw) * 16;
     const uint32_t xread = wt * BR * TB * ROWB, wread = kWBase + wf * BR * FB * ROWB;
 
-    f32x4 acc[FB][TB];
+    typename LinAcc<OP>::type acc[FB][TB];
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[fb][tb][r] = 0.f;
+            for (int r = 0; r < 4; ++r) acc[fb][tb][r] = 0;
 
     // Operand fragments.  A slice (32 contraction indices) takes FB fragments of w and TB of x and feeds
     // FB x TB MFMAs, walked by pairs of token blocks, both blocks of a pair on one w fragment before the next: of the
@@ -259,26 +260,61 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         const int lr = l & 15, lg = l >> 4, rrow = l / PR, rp = l % PR;
         const int n = tn * kLinBN + wf * BR * FB + rp * (16 / ES);
         uint2 bb[FB];
+        f32x4 ws[FB];  // (8-bit operands)
+        [[maybe_unused]] auto load_features = [&](int lgp) __attribute__((always_inline)) {
 #pragma unroll
-        for (int fb = 0; fb < FB; ++fb) {
-            const int n0 = tn * kLinBN + wf * BR * FB + fb * BR + 4 * lg;
-            bb[fb] = make_uint2(0u, 0u);
-            if (a.bias && n0 < a.N) bb[fb] = *reinterpret_cast<const uint2*>(a.bias + n0);
+            for (int fb = 0; fb < FB; ++fb) {
+                const int n0 = tn * kLinBN + wf * BR * FB + fb * BR + 4 * lgp;
+                bb[fb] = bias_of_4<false>(a.bias, n0, a.N);
+                ws[fb] = scales_of_4<false>(a.w_scale, n0, a.N);
+            }
+        };
+        if constexpr (OP == OP_I8) {
+            if constexpr (!OUT_F32) load_features(lg);
+        } else {
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb) {
+                const int n0 = tn * kLinBN + wf * BR * FB + fb * BR + 4 * lg;
+                bb[fb] = make_uint2(0u, 0u);
+                if (a.bias && n0 < a.N) bb[fb] = *reinterpret_cast<const uint2*>(a.bias + n0);
+            }
         }
         // (16-bit output only: with fp32 output the extra path costs the step loop a register)
         const bool full = !OUT_F32 && (tm + 1) * kLinBM <= a.M && (tn + 1) * kLinBN <= a.N;  // uniform
 #pragma unroll
         for (int pass = 0; pass < TB / TBP; ++pass) {
+            if constexpr (OP == OP_I8 && OUT_F32) {
+                // (read again in every pass: held through all of them they cost spills)
+                int lgp = lg;
+                asm volatile("" : "+v"(lgp));
+                load_features(lgp);
+            }
 #pragma unroll
             for (int h = 0; h < TBP; ++h) {
                 const int tb = pass * TBP + h;
                 const int row = BR * h + lr;
+                float xs = 1.f;
+                if constexpr (OP == OP_I8) {
+                    const int m = tm * kLinBM + (wt * TB + tb) * BR + lr;
+                    xs = a.x_scale[m < a.M ? m : a.M - 1];
+                }
 #pragma unroll
                 for (int fb = 0; fb < FB; ++fb) {
                     const float b0 = __uint_as_float(bb[fb].x << 16), b1 = __uint_as_float(bb[fb].x & 0xffff0000u);
                     const float b2 = __uint_as_float(bb[fb].y << 16), b3 = __uint_as_float(bb[fb].y & 0xffff0000u);
-                    const float y0 = acc[fb][tb][0] + b0, y1 = acc[fb][tb][1] + b1;
-                    const float y2 = acc[fb][tb][2] + b2, y3 = acc[fb][tb][3] + b3;
+                    float y0, y1, y2, y3;
+                    if constexpr (OP == OP_I8) {
+                        // (the sum is rounded to fp32 here, a relative 2^-24)
+                        y0 = fmaf((float)acc[fb][tb][0], xs * ws[fb][0], b0);
+                        y1 = fmaf((float)acc[fb][tb][1], xs * ws[fb][1], b1);
+                        y2 = fmaf((float)acc[fb][tb][2], xs * ws[fb][2], b2);
+                        y3 = fmaf((float)acc[fb][tb][3], xs * ws[fb][3], b3);
+                    } else {
+                        y0 = acc[fb][tb][0] + b0;
+                        y1 = acc[fb][tb][1] + b1;
+                        y2 = acc[fb][tb][2] + b2;
+                        y3 = acc[fb][tb][3] + b3;
+                    }
                     const int col = (BR * fb + 4 * lg) * ES;
                     uint8_t* const dst = region + row * RB + (((col >> 4) ^ (row & (PR - 1))) << 4) + (col & 15);
                     if constexpr (OUT_F32) *reinterpret_cast<float4*>(dst) = make_float4(y0, y1, y2, y3);
@@ -330,7 +366,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[fb][tb][r] = 0.f;
+                for (int r = 0; r < 4; ++r) acc[fb][tb][r] = 0;
         __builtin_amdgcn_s_barrier();
     };
 
@@ -596,7 +632,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
             }
             static_for<0, 2 * FB>([&](auto mc) __attribute__((always_inline)) {
                 constexpr int m = decltype(mc)::value, fb = m >> 1, tb = T + (m & 1);
-                acc[fb][tb] = mfma16<OP_BF16>(W[cur][fb], X[tb], acc[fb][tb]);
+                acc[fb][tb] = LinAcc<OP>::mfma(W[cur][fb], X[tb], acc[fb][tb]);
                 __builtin_amdgcn_sched_barrier(0);
                 // the x fragments of the pair before: their MFMAs have issued
                 if constexpr (m < 2) {
@@ -633,7 +669,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         wb = wb_next;
         if constexpr (LOADS) next_load_step();
         if (++kt == nK) {
-            if constexpr (QKV) store_tile_qkv(tm, tn, xb == 0 ? SX - 1 : xb - 1);
+            if constexpr (QKV != 0) store_tile_qkv(tm, tn, xb == 0 ? SX - 1 : xb - 1);
             else store_tile(tm, tn, xb == 0 ? SX - 1 : xb - 1);
             // The per-lane fragment offset is worked out again behind every store of a tile, from a lane number the
             // compiler cannot see through: it is then a new value here, not one that has to survive the store, which
@@ -658,9 +694,9 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last steps
 }
 
-template <bool OUT_F32, int QKV>
+template <int OP, bool OUT_F32, int QKV>
 hipError_t launch_linear_inst(const LinearArgs& a, int cus, hipStream_t s) {
-    auto kern = linear_kernel<OUT_F32, QKV>;
+    auto kern = linear_kernel<OP, OUT_F32, QKV>;
     constexpr int smem = (kLinSX + kLinSW) * kLinTileBytes;
     static std::atomic<uint64_t> attr_set{0};
     hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
@@ -679,11 +715,18 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     const hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
     if (a.qkv) {
-        if (a.qkv_norm == 2) return launch_linear_inst<false, 3>(a, cus, s);
-        return a.qkv_norm ? launch_linear_inst<false, 2>(a, cus, s) : launch_linear_inst<false, 1>(a, cus, s);
+        if (a.qkv_norm == 2) return launch_linear_inst<OP_BF16, false, 3>(a, cus, s);
+        return a.qkv_norm ? launch_linear_inst<OP_BF16, false, 2>(a, cus, s) : launch_linear_inst<OP_BF16, false, 1>(a, cus, s);
     }
     if (const int form = choose_linear_form(a.M, a.N, a.K, cus)) return launch_linear_small(a, form, s);
-    return a.out_f32 ? launch_linear_inst<true, false>(a, cus, s) : launch_linear_inst<false, false>(a, cus, s);
+    return a.out_f32 ? launch_linear_inst<OP_BF16, true, 0>(a, cus, s) : launch_linear_inst<OP_BF16, false, 0>(a, cus, s);
+}
+
+hipError_t launch_linear_i8(const LinearArgs& a, hipStream_t s) {
+    int cus = 0;
+    const hipError_t e = compute_units(&cus);
+    if (e != hipSuccess) return e;
+    return a.out_f32 ? launch_linear_inst<OP_I8, true, 0>(a, cus, s) : launch_linear_inst<OP_I8, false, 0>(a, cus, s);
 }
 
 }  // namespace dit

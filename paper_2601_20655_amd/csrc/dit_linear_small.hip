@@ -45,10 +45,12 @@ struct LinTile {
     static constexpr int FULL = FB + TB / 2, LOADS = FULL + (TB & 1);
 };
 
-template <int TB, int FB, bool OUT_F32>
+// ANY (8-bit operands): N is no multiple of 8, or integers are left behind the whole steps.
+template <int OP, int TB, int FB, bool OUT_F32, bool ANY>
 __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_tile_kernel(const LinearArgs a) {
     using T = LinTile<TB, FB>;
     constexpr int S = T::S;
+    static_assert(OP == OP_I8 || !ANY, "16-bit operands come in whole pieces");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -83,13 +85,13 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
 #pragma unroll
     for (int i = 0; i < FULL; ++i) src[i] = src_of(wave + 8 * i);
     if constexpr (TB & 1) src[FULL] = src_of(8 * FULL + (wave >> 1));  // half a chunk per wavefront
-    f32x4 acc[FB][TB];
+    typename LinAcc<OP>::type acc[FB][TB];
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[fb][tb][r] = 0.f;
+            for (int r = 0; r < 4; ++r) acc[fb][tb][r] = 0;
 
     const int sw = (lr >> 1) & 7;
     const int wread = (wf * 16 * FB + lr) * 128;
@@ -124,21 +126,23 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
                 __builtin_amdgcn_global_load_lds((gptr_t)src[I], (lptr_t)(dst + (8 * FULL + (wave >> 1)) * 1024), 16, 0, 0);
         }
     };
-#pragma unroll
-    for (int s = 0; s < S - 1; ++s) {
-        static_for<0, T::LOADS>([&](auto i) __attribute__((always_inline)) { request_piece(i, s); });
-        ++requested;
-    }
-    sync_stage();
     u32x4 W0[FB], X0[TB], W1[FB], X1[TB];
     constexpr int R = FB + TB;  // fragments of a slice
-    static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W0, X0, i, 0, 0); });
     // While one slice is multiplied, token block by token block, the next one is read: nothing ahead of the first block
     // (the wait for its own fragments would wait for what was just asked for too) nor of the last one (whose MFMAs
     // cover the youngest reads), PER fragments ahead of each block between.  (Left to the compiler the reads sank
     // behind the MFMAs and were waited for there: 641 x 3,320 x 1,664 14.6 -> 12.8 us, 3,600 x 5,120 x 5,120 166 -> 159.)
     constexpr int GAPS = TB > 2 ? TB - 2 : 1, PER = (R + GAPS - 1) / GAPS, LPER = (T::LOADS + GAPS - 1) / GAPS;
     int stage = 0, free_stage = S - 1;
+    if (!ANY || nK > 0) {
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) {
+            static_for<0, T::LOADS>([&](auto i) __attribute__((always_inline)) { request_piece(i, s); });
+            ++requested;
+        }
+        sync_stage();
+        static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W0, X0, i, 0, 0); });
+    }
     for (int k = 0; k < nK; ++k) {
         const int next = stage + 1 == S ? 0 : stage + 1;
         auto slice = [&](u32x4 (&W)[FB], u32x4 (&X)[TB], u32x4 (&Wn)[FB], u32x4 (&Xn)[TB], int nstage, auto ksn) __attribute__((always_inline)) {
@@ -156,7 +160,7 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
                     __builtin_amdgcn_sched_barrier(0);
                 }
 #pragma unroll
-                for (int fb = 0; fb < FB; ++fb) acc[fb][tb] = mfma16<OP_BF16>(W[fb], X[tb], acc[fb][tb]);
+                for (int fb = 0; fb < FB; ++fb) acc[fb][tb] = LinAcc<OP>::mfma(W[fb], X[tb], acc[fb][tb]);
                 __builtin_amdgcn_sched_barrier(0);
                 // step k + 1 has arrived, everybody has read step k (its fragments have been waited for)
                 if constexpr (KSN == 0 && tb == 0) sync_stage();
@@ -176,6 +180,37 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    // ---- what is left of K: one more step, staged through registers, the bytes behind the rows' ends zeros
+    if constexpr (ANY) {
+        if (a.tail > 0) {
+            for (int p = tid; p < (T::BN + T::BM) * 8; p += 512) {
+                const int line = p >> 3, r = line < T::BN ? line : line - T::BN;
+                const int at = 16 * ((p & 7) ^ ((r >> 1) & 7));
+                const bool is_w = line < T::BN;
+                const int row0 = is_w ? tn * T::BN : tm * T::BM, end = is_w ? a.N : a.M;
+                const int row = row0 + r < end ? row0 + r : end - 1;
+                const uint16_t* const from = (is_w ? a.w + (int64_t)row * a.ldw : a.x + (int64_t)row * a.ldx) + a.K;
+                u32x4 v = mk4(0u, 0u, 0u, 0u);
+                if (at < a.tail) v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(from) + at);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int bits = 8 * (a.tail - at - 4 * i);  // of this dword, those that count
+                    v[i] = bits <= 0 ? 0u : bits < 32 ? v[i] & ((1u << bits) - 1u) : v[i];
+                }
+                *reinterpret_cast<u32x4*>(smem + 16 * p) = v;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W0, X0, i, 0, ks); });
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                    for (int fb = 0; fb < FB; ++fb) acc[fb][tb] = LinAcc<OP>::mfma(W0[fb], X0[tb], acc[fb][tb]);
+            }
+            __syncthreads();
+        }
+    }
 
     // ---- store: 16 token rows at a time through an area of the wavefront's own, so that rows leave in 16-byte pieces
     // (Tried: non-temporal stores.  769 x 10,240 x 5,120 72.1 -> 70.6 us on the operands of the call before, 89.4 ->
@@ -190,11 +225,17 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     // where piece c of staged row r lies: spread over the banks by the row number
     auto slot = [](int r, int c) { return c ^ (r & (PR - 1)); };
     float b[FB][4];
+    f32x4 ws[FB];  // (8-bit operands)
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb) {
         const int n0 = tn * T::BN + (wf * FB + fb) * 16 + 4 * lg;
         uint2 bb = make_uint2(0u, 0u);
-        if (a.bias && n0 < a.N) bb = *reinterpret_cast<const uint2*>(a.bias + n0);
+        if constexpr (OP == OP_I8) {
+            bb = bias_of_4<ANY>(a.bias, n0, a.N);
+            ws[fb] = scales_of_4<ANY>(a.w_scale, n0, a.N);
+        } else {
+            if (a.bias && n0 < a.N) bb = *reinterpret_cast<const uint2*>(a.bias + n0);
+        }
         b[fb][0] = bf16_lo(bb.x);
         b[fb][1] = bf16_hi(bb.x);
         b[fb][2] = bf16_lo(bb.y);
@@ -202,10 +243,26 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     }
 #pragma unroll
     for (int tb = 0; tb < TB; ++tb) {
+        float xs = 1.f;
+        if constexpr (OP == OP_I8) {
+            const int m = tm * T::BM + (wt * TB + tb) * 16 + lr;
+            xs = a.x_scale[m < a.M ? m : a.M - 1];
+        }
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb) {
-            const float y0 = acc[fb][tb][0] + b[fb][0], y1 = acc[fb][tb][1] + b[fb][1];
-            const float y2 = acc[fb][tb][2] + b[fb][2], y3 = acc[fb][tb][3] + b[fb][3];
+            float y0, y1, y2, y3;
+            if constexpr (OP == OP_I8) {
+                // (the sum is rounded to fp32 here, a relative 2^-24)
+                y0 = fmaf((float)acc[fb][tb][0], xs * ws[fb][0], b[fb][0]);
+                y1 = fmaf((float)acc[fb][tb][1], xs * ws[fb][1], b[fb][1]);
+                y2 = fmaf((float)acc[fb][tb][2], xs * ws[fb][2], b[fb][2]);
+                y3 = fmaf((float)acc[fb][tb][3], xs * ws[fb][3], b[fb][3]);
+            } else {
+                y0 = acc[fb][tb][0] + b[fb][0];
+                y1 = acc[fb][tb][1] + b[fb][1];
+                y2 = acc[fb][tb][2] + b[fb][2];
+                y3 = acc[fb][tb][3] + b[fb][3];
+            }
             const int col = (16 * fb + 4 * lg) * ES;
             uint8_t* const dst = area + lr * RB + slot(lr, col >> 4) * 16 + (col & 15);
             if constexpr (OUT_F32) *reinterpret_cast<float4*>(dst) = make_float4(y0, y1, y2, y3);
@@ -218,9 +275,15 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
             const int r = p / PR, c = p % PR;
             const int m = tm * T::BM + (wt * TB + tb) * 16 + r;
             const int n = tn * T::BN + wf * FB * 16 + c * (16 / ES);
-            // N is a multiple of 8: a piece of a row is inside or outside as a whole
+            // (N a multiple of 8: a piece of a row is inside or outside as a whole)
             if ((NP >= 64 || p < NP) && m < a.M && n < a.N) {
                 const u32x4 v = *reinterpret_cast<const u32x4*>(area + r * RB + slot(r, c) * 16);
+                if constexpr (ANY) {
+                    if (n + 16 / ES > a.N) {
+                        store_cut_piece<OUT_F32>(static_cast<uint8_t*>(a.y) + (int64_t)m * a.ldy * ES, n, a.N, v);
+                        continue;
+                    }
+                }
                 *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES) = v;
             }
         }
@@ -228,10 +291,10 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     }
 }
 
-template <int TB, int FB, bool OUT_F32>
+template <int OP, int TB, int FB, bool OUT_F32, bool ANY>
 hipError_t launch_tile(LinearArgs a, hipStream_t s) {
     using T = LinTile<TB, FB>;
-    auto kern = linear_tile_kernel<TB, FB, OUT_F32>;
+    auto kern = linear_tile_kernel<OP, TB, FB, OUT_F32, ANY>;
     constexpr int smem = T::S * T::STAGE;
     static std::atomic<uint64_t> attr_set{0};
     hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
@@ -255,18 +318,13 @@ struct Form {
 constexpr Form kForms[] = {{1, 1, 0.20, 0.35, 2.5}, {2, 1, 0.215, 0.36, 2.5}, {2, 2, 0.33, 0.55, 3.0}, {4, 2, 0.47, 0.0, 3.0},
                            {3, 4, 0.74, 0.0, 3.5},  {4, 4, 0.76, 0.0, 4.0},   {5, 4, 1.05, 0.0, 4.0}};
 
-}  // namespace
-
-// The tile the estimate says is fastest (10 TB + FB), 0 for the big kernel, which keeps what is not 5 % slower there.
-// Measured, us a call one after the other on the same operands: M x N x K = 769 x 10,240 x 5,120: 98 in 256 x 256 tiles
-// (160 of them), 80 in 160 x 256 (with other work between the calls 98 and 88); 769 x 5,120 x 5,120: 82 and 56 (96 x 256);
-// 512 x 3,072 x 1,536: 28 and 9 (64 x 128); 172 x 3,664 x 3,072: 51 and 11 (64 x 64); 1 x 15,360 x 5,120: 80 and 23;
-// 3,600 x 5,120 x 5,120: 193 and 161 (160 x 256); kept: 14,040 x 1,536 x 1,536 (66), 3,600 x 15,360 x 5,120 (430).
-int choose_linear_form(int M, int N, int K, int cus) {
-    const double nK = K / kLinBK;
+// The tile the estimate says is fastest for nK steps (10 TB + FB), 0 for the big kernel, which keeps what is not 5 % slower
+// there (and is left out of it without `big_too`).
+int best_form(int M, int N, double nK, int cus, bool big_too) {
     auto tiles_of = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const int64_t big = tiles_of(kLinBM, kLinBN), full = big / cus, rest = big % cus;
     double best = 0.95 * (7.0 + full * (1.2 * nK + 3.5) + (rest == 0 ? 0.0 : (rest <= cus / 2 ? 1.0 : 1.2) * nK + 3.5));
+    if (!big_too) best = 1e30;
     int form = 0;
     for (const Form& f : kForms) {
         const int64_t tiles = tiles_of(32 * f.tb, 64 * f.fb);
@@ -283,9 +341,42 @@ int choose_linear_form(int M, int N, int K, int cus) {
     return form;
 }
 
+}  // namespace
+
+// Measured, us a call one after the other on the same operands: M x N x K = 769 x 10,240 x 5,120: 98 in 256 x 256 tiles
+// (160 of them), 80 in 160 x 256 (with other work between the calls 98 and 88); 769 x 5,120 x 5,120: 82 and 56 (96 x 256);
+// 512 x 3,072 x 1,536: 28 and 9 (64 x 128); 172 x 3,664 x 3,072: 51 and 11 (64 x 64); 1 x 15,360 x 5,120: 80 and 23;
+// 3,600 x 5,120 x 5,120: 193 and 161 (160 x 256); kept: 14,040 x 1,536 x 1,536 (66), 3,600 x 15,360 x 5,120 (430).
+int choose_linear_form(int M, int N, int K, int cus) { return best_form(M, N, K / kLinBK, cus, true); }
+
 hipError_t launch_linear_small(const LinearArgs& a, int form, hipStream_t s) {
 #define DIT_TILE(TB, FB) \
-    if (form == 10 * TB + FB) return a.out_f32 ? launch_tile<TB, FB, true>(a, s) : launch_tile<TB, FB, false>(a, s);
+    if (form == 10 * TB + FB)       \
+        return a.out_f32 ? launch_tile<OP_BF16, TB, FB, true, false>(a, s) : launch_tile<OP_BF16, TB, FB, false, false>(a, s);
+    DIT_TILE(1, 1)
+    DIT_TILE(2, 1)
+    DIT_TILE(2, 2)
+    DIT_TILE(4, 2)
+    DIT_TILE(3, 4)
+    DIT_TILE(4, 4)
+    DIT_TILE(5, 4)
+#undef DIT_TILE
+    return hipErrorInvalidValue;
+}
+
+// A step of 8-bit operands is the same bytes and the same number of matrix instructions of the same length as one of 16-bit
+// operands, of twice the contraction indices: the same estimates.
+int choose_linear_form_i8(int M, int N, int K, bool big_too, int cus) {
+    return best_form(M, N, (K + 127) / 128, cus, big_too);
+}
+
+hipError_t launch_linear_small_i8(const LinearArgs& a, int form, hipStream_t s) {
+    const bool any = a.tail > 0 || a.N % 8 != 0;
+#define DIT_TILE(TB, FB)                                                                                            \
+    if (form == 10 * TB + FB) {                                                                                     \
+        if (any) return a.out_f32 ? launch_tile<OP_I8, TB, FB, true, true>(a, s) : launch_tile<OP_I8, TB, FB, false, true>(a, s); \
+        return a.out_f32 ? launch_tile<OP_I8, TB, FB, true, false>(a, s) : launch_tile<OP_I8, TB, FB, false, false>(a, s);        \
+    }
     DIT_TILE(1, 1)
     DIT_TILE(2, 1)
     DIT_TILE(2, 2)
