@@ -59,11 +59,12 @@ __device__ __forceinline__ void static_for(F&& f) {
     }
 }
 
-template <int OP, bool OUT_F32, int QKV>
+// TAIL (8-bit operands): integers are left behind the whole steps (a.tail), and make one more
+template <int OP, bool OUT_F32, int QKV, bool TAIL = false>
 __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearArgs a) {
     // QKV: 0 plain rows; 1 the fused q/k/v form; 2 the same with the k rows RMS-normalised per head; 3 with the
     // per-token normalisation's first half (weights applied, sums of squares left for k_rescale_kernel)
-    static_assert(OP == OP_BF16 || (OP == OP_I8 && !QKV), "operand types");
+    static_assert(OP == OP_BF16 ? !TAIL : OP == OP_I8 && !QKV, "operand types");
     static_assert(!(OUT_F32 && QKV), "the fused q/k/v form writes 16-bit rows and tiles");
     static_assert(kLinBM == 256 && kLinBN == 256 && kLinBK == 64, "tile shape");
     constexpr int SX = kLinSX;
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     // chunk (chunks are 32 rows apart, the swizzle has period 16 rows): two registers instead of a table
     // of sixteen.  The tile base and the step's column offset are wavefront-uniform.
     // The loads run two steps ahead of the MFMAs, so they have a tile and a step of their own.
-    const int nK = a.K / kLinBK;
+    const int nK = a.K / kLinBK + (TAIL ? 1 : 0);
     const int load_row0 = 8 * (wave & (NLW - 1)) + (lane >> 3);
     const uint32_t load_piece = 16u * ((lane & 7) ^ ((load_row0 >> 1) & 7));
     const uint32_t ldx2 = (uint32_t)(a.ldx * 2), ldw2 = (uint32_t)(a.ldw * 2);
@@ -155,7 +156,12 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         asm volatile("" : "+v"(r));
         r += 8 * NLW * i;
         r = r < row_max ? r : row_max;
-        uint32_t o = (uint32_t)r * ld2 + load_piece;
+        uint32_t piece = load_piece;
+        if constexpr (TAIL) {  // in a tile's last step no further than the row's last piece
+            const uint32_t last = load_kt + 1 == nK ? (uint32_t)(a.tail - 1) & ~15u : 112u;
+            piece = piece < last ? piece : last;
+        }
+        uint32_t o = (uint32_t)r * ld2 + piece;
         asm volatile("" : "+v"(o));
         __builtin_amdgcn_global_load_lds((gptr_t)(tile + load_kt * (kLinBK * 2) + o),
                                          (lptr_t)(smem + lds_byte + ((wave & (NLW - 1)) + i * NLW) * 1024), 16, 0, 0);
@@ -235,6 +241,29 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    // Behind the end of the rows the w tile of a tile's last step holds something else, and what the x tile holds there is
+    // multiplied by it: zeros are written over it (integers: zero times anything is zero).  A loading wavefront mends
+    // the 64 rows it has fetched itself, one a lane, before the barrier that hands the tile on.
+    auto mend_w = [&](int buf) __attribute__((always_inline)) {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        const int r = 8 * ((wave & (NLW - 1)) + NLW * (l >> 3)) + (l & 7);
+        uint8_t* const row = smem + kWBase + buf * kLinTileBytes + r * ROWB;
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NCH) : "memory");
+        for (int p = a.tail >> 4; p < 8; ++p) {
+            u32x4* const at = reinterpret_cast<u32x4*>(row + 16 * (p ^ ((r >> 1) & 7)));
+            u32x4 v = mk4(0u, 0u, 0u, 0u);
+            if (p == a.tail >> 4 && (a.tail & 15)) {
+                v = *at;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int bits = 8 * ((a.tail & 15) - 4 * i);  // of this dword, those that count
+                    v[i] = bits <= 0 ? 0u : bits < 32 ? v[i] & ((1u << bits) - 1u) : v[i];
+                }
+            }
+            *at = v;
+        }
+    };
     // ---- store of a finished tile.  A lane holds token (column lr of block tb) and four consecutive features
     // per accumulator (16 fb + 4 lg + e of its wavefront's 64), so stored from the accumulators a wavefront
     // instruction would write sixteen 32-byte pieces, and a tile's 4,096 such pieces held the stream up for a
@@ -261,6 +290,8 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         const int n = tn * kLinBN + wf * BR * FB + rp * (16 / ES);
         uint2 bb[FB];
         f32x4 ws[FB];  // (8-bit operands)
+        // (read again in every pass where holding them through all of them costs spills)
+        constexpr bool REREAD = OP == OP_I8 && (OUT_F32 || TAIL);
         [[maybe_unused]] auto load_features = [&](int lgp) __attribute__((always_inline)) {
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
@@ -270,7 +301,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
             }
         };
         if constexpr (OP == OP_I8) {
-            if constexpr (!OUT_F32) load_features(lg);
+            if constexpr (!REREAD) load_features(lg);
         } else {
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
@@ -283,8 +314,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         const bool full = !OUT_F32 && (tm + 1) * kLinBM <= a.M && (tn + 1) * kLinBN <= a.N;  // uniform
 #pragma unroll
         for (int pass = 0; pass < TB / TBP; ++pass) {
-            if constexpr (OP == OP_I8 && OUT_F32) {
-                // (read again in every pass: held through all of them they cost spills)
+            if constexpr (REREAD) {
                 int lgp = lg;
                 asm volatile("" : "+v"(lgp));
                 load_features(lgp);
@@ -597,6 +627,9 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     dma_w(0);
     next_load_step();
     dma_x(1);
+    if constexpr (TAIL) {
+        if (nK == 1 && loader) mend_w(0);
+    }
     sync_point();
     dma_w(1);
     next_load_step();
@@ -641,7 +674,12 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 }
                 // (after the last step the loads and reads behind this barrier go to buffers nobody uses:
                 // uniform control flow)
-                if constexpr (last && P == 0 && m == 4) sync_point();
+                if constexpr (last && P == 0 && m == 4) {
+                    if constexpr (TAIL && LOADS) {
+                        if ((kt + 1 == nK ? 0 : kt + 1) + 1 == nK) mend_w(wb_next);
+                    }
+                    sync_point();
+                }
                 // the next slice's w fragments, two at a time (behind the barrier in the last slice)
                 if constexpr (P == 0 && (m == 4 || m == 6)) {
                     constexpr int wi = m - 4;
@@ -694,9 +732,9 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last steps
 }
 
-template <int OP, bool OUT_F32, int QKV>
+template <int OP, bool OUT_F32, int QKV, bool TAIL = false>
 hipError_t launch_linear_inst(const LinearArgs& a, int cus, hipStream_t s) {
-    auto kern = linear_kernel<OP, OUT_F32, QKV>;
+    auto kern = linear_kernel<OP, OUT_F32, QKV, TAIL>;
     constexpr int smem = (kLinSX + kLinSW) * kLinTileBytes;
     static std::atomic<uint64_t> attr_set{0};
     hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
@@ -726,6 +764,8 @@ hipError_t launch_linear_i8(const LinearArgs& a, hipStream_t s) {
     int cus = 0;
     const hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
+    if (a.tail > 0)
+        return a.out_f32 ? launch_linear_inst<OP_I8, true, 0, true>(a, cus, s) : launch_linear_inst<OP_I8, false, 0, true>(a, cus, s);
     return a.out_f32 ? launch_linear_inst<OP_I8, true, 0>(a, cus, s) : launch_linear_inst<OP_I8, false, 0>(a, cus, s);
 }
 

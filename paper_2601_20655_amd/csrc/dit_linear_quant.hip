@@ -1,14 +1,15 @@
 // Projection of 8-bit rows: y[m, n] = (sum_k x[m, k] w[n, k]) * (x_scale[m] * w_scale[n]) + bias[n], the sum an exact 32-bit
 // integer on the matrix cores.  Few token rows are done here, straight from memory; more by the tiles of dit_linear.hip and
 // dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
+#ifdef SWEEP
+#include <stdlib.h>
+#endif
 #include "dit_attn_device.h"
 #include "dit_attn_internal.h"
 
 namespace dit {
 
 namespace {
-
-constexpr int kFewWaves = 8;
 
 // 16 bytes of a row from byte `at` on, those from `end` on zeros.
 __device__ __forceinline__ u32x4 load_cut_piece(const int8_t* row, int at, int end) {
@@ -22,75 +23,139 @@ __device__ __forceinline__ u32x4 load_cut_piece(const int8_t* row, int at, int e
     return v;
 }
 
-// A workgroup takes 16 features and all token rows (16 TB at most); its wavefronts share K in blocks of 128.  w rows ride the
-// A operand of v_mfma_i32_16x16x64_i8, token rows the B operand, both straight from memory: a lane (i, g) holds 16
-// bytes of row i and ends with token i, features 4 g .. 4 g + 3.
-template <int TB, bool OUT_F32>
-__global__ void __launch_bounds__(64 * kFewWaves) linear_few_kernel(const LinearQuantArgs a) {
-    __shared__ i32x4 part[kFewWaves][TB][64];
+typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
+
+// Few token rows: XI groups of 8.  A workgroup takes all of them and F features, WI groups of 8 (the last one may be cut); its
+// NW wavefronts share K in blocks of 128 bytes, one after the other, and add their sums at the end.  A wavefront streams its
+// blocks through S stages of LDS of its own: the load-to-LDS DMA moves 8 rows of a block an instruction, whole lines, and no
+// wavefront waits for another before the end.
+template <int XI, int WI, int NW, int S>
+struct FewTile {
+    static constexpr int TB = (XI + 1) / 2, FB = (WI + 1) / 2;  // 16-token and 16-feature blocks
+    static constexpr int LOADS = WI + XI;                       // DMA instructions of a block
+    static constexpr int STAGE = 2048 * (FB + TB);
+    static constexpr int RING = NW * S * STAGE, SUMS = NW * FB * TB * 1024;
+    static constexpr int LDS = RING > SUMS ? RING : SUMS;
+};
+
+// the FB + TB fragments of one half block, waited for
+template <int N>
+__device__ __forceinline__ void read_fragments(u32x4 (&f)[N], uint32_t at) {
+    static_assert(N >= 2 && N <= 6, "fragments of a half block");
+    if constexpr (N == 2) {
+        asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:2048\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f[0]), "=&v"(f[1]) : "v"(at) : "memory");
+    } else if constexpr (N == 3) {
+        asm volatile("ds_read_b128 %0, %3\n\tds_read_b128 %1, %3 offset:2048\n\tds_read_b128 %2, %3 offset:4096\n\t"
+                     "s_waitcnt lgkmcnt(0)" : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]) : "v"(at) : "memory");
+    } else if constexpr (N == 4) {
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:2048\n\tds_read_b128 %2, %4 offset:4096\n\t"
+                     "ds_read_b128 %3, %4 offset:6144\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]) : "v"(at) : "memory");
+    } else if constexpr (N == 5) {
+        asm volatile("ds_read_b128 %0, %5\n\tds_read_b128 %1, %5 offset:2048\n\tds_read_b128 %2, %5 offset:4096\n\t"
+                     "ds_read_b128 %3, %5 offset:6144\n\tds_read_b128 %4, %5 offset:8192\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]) : "v"(at) : "memory");
+    } else {
+        asm volatile("ds_read_b128 %0, %6\n\tds_read_b128 %1, %6 offset:2048\n\tds_read_b128 %2, %6 offset:4096\n\t"
+                     "ds_read_b128 %3, %6 offset:6144\n\tds_read_b128 %4, %6 offset:8192\n\t"
+                     "ds_read_b128 %5, %6 offset:10240\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]) : "v"(at) : "memory");
+    }
+}
+
+template <int XI, int WI, int NW, int S, bool OUT_F32>
+__global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantArgs a, int F) {
+    using T = FewTile<XI, WI, NW, S>;
+    constexpr int TB = T::TB, FB = T::FB;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 15, lg = lane >> 4;
-    const int n0 = blockIdx.x * 16;
-    // (rows past the end are the last one again: their sums are not stored)
-    const int8_t* const wrow = a.w + (int64_t)(n0 + lr < a.N ? n0 + lr : a.N - 1) * a.ldw;
-    const int8_t* xrow[TB];
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) xrow[tb] = a.x + (int64_t)(16 * tb + lr < a.M ? 16 * tb + lr : a.M - 1) * a.ldx;
-    i32x4 acc[TB];
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) acc[tb] = i32x4{0, 0, 0, 0};
+    const int n0 = blockIdx.x * F, n1 = n0 + F < a.N ? n0 + F : a.N;  // its features
 
-    const int blocks = a.K >> 7;
-    constexpr int U = 4;
-    int b = wave;
-    for (; b + (U - 1) * kFewWaves < blocks; b += U * kFewWaves) {
-        u32x4 w[U][2], x[U][2][TB];
+    // DMA sources: 8 rows of 128 bytes an instruction.  LDS is filled in lane order, so the bank swizzle (piece p of row r in slot
+    // p ^ ((r >> 1) & 7)) is in which piece a lane fetches.  Rows past the end are the last one again (their sums are not
+    // stored); groups of 8 token rows that do not exist are not fetched.
+    const int8_t* src[T::LOADS];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+    for (int i = 0; i < T::LOADS; ++i) {
+        const int r = 8 * (i < WI ? i : i - WI) + (lane >> 3);
+        const int row = i < WI ? (n0 + r < n1 ? n0 + r : n1 - 1) : (r < a.M ? r : a.M - 1);
+        src[i] = (i < WI ? a.w + (int64_t)row * a.ldw : a.x + (int64_t)row * a.ldx) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
+    }
+    const int whole = a.K >> 7;
+    const int mine = whole > wave ? (whole - wave + NW - 1) / NW : 0;  // blocks wave, wave + NW, ..
+    uint8_t* const ring = smem + wave * (S * T::STAGE);
+    auto request = [&](int j, int stage) __attribute__((always_inline)) {  // past the end: the last one again, for nobody
+        const int at = 128 * (wave + NW * (j < mine ? j : mine - 1));
+#pragma unroll
+        for (int i = 0; i < T::LOADS; ++i)
+            __builtin_amdgcn_global_load_lds((gptr_t)(src[i] + at), (lptr_t)(ring + stage * T::STAGE + 1024 * (i < WI ? i : 2 * FB + i - WI)), 16,
+                                             0, 0);
+    };
+    // w rows ride the A operand of v_mfma_i32_16x16x64_i8, token rows the B operand: a lane (i, g) supplies 16 bytes of row i and
+    // ends with token i, features 4 g .. 4 g + 3
+    i32x4 acc[FB][TB];
+#pragma unroll
+    for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) acc[fb][tb] = i32x4{0, 0, 0, 0};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)ring + lr * 128 + 16 * (lg ^ ((lr >> 1) & 7));
+    if (mine > 0) {
+#pragma unroll
+        for (int j = 0; j < S - 1; ++j) request(j, j);
+        int stage = 0, free_stage = S - 1;
+        for (int j = 0; j < mine; ++j) {
+            // (the stage read in the step before: its fragments have been waited for)
+            request(j + S - 1, free_stage);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 1) * T::LOADS) : "memory");
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int at = (b + u * kFewWaves) * 128 + 64 * h + 16 * lg;
-                w[u][h] = *reinterpret_cast<const u32x4*>(wrow + at);
+                u32x4 f[FB + TB];
+                read_fragments(f, (lds0 + stage * T::STAGE) ^ (64 * h));
 #pragma unroll
-                for (int tb = 0; tb < TB; ++tb) x[u][h][tb] = *reinterpret_cast<const u32x4*>(xrow[tb] + at);
+                for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+                    for (int tb = 0; tb < TB; ++tb) acc[fb][tb] = mfma16_i8(f[fb], f[FB + tb], acc[fb][tb]);
             }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int tb = 0; tb < TB; ++tb) acc[tb] = mfma16_i8(w[u][h], x[u][h][tb], acc[tb]);
+            free_stage = stage;
+            stage = stage + 1 == S ? 0 : stage + 1;
+        }
     }
-    for (; b < blocks; b += kFewWaves) {
+    if ((a.K & 127) && wave == whole % NW) {  // what is left behind the whole blocks is one wavefront's
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int at = b * 128 + 64 * h + 16 * lg;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(wrow + at);
+            const int at = whole * 128 + 64 * h + 16 * lg;
+            u32x4 x[TB];
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb)
-                acc[tb] = mfma16_i8(w, *reinterpret_cast<const u32x4*>(xrow[tb] + at), acc[tb]);
+                x[tb] = load_cut_piece(a.x + (int64_t)(16 * tb + lr < a.M ? 16 * tb + lr : a.M - 1) * a.ldx, at, a.K);
+#pragma unroll
+            for (int fb = 0; fb < FB; ++fb) {
+                const int n = n0 + 16 * fb + lr;
+                const u32x4 w = load_cut_piece(a.w + (int64_t)(n < n1 ? n : n1 - 1) * a.ldw, at, a.K);
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb) acc[fb][tb] = mfma16_i8(w, x[tb], acc[fb][tb]);
+            }
         }
     }
-    if (b == blocks && (a.K & 127)) {  // what is left behind the whole blocks is one wavefront's
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int at = b * 128 + 64 * h + 16 * lg;
-            const u32x4 w = load_cut_piece(wrow, at, a.K);
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb) acc[tb] = mfma16_i8(w, load_cut_piece(xrow[tb], at, a.K), acc[tb]);
-        }
-    }
-#pragma unroll
-    for (int tb = 0; tb < TB; ++tb) part[wave][tb][lane] = acc[tb];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the loads for nobody)
     __syncthreads();
-    // thread t: token t / 16 of a block of 32, feature t % 16
-    for (int i = tid; i < 256 * TB; i += 64 * kFewWaves) {
-        const int m = i >> 4, f = i & 15, n = n0 + f;
-        if (m >= a.M || n >= a.N) continue;
+    i32x4* const part = reinterpret_cast<i32x4*>(smem);  // [wave][fb][tb][lane]
+#pragma unroll
+    for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb) part[((wave * FB + fb) * TB + tb) * 64 + lane] = acc[fb][tb];
+    __syncthreads();
+    for (int i = tid; i < 16 * FB * a.M; i += 64 * NW) {
+        const int m = i / (16 * FB), f = i % (16 * FB), n = n0 + f;
+        if (n >= n1) continue;
+        const int at = (f >> 4) * TB + (m >> 4), l = 16 * ((f & 15) >> 2) + (m & 15);
         int sum = 0;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) sum += part[w][m >> 4][16 * (f >> 2) + (m & 15)][f & 3];
+        for (int w = 0; w < NW; ++w) sum += part[(w * FB * TB + at) * 64 + l][f & 3];
         const float y = fmaf((float)sum, a.x_scale[m] * a.w_scale[n], a.bias ? __uint_as_float((uint32_t)a.bias[n] << 16) : 0.f);
         const int64_t o = (int64_t)m * a.ldy + n;
         if constexpr (OUT_F32) static_cast<float*>(a.y)[o] = y;
@@ -98,11 +163,26 @@ __global__ void __launch_bounds__(64 * kFewWaves) linear_few_kernel(const Linear
     }
 }
 
-template <int TB>
-hipError_t launch_few(const LinearQuantArgs& a, hipStream_t s) {
-    const auto kern = a.out_f32 ? linear_few_kernel<TB, true> : linear_few_kernel<TB, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + 15) / 16)), dim3(64 * kFewWaves), 0, s, a);
+template <int XI, int WI, int NW, int S, bool OUT_F32>
+hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
+    constexpr int smem = FewTile<XI, WI, NW, S>::LDS;
+    const auto kern = linear_few_kernel<XI, WI, NW, S, OUT_F32>;
+    static std::atomic<uint64_t> attr_set{0};
+    const hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + F - 1) / F)), dim3(64 * NW), smem, s, a, F);
     return hipGetLastError();
+}
+
+template <int XI, int NW, int S>
+hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
+    switch ((F + 7) / 8) {
+        case 1: return a.out_f32 ? launch_few<XI, 1, NW, S, true>(a, F, s) : launch_few<XI, 1, NW, S, false>(a, F, s);
+        case 2: return a.out_f32 ? launch_few<XI, 2, NW, S, true>(a, F, s) : launch_few<XI, 2, NW, S, false>(a, F, s);
+        case 3: return a.out_f32 ? launch_few<XI, 3, NW, S, true>(a, F, s) : launch_few<XI, 3, NW, S, false>(a, F, s);
+        case 4: return a.out_f32 ? launch_few<XI, 4, NW, S, true>(a, F, s) : launch_few<XI, 4, NW, S, false>(a, F, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -111,7 +191,26 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     int cus = 0;
     hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
-    if (q.M <= 16) return launch_few<1>(q, s);
+#ifdef SWEEP
+    const char* force = getenv("DIT_FORM");
+    const int forced = force ? atoi(force) : -1;
+#endif
+    {
+        const int per = (q.N + 32 * cus - 1) / (32 * cus);  // workgroups a compute unit, 32 features each at most
+        int F = (q.N + per * cus - 1) / (per * cus);
+        if (F < 8) F = 8;
+#ifdef SWEEP
+        const bool few = forced < 0 ? q.M <= 16 : forced == 99 && q.M <= 64;
+#else
+        const bool few = q.M <= 16 ? per <= 2 : q.M <= 64 && per == 1;
+#endif
+        if (few) {
+            if (q.M <= 8) return launch_few<1, 4, 3>(q, F, s);
+            if (q.M <= 16) return launch_few<2, 4, 3>(q, F, s);
+            if (q.M <= 32) return launch_few<4, 4, 2>(q, F, s);
+            return launch_few<8, 4, 2>(q, F, s);
+        }
+    }
     LinearArgs a{};
     a.x = reinterpret_cast<const uint16_t*>(q.x);
     a.w = reinterpret_cast<const uint16_t*>(q.w);
@@ -127,8 +226,12 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     a.ldw = q.ldw / 2;
     a.ldy = q.ldy;
     a.out_f32 = q.out_f32;
-    const bool big_too = a.tail == 0 && a.N >= 8;
+    const bool big_too = a.N >= 8;
+#ifdef SWEEP
+    const int form = forced >= 0 && (forced > 0 || big_too) && forced != 99 ? forced : choose_linear_form_i8(q.M, q.N, q.K, big_too, cus);
+#else
     const int form = choose_linear_form_i8(q.M, q.N, q.K, big_too, cus);
+#endif
     if (form) return launch_linear_small_i8(a, form, s);
     // 256 x 256 tiles store whole 16-byte pieces: the last N % 8 features are a call of their own
     const int rest = a.N % 8;
