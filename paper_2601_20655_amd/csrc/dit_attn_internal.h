@@ -300,6 +300,12 @@ struct KRescaleArgs {
 };
 hipError_t launch_k_rescale(const KRescaleArgs& a, hipStream_t s);
 
+// Rows of more bytes than the chip's caches hold are stored, and 16-bit ones read, past them: they would push out what the
+// next call reads.  Smaller ones were often just written, and are still there.  Past the caches and through them: norm and
+// reading back, 32,760 x 5,120, 277 us and 295; 8-bit projection 32,760 x 15,360 x 5,120 1,834 and 1,864, with fp32 rows
+// 2,147 and 2,364; 7,800 x 4,608 x 1,536, whose rows the caches keep, 65 and 63; norm of 7,800 x 1,536 18 and 16.
+inline bool exceeds_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
+
 // ---- 8-bit rows: N signed 8-bit integers and one fp32 scale a row (dit_rows_quant.hip) ----
 constexpr float kQuantTop = 127.0f;            // the largest magnitude of a row becomes this integer
 constexpr float kQuantZero = 0x1p-120f;        // rows whose largest magnitude is below count as zero (127 / amax stays finite)
@@ -317,7 +323,6 @@ struct QuantArgs {
     int x_f32, r_f32;
     int norm;  // RMS normalisation (else rows as they are, or through act)
     int gelu;
-    int past_caches;  // set by launch_quant_rows
 };
 hipError_t launch_quant_rows(const QuantArgs& a, hipStream_t s);
 struct DequantArgs {
@@ -327,7 +332,6 @@ struct DequantArgs {
     int M, N;
     int64_t ldq, ldy;
     int out_f32;
-    int past_caches;  // set by launch_dequant_rows
 };
 hipError_t launch_dequant_rows(const DequantArgs& a, hipStream_t s);
 

@@ -59,12 +59,14 @@ __device__ __forceinline__ void static_for(F&& f) {
     }
 }
 
-// TAIL (8-bit operands): integers are left behind the whole steps (a.tail), and make one more
-template <int OP, bool OUT_F32, int QKV, bool TAIL = false>
+// 8-bit operands.  TAIL: integers are left behind the whole steps (a.tail), and make one more.  PAST: the rows are stored past
+// the caches (exceeds_caches; a branch in the store instead costs the step loop registers, 1,830 -> 2,010 us at 32,760 x
+// 15,360 x 5,120).
+template <int OP, bool OUT_F32, int QKV, bool TAIL = false, bool PAST = false>
 __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearArgs a) {
     // QKV: 0 plain rows; 1 the fused q/k/v form; 2 the same with the k rows RMS-normalised per head; 3 with the
     // per-token normalisation's first half (weights applied, sums of squares left for k_rescale_kernel)
-    static_assert(OP == OP_BF16 ? !TAIL : OP == OP_I8 && !QKV, "operand types");
+    static_assert(OP == OP_BF16 ? !TAIL && !PAST : OP == OP_I8 && !QKV, "operand types");
     static_assert(!(OUT_F32 && QKV), "the fused q/k/v form writes 16-bit rows and tiles");
     static_assert(kLinBM == 256 && kLinBN == 256 && kLinBK == 64, "tile shape");
     constexpr int SX = kLinSX;
@@ -310,6 +312,10 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 if (a.bias && n0 < a.N) bb[fb] = *reinterpret_cast<const uint2*>(a.bias + n0);
             }
         }
+        auto store_piece = [&](u32x4* at, u32x4 v) __attribute__((always_inline)) {
+            if constexpr (PAST) __builtin_nontemporal_store(v, at);
+            else *at = v;
+        };
         // (16-bit output only: with fp32 output the extra path costs the step loop a register)
         const bool full = !OUT_F32 && (tm + 1) * kLinBM <= a.M && (tn + 1) * kLinBN <= a.N;  // uniform
 #pragma unroll
@@ -359,7 +365,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 const int m = tm * kLinBM + wt * BR * TB + pass * RP + k * (64 / PR) + rrow;
                 // N is a multiple of 8: a piece of a row is inside or outside as a whole
                 if (m < a.M && n < a.N)
-                    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES) = v;
+                    store_piece(reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES), v);
             };
             if (full) {
                 // a tile inside y stores without tests, and all four pieces of the pass are read back before the
@@ -374,7 +380,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int m = tm * kLinBM + wt * BR * TB + pass * RP + k * (64 / PR) + rrow;
-                    *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES) = v[k];
+                    store_piece(reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES), v[k]);
                 }
             } else {
                 // (two at a time: the loop around this leaves few registers free)
@@ -732,9 +738,9 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last steps
 }
 
-template <int OP, bool OUT_F32, int QKV, bool TAIL = false>
+template <int OP, bool OUT_F32, int QKV, bool TAIL = false, bool PAST = false>
 hipError_t launch_linear_inst(const LinearArgs& a, int cus, hipStream_t s) {
-    auto kern = linear_kernel<OP, OUT_F32, QKV, TAIL>;
+    auto kern = linear_kernel<OP, OUT_F32, QKV, TAIL, PAST>;
     constexpr int smem = (kLinSX + kLinSW) * kLinTileBytes;
     static std::atomic<uint64_t> attr_set{0};
     hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
@@ -760,13 +766,22 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
     return a.out_f32 ? launch_linear_inst<OP_BF16, true, 0>(a, cus, s) : launch_linear_inst<OP_BF16, false, 0>(a, cus, s);
 }
 
+namespace {
+
+template <bool OUT_F32, bool TAIL>
+hipError_t launch_linear_i8(const LinearArgs& a, int cus, hipStream_t s) {
+    if (exceeds_caches((int64_t)a.M * a.N * (OUT_F32 ? 4 : 2))) return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, true>(a, cus, s);
+    return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false>(a, cus, s);
+}
+
+}  // namespace
+
 hipError_t launch_linear_i8(const LinearArgs& a, hipStream_t s) {
     int cus = 0;
     const hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
-    if (a.tail > 0)
-        return a.out_f32 ? launch_linear_inst<OP_I8, true, 0, true>(a, cus, s) : launch_linear_inst<OP_I8, false, 0, true>(a, cus, s);
-    return a.out_f32 ? launch_linear_inst<OP_I8, true, 0>(a, cus, s) : launch_linear_inst<OP_I8, false, 0>(a, cus, s);
+    if (a.tail > 0) return a.out_f32 ? launch_linear_i8<true, true>(a, cus, s) : launch_linear_i8<false, true>(a, cus, s);
+    return a.out_f32 ? launch_linear_i8<true, false>(a, cus, s) : launch_linear_i8<false, false>(a, cus, s);
 }
 
 }  // namespace dit

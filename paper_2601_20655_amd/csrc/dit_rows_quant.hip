@@ -6,11 +6,12 @@
 // normalisation's factor 1 / sqrt(mean + eps) is common to the row, so it cancels in the integers
 // q = rint(t * 127 / max|t|), t = h * gamma, and appears in the scale alone: the integers do not wait for the sum.
 //
-// What bounds it: memory.  32,760 x 5,120, new rows at every call: norm with 16-bit residual 201 us (5.8 TB/s of reads and
-// writes), with a 32-bit one 333 (5.5), 16-bit rows to 8 bits 85 (5.9), back to 16 bits 88 (5.7) and 32 bits 134 (6.2);
-// GELU, 32,760 x 20,480, 350 (5.7).  (Copying 2 GiB by torch: 4.9 TB/s.)  Tried without gain: workgroups that walk several
-// rows with the weights in registers (201 -> 219 to 249 us; 105 -> 98 without a residual), weights asked for ahead of their
-// use (121 us against 105 without a residual: the registers cost a wavefront a SIMD).
+// What bounds it: memory.  32,760 x 5,120, new rows at every call: norm with 16-bit residual 194 us (6.0 TB/s of reads and
+// writes), with a 32-bit one 332 (5.6), without 104 (4.8), 16-bit rows to 8 bits 82 (6.1), back to 16 bits 82 (6.1) and 32 bits
+// 128 (6.6); GELU, 32,760 x 20,480, 355 (5.7).  (Copying 2 GiB by torch: 4.9 TB/s.)  One row: 3.7 us, launch included.
+// Tried without gain: workgroups that walk several rows with the weights in registers (norm 201 -> 219 to 249 us; 105 -> 98
+// without a residual), weights asked for ahead of their use (105 -> 121 without a residual: the registers cost a wavefront a
+// SIMD).
 #include <type_traits>
 
 #include "dit_attn_device.h"
@@ -33,15 +34,35 @@ __device__ __forceinline__ float gelu_tanh(float x) {
     return x * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
-// Eight columns from `col` on.  PAST: past the caches, for rows that they cannot keep (rows_pass_caches).  Not for 32-bit
-// rows, whose eight columns are two loads or stores that each touch half of every 32 bytes: the caches join them (norm with a
-// 32-bit residual 333 us, past the caches 365).
+// Eight columns from `col` on, as they lie in memory.  PAST: past the caches, for rows that they cannot keep
+// (exceeds_caches).  Not for 32-bit rows, whose eight columns are two loads or stores that each touch half of every 32 bytes:
+// the caches join them (norm with a 32-bit residual 333 us, past the caches 365).
+template <bool F32>
+struct Chunk {
+    u32x4 v[F32 ? 2 : 1];
+};
 template <bool F32, bool PAST>
-__device__ __forceinline__ void load_chunk(const void* row, int col, float v[8]) {
-    if constexpr (F32 || !PAST)
-        load8(row, col, F32, v);
-    else
-        widen8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(row) + col)), v);
+__device__ __forceinline__ Chunk<F32> load_chunk(const void* row, int col) {
+    const u32x4* const p = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(row) + (size_t)col * (F32 ? 4 : 2));
+    Chunk<F32> k;
+    if constexpr (F32) {
+        k.v[0] = p[0];
+        k.v[1] = p[1];
+    } else if constexpr (PAST) {
+        k.v[0] = __builtin_nontemporal_load(p);
+    } else {
+        k.v[0] = p[0];
+    }
+    return k;
+}
+template <bool F32>
+__device__ __forceinline__ void to_numbers(const Chunk<F32>& k, float v[8]) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(k.v[i >> 2][i & 3]);
+    } else {
+        widen8(k.v[0], v);
+    }
 }
 template <bool F32, bool PAST>
 __device__ __forceinline__ void store_chunk(void* row, int col, const float v[8]) {
@@ -75,8 +96,9 @@ __device__ __forceinline__ uint32_t to_bytes(const float v[4], float inverse) {
     return lo | hi;
 }
 
-// W wavefronts a row, one row a workgroup or several.  CUT: N is no multiple of 8.
-template <int MODE, bool X_F32, int RES, int C, bool CUT>
+// W wavefronts a row, one row a workgroup or several.  CUT: N is no multiple of 8.  PAST: 16-bit rows past the
+// caches.
+template <int MODE, bool X_F32, int RES, int C, bool CUT, bool PAST>
 __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int W) {
     constexpr bool R_F32 = RES == ROW_F32;
     __shared__ float s_top[16], s_sum[16];
@@ -94,49 +116,77 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
     // one it is loaded again, and counts as zeros.  (One chunk a lane: there may be no whole one.)  A last chunk that N cuts
     // is loaded number by number, by its one lane.
     const int whole = a.N >> 3, rest = CUT ? a.N & 7 : 0;
-    float t[C][8];
     const int first = part * 64 + lane, step = W * 64;
-    auto load_all = [&](auto f32, auto past, const void* row, auto&& take) __attribute__((always_inline)) {
+    float t[C][8];
+    if constexpr (C == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[0][i] = 0.f;
+        if (first < whole) {
+            const Chunk<X_F32> kx = load_chunk<X_F32, PAST>(x, 8 * first);
+            float v[8];
+            if constexpr (RES != ROW_NONE) to_numbers<R_F32>(load_chunk<R_F32, PAST>(r, 8 * first), v);
+            to_numbers<X_F32>(kx, t[0]);
+            if constexpr (RES != ROW_NONE) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[0][i] += v[i];
+            }
+        }
+    } else {
+        Chunk<X_F32> kx[C];
+        Chunk<R_F32> kr[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = first + c * step;
+            kx[c] = load_chunk<X_F32, PAST>(x, 8 * (at < whole ? at : whole - 1));
+        }
+        if constexpr (RES != ROW_NONE) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = first + c * step;
+                kr[c] = load_chunk<R_F32, PAST>(r, 8 * (at < whole ? at : whole - 1));
+            }
+        }
+        // (All are asked for before the first is used.  Left to the compiler, loads sank behind the test for the row's end and
+        // were waited for one by one: norm of 7,800 x 1,536 17.3 us, 16.2 this way, 32,760 x 5,120 200 and 194.  Not the longest
+        // rows, whose registers do not reach for it.)
+        if constexpr (C <= 5) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                for (u32x4& u : kx[c].v) asm volatile("" : "+v"(u));
+                if constexpr (RES != ROW_NONE) {
+                    for (u32x4& u : kr[c].v) asm volatile("" : "+v"(u));
+                }
+            }
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = first + c * step;
             float v[8];
-            if constexpr (C == 1) {
+            to_numbers<X_F32>(kx[c], t[c]);
+            if constexpr (RES != ROW_NONE) to_numbers<R_F32>(kr[c], v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0.f;
-                if (at < whole) load_chunk<decltype(f32)::value, decltype(past)::value>(row, 8 * at, v);
-            } else {
-                load_chunk<decltype(f32)::value, decltype(past)::value>(row, 8 * (at < whole ? at : whole - 1), v);
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (RES != ROW_NONE) t[c][i] += v[i];
+                t[c][i] = at < whole ? t[c][i] : 0.f;
             }
-            take(c, v);
         }
-    };
-    auto load_rows = [&](auto past) __attribute__((always_inline)) {
-        load_all(std::bool_constant<X_F32>(), past, x, [&](int c, const float v[8]) __attribute__((always_inline)) {
+    }
+    if constexpr (CUT) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[c][i] = v[i];
-        });
-        if constexpr (RES != ROW_NONE)
-            load_all(std::bool_constant<R_F32>(), past, r, [&](int c, const float v[8]) __attribute__((always_inline)) {
+        for (int c = 0; c < C; ++c) {
+            if (first + c * step != whole) continue;
+            float v[7], w[7];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[c][i] += v[i];
-            });
-    };
-    if (a.past_caches) load_rows(std::true_type());
-    else load_rows(std::false_type());
+            for (int i = 0; i < 7; ++i) v[i] = load_number<X_F32>(x, 8 * whole + (i < rest ? i : 0));
+            if constexpr (RES != ROW_NONE) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int at = first + c * step;
+                for (int i = 0; i < 7; ++i) w[i] = load_number<R_F32>(r, 8 * whole + (i < rest ? i : 0));
+            }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t[c][i] = at < whole ? t[c][i] : 0.f;
-        if (CUT && at == whole) {
-#pragma unroll
-            for (int i = 0; i < 7; ++i)
-                if (i < rest) {
-                    float v = load_number<X_F32>(x, 8 * at + i);
-                    if constexpr (RES != ROW_NONE) v += load_number<R_F32>(r, 8 * at + i);
-                    t[c][i] = v;
-                }
+            for (int i = 0; i < 7; ++i) {
+                if constexpr (RES != ROW_NONE) v[i] += w[i];
+                t[c][i] = i < rest ? v[i] : 0.f;
+            }
         }
     }
 
@@ -147,8 +197,7 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
             for (int c = 0; c < C; ++c) {
                 const int at = first + c * step;
                 if (at < whole) {
-                    if (a.past_caches) store_chunk<R_F32, true>(h, 8 * at, t[c]);
-                    else store_chunk<R_F32, false>(h, 8 * at, t[c]);
+                    store_chunk<R_F32, PAST>(h, 8 * at, t[c]);
                 } else if (CUT && at == whole) {
 #pragma unroll
                     for (int i = 0; i < 7; ++i)
@@ -173,9 +222,11 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
 #pragma unroll
                     for (int i = 0; i < 8; ++i) t[c][i] *= g[i];
                 } else if (CUT && at == whole) {
+                    float g[7];
 #pragma unroll
-                    for (int i = 0; i < 7; ++i)
-                        if (i < rest) t[c][i] *= a.gamma[8 * at + i];
+                    for (int i = 0; i < 7; ++i) g[i] = a.gamma[8 * whole + (i < rest ? i : 0)];
+#pragma unroll
+                    for (int i = 0; i < 7; ++i) t[c][i] = i < rest ? t[c][i] * g[i] : t[c][i];
                 }
             }
         }
@@ -237,7 +288,7 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
 }
 
 // A lane writes 16 bytes at a time: V = 8 or 4 columns.  `parts` wavefronts a row, C pieces a lane.
-template <bool OUT_F32, int C, bool CUT>
+template <bool OUT_F32, int C, bool CUT, bool PAST>
 __global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, int parts) {
     constexpr int V = OUT_F32 ? 4 : 8;
     typedef std::conditional_t<OUT_F32, uint32_t, uint2> piece_t;
@@ -266,14 +317,13 @@ __global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, 
             if constexpr (OUT_F32) {
                 const f32x4 v = {number(b[c], 0), number(b[c], 1), number(b[c], 2), number(b[c], 3)};
                 f32x4* const p = reinterpret_cast<f32x4*>(static_cast<float*>(y) + V * (int64_t)at);
-                if (a.past_caches) __builtin_nontemporal_store(v, p);
+                if constexpr (PAST) __builtin_nontemporal_store(v, p);
                 else *p = v;
             } else {
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = number(i < 4 ? b[c].x : b[c].y, i & 3);
-                if (a.past_caches) store_chunk<false, true>(y, V * at, v);
-                else store_chunk<false, false>(y, V * at, v);
+                store_chunk<false, PAST>(y, V * at, v);
             }
         } else if (CUT && at == whole) {
             for (int i = 0; i < rest; ++i) store_number<OUT_F32>(y, V * at + i, (float)q[V * at + i] * scale);
@@ -282,8 +332,10 @@ __global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, 
 }
 
 // How rows lie over wavefronts.  Where there are wavefronts enough to keep the memory busy, `most` chunks a lane; where there
-// are not, one, the row over as many wavefronts as it takes (at most 16, a workgroup).
-constexpr int kBusy = 16 * kCUs;
+// are not, one, the row over as many wavefronts as it takes (at most 16, a workgroup).  (A wavefront a SIMD is enough: norm of
+// 769 x 5,120 9.3 us if four are asked for, 8.1 with one, 1,560 x 5,120 without a residual 11.2 and 8.5; 1,560 x 5,000 with a
+// 32-bit one 21.6 and 24.6.)
+constexpr int kBusy = 4 * kCUs;
 struct RowLayout {
     int waves, per_lane, rows;  // wavefronts a row, chunks a lane, rows a workgroup
 };
@@ -299,7 +351,10 @@ RowLayout layout_rows(int M, int N, int most) {
 
 template <int MODE, bool X_F32, int RES, int C>
 hipError_t launch_quant(const QuantArgs& a, const RowLayout& l, hipStream_t s) {
-    const auto kern = a.N % 8 ? quant_rows_kernel<MODE, X_F32, RES, C, true> : quant_rows_kernel<MODE, X_F32, RES, C, false>;
+    constexpr bool SOME_16 = !X_F32 || RES == ROW_BF16;
+    const bool past = SOME_16 && exceeds_caches((int64_t)a.M * a.N * ((X_F32 ? 4 : 2) + (RES == ROW_F32 ? 4 : RES == ROW_BF16 ? 2 : 0)));
+    const auto kern = a.N % 8 ? past ? quant_rows_kernel<MODE, X_F32, RES, C, true, SOME_16> : quant_rows_kernel<MODE, X_F32, RES, C, true, false>
+                              : past ? quant_rows_kernel<MODE, X_F32, RES, C, false, SOME_16> : quant_rows_kernel<MODE, X_F32, RES, C, false, false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)a.M + l.rows - 1) / l.rows)),
                        dim3(64 * l.waves * l.rows), 0, s, a, l.waves);
     return hipGetLastError();
@@ -330,7 +385,9 @@ hipError_t launch_dequant(const DequantArgs& a, int need, hipStream_t s) {
     const int parts = (need + C - 1) / C;
     const int64_t groups = ((int64_t)a.M * parts + 3) / 4;
     if (groups > 0x7fffffff) return hipErrorInvalidValue;
-    const auto kern = a.N % V ? dequant_rows_kernel<OUT_F32, C, true> : dequant_rows_kernel<OUT_F32, C, false>;
+    const bool past = exceeds_caches((int64_t)a.M * a.N * (OUT_F32 ? 4 : 2));
+    const auto kern = a.N % V ? past ? dequant_rows_kernel<OUT_F32, C, true, true> : dequant_rows_kernel<OUT_F32, C, true, false>
+                              : past ? dequant_rows_kernel<OUT_F32, C, false, true> : dequant_rows_kernel<OUT_F32, C, false, false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), 0, s, a, parts);
     return hipGetLastError();
 }
@@ -343,16 +400,9 @@ hipError_t launch_dequant(const DequantArgs& a, hipStream_t s) {
     return (int64_t)a.M * need < kBusy ? launch_dequant<OUT_F32, 1>(a, need, s) : launch_dequant<OUT_F32, 2>(a, need, s);
 }
 
-// Rows of more bytes than the chip's caches hold (256 MB) are read and written past them: they would push out what the next
-// call reads (norm and reading back, 32,760 x 5,120: 314 us through the caches, 284 past them).  Smaller ones were often just
-// written, and are still there (norm of 7,800 x 1,536 16 us through the caches, 18 past them).
-bool rows_pass_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
-
 }  // namespace
 
-hipError_t launch_quant_rows(const QuantArgs& args, hipStream_t s) {
-    QuantArgs a = args;
-    a.past_caches = rows_pass_caches((int64_t)a.M * a.N * ((a.x_f32 ? 4 : 2) + (a.residual ? a.r_f32 ? 4 : 2 : 0)));
+hipError_t launch_quant_rows(const QuantArgs& a, hipStream_t s) {
     if (!a.norm) {
         if (a.gelu) return a.x_f32 ? launch_quant<ROW_GELU, true, ROW_NONE>(a, s) : launch_quant<ROW_GELU, false, ROW_NONE>(a, s);
         return a.x_f32 ? launch_quant<ROW_PLAIN, true, ROW_NONE>(a, s) : launch_quant<ROW_PLAIN, false, ROW_NONE>(a, s);
@@ -362,9 +412,7 @@ hipError_t launch_quant_rows(const QuantArgs& args, hipStream_t s) {
     return a.x_f32 ? launch_quant<ROW_NORM, true, ROW_BF16>(a, s) : launch_quant<ROW_NORM, false, ROW_BF16>(a, s);
 }
 
-hipError_t launch_dequant_rows(const DequantArgs& args, hipStream_t s) {
-    DequantArgs a = args;
-    a.past_caches = rows_pass_caches((int64_t)a.M * a.N * (a.out_f32 ? 4 : 2));
+hipError_t launch_dequant_rows(const DequantArgs& a, hipStream_t s) {
     return a.out_f32 ? launch_dequant<true>(a, s) : launch_dequant<false>(a, s);
 }
 
