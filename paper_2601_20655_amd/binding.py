@@ -277,8 +277,8 @@ def _stream_ptr(stream):
         return stream.cuda_stream
     # (the raw handle: building the Stream object around it took 2.5 us, a seventh of what a small call takes the host)
     try:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    except AttributeError:  # not a public function: this torch may not have it
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    except AttributeError:  # not public functions: this torch may not have them
         return torch.cuda.current_stream().cuda_stream
 
 
@@ -624,47 +624,53 @@ def dit_qkv_proj_forward(x, w, bias, grid, split, H, q_out=None, origin=(0, 0, 0
     return q_out, workspace
 
 
-def _empty_rows(M, N, dtype, device):
-    """An [M, N] tensor whose rows start on multiples of 16 bytes."""
-    per = 16 // dtype.itemsize
+def _empty_rows(M, N, dtype, device, multiple=16):
+    """An [M, N] tensor whose rows start on multiples of so many bytes."""
+    per = multiple // dtype.itemsize
     return torch.empty((M, (N + per - 1) // per * per), dtype=dtype, device=device)[:, :N]
 
 
-def _check_rows(what, name, t, shape, dtype, device):
-    """t: a [M, N] tensor of that type on that device, contiguous along its rows.  dtype None: bf16 or float32."""
-    if t.shape != shape or t.stride(1) != 1 and shape[1] != 1:
-        raise ValueError("%s: %s must be a %s tensor with contiguous rows" % (what, name, tuple(shape)))
-    if dtype is None:
-        _dtype_code(t)
-    elif t.dtype != dtype:
+# (The checks below cost the host about half a microsecond a tensor; of a small call's time it is the larger part.)
+
+def _row_stride(what, name, t, shape, dtype, device):
+    """Row stride of t: a tensor of that [M, N] shape and type on that device (its index), contiguous along its rows."""
+    if t.shape != shape:
+        raise ValueError("%s: %s has shape %s, expected %s" % (what, name, tuple(t.shape), tuple(shape)))
+    if t.dtype != dtype:
         raise TypeError("%s: %s must be %s, got %s" % (what, name, dtype, t.dtype))
-    if not t.is_cuda or t.device != device:
+    if t.get_device() != device or device < 0:
         raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+    s = t.stride()
+    if s[1] != 1 and shape[1] != 1:
+        raise ValueError("%s: %s must have contiguous rows" % (what, name))
+    return s[0]
 
 
 def _check_vector(what, name, t, n, dtype, device):
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s: %s must be a dense tensor of %d elements" % (what, name, n))
     if t.dtype != dtype:
         raise TypeError("%s: %s must be %s, got %s" % (what, name, dtype, t.dtype))
-    if t.device != device:
+    if t.get_device() != device:
         raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
 
 
 def _quant_outputs(what, x, q, scale):
-    """q and scale of x's rows: allocated, or checked."""
-    if x.dim() != 2:
+    """(shape, device index, type code of x, row stride of x, q, row stride of q, scale): q and scale allocated, or checked."""
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("%s: x must be [M, N]" % what)
-    M, N = x.shape
+    device = x.get_device()
+    code = _dtype_code(x)
+    ldx = _row_stride(what, "x", x, shape, x.dtype, device)
     if q is None:
-        q = _empty_rows(M, N, torch.int8, x.device)
-    else:
-        _check_rows(what, "q", q, x.shape, torch.int8, x.device)
+        # (lines of 128 bytes to themselves: the projection reads rows of such strides a quarter faster)
+        q = _empty_rows(shape[0], shape[1], torch.int8, x.device, 128)
+    ldq = _row_stride(what, "q", q, shape, torch.int8, device)
     if scale is None:
-        scale = torch.empty(M, dtype=torch.float32, device=x.device)
-    else:
-        _check_vector(what, "scale", scale, M, torch.float32, x.device)
-    return q, scale
+        scale = torch.empty(shape[0], dtype=torch.float32, device=x.device)
+    _check_vector(what, "scale", scale, shape[0], torch.float32, device)
+    return shape, device, code, ldx, q, ldq, scale
 
 
 _ACT_CODES = {"none": DIT_ACT_NONE, "gelu": DIT_ACT_GELU_TANH}
@@ -673,14 +679,14 @@ _ACT_CODES = {"none": DIT_ACT_NONE, "gelu": DIT_ACT_GELU_TANH}
 def dit_quant_rows_forward(x, act="none", q=None, scale=None, stream=None):
     """Rows of x [M, N] (bf16 or float32), through act ("none" or "gelu"), to 8-bit rows: returns q [M, N] int8 and
     scale [M] float32; the rows stand for q * scale[:, None]."""
+    what = "dit_quant_rows_forward"
     if act not in _ACT_CODES:
-        raise ValueError("dit_quant_rows_forward: act must be one of %s" % ", ".join(sorted(_ACT_CODES)))
-    q, scale = _quant_outputs("dit_quant_rows_forward", x, q, scale)
-    _check_rows("dit_quant_rows_forward", "x", x, x.shape, None, x.device)
-    p = dit_quant_rows_params(x.shape[0], x.shape[1], x.stride(0), q.stride(0), _dtype_code(x), _ACT_CODES[act], 0)
+        raise ValueError("%s: act must be one of %s" % (what, ", ".join(sorted(_ACT_CODES))))
+    (M, N), _, code, ldx, q, ldq, scale = _quant_outputs(what, x, q, scale)
+    p = dit_quant_rows_params(M, N, ldx, ldq, code, _ACT_CODES[act], 0)
     st = lib().dit_quant_rows_forward(x.data_ptr(), q.data_ptr(), scale.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
     if st != DIT_OK:
-        raise DitError(st, "dit_quant_rows_forward")
+        raise DitError(st, what)
     return q, scale
 
 
@@ -689,21 +695,19 @@ def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=Non
     float32 or None, residual [M, N] bf16 or float32 or None.  Returns (q, scale), and with a residual (q, scale, h): h in
     residual's type, in h_out if given (residual itself: the sum replaces it)."""
     what = "dit_rms_norm_quant_forward"
-    q, scale = _quant_outputs(what, x, q, scale)
-    _check_rows(what, "x", x, x.shape, None, x.device)
+    shape, device, code, ldx, q, ldq, scale = _quant_outputs(what, x, q, scale)
     if gamma is not None:
-        _check_vector(what, "gamma", gamma, x.shape[1], torch.float32, x.device)
+        _check_vector(what, "gamma", gamma, shape[1], torch.float32, device)
     ldr = ldh = r_code = 0
     if residual is not None:
-        _check_rows(what, "residual", residual, x.shape, None, x.device)
+        r_code = _dtype_code(residual)
+        ldr = _row_stride(what, "residual", residual, shape, residual.dtype, device)
         if h_out is None:
-            h_out = _empty_rows(x.shape[0], x.shape[1], residual.dtype, x.device)
-        else:
-            _check_rows(what, "h_out", h_out, x.shape, residual.dtype, x.device)
-        ldr, ldh, r_code = residual.stride(0), h_out.stride(0), _dtype_code(residual)
+            h_out = _empty_rows(shape[0], shape[1], residual.dtype, x.device)
+        ldh = _row_stride(what, "h_out", h_out, shape, residual.dtype, device)
     elif h_out is not None:
         raise ValueError("%s: h_out needs a residual" % what)
-    p = dit_norm_quant_params(x.shape[0], x.shape[1], x.stride(0), ldr, ldh, q.stride(0), eps, _dtype_code(x), r_code, 0)
+    p = dit_norm_quant_params(shape[0], shape[1], ldx, ldr, ldh, ldq, eps, code, r_code, 0)
     st = lib().dit_rms_norm_quant_forward(x.data_ptr(), residual.data_ptr() if residual is not None else None,
                                           gamma.data_ptr() if gamma is not None else None,
                                           h_out.data_ptr() if h_out is not None else None, q.data_ptr(),
@@ -716,24 +720,25 @@ def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=Non
 def dit_dequant_rows_forward(q, scale, out=None, out_dtype=None, stream=None):
     """8-bit rows read back: q [M, N] int8 times scale [M] float32, as bf16 (default) or float32 rows."""
     what = "dit_dequant_rows_forward"
-    if q.dim() != 2:
+    shape, device = q.shape, q.get_device()
+    if len(shape) != 2:
         raise ValueError("%s: q must be [M, N]" % what)
-    _check_rows(what, "q", q, q.shape, torch.int8, q.device)
-    _check_vector(what, "scale", scale, q.shape[0], torch.float32, q.device)
+    ldq = _row_stride(what, "q", q, shape, torch.int8, device)
+    _check_vector(what, "scale", scale, shape[0], torch.float32, device)
     if out is None:
-        out = _empty_rows(q.shape[0], q.shape[1], out_dtype or torch.bfloat16, q.device)
-    _check_rows(what, "out", out, q.shape, None, q.device)
-    p = dit_dequant_rows_params(q.shape[0], q.shape[1], q.stride(0), out.stride(0), _dtype_code(out), 0)
+        out = _empty_rows(shape[0], shape[1], out_dtype or torch.bfloat16, q.device)
+    code = _dtype_code(out)
+    p = dit_dequant_rows_params(shape[0], shape[1], ldq, _row_stride(what, "out", out, shape, out.dtype, device), code, 0)
     st = lib().dit_dequant_rows_forward(q.data_ptr(), scale.data_ptr(), out.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
     if st != DIT_OK:
         raise DitError(st, what)
     return out
 
 
-def _check_pieces(what, name, t):
+def _check_pieces(what, name, t, ld):
     """The projection reads 8-bit rows in whole 16-byte pieces, the last row too: its storage has to hold the last piece."""
-    end = t.storage_offset() + (t.shape[0] - 1) * t.stride(0) + (t.shape[1] + 15) // 16 * 16
-    if t.shape[1] % 16 and t.shape[0] and end > t.untyped_storage().nbytes():
+    M, K = t.shape
+    if t.storage_offset() + (M - 1) * ld + (K + 15) // 16 * 16 > t.untyped_storage().nbytes():
         raise ValueError("%s: the storage of %s ends inside the last 16-byte piece of its last row" % (what, name))
 
 
@@ -741,22 +746,23 @@ def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dt
     """y = (x w^T) * x_scale[:, None] * w_scale[None, :] + bias on 8-bit rows: x [M, K] and w [N, K] int8, x_scale [M] and
     w_scale [N] float32, bias [N] bf16 or None; y [M, N] bf16 (default) or float32."""
     what = "dit_linear_quant_forward"
-    if x.dim() != 2 or w.dim() != 2 or w.shape[1] != x.shape[1]:
+    xshape, wshape, device = x.shape, w.shape, x.get_device()
+    if len(xshape) != 2 or len(wshape) != 2 or wshape[1] != xshape[1]:
         raise ValueError("%s: shapes do not fit y[M, N] = x[M, K] w[N, K]^T" % what)
-    M, K = x.shape
-    N = w.shape[0]
-    _check_rows(what, "x", x, x.shape, torch.int8, x.device)
-    _check_rows(what, "w", w, w.shape, torch.int8, x.device)
-    _check_pieces(what, "x", x)
-    _check_pieces(what, "w", w)
-    _check_vector(what, "x_scale", x_scale, M, torch.float32, x.device)
-    _check_vector(what, "w_scale", w_scale, N, torch.float32, x.device)
+    (M, K), N = xshape, wshape[0]
+    ldx = _row_stride(what, "x", x, xshape, torch.int8, device)
+    ldw = _row_stride(what, "w", w, wshape, torch.int8, device)
+    if K % 16 and M and N:
+        _check_pieces(what, "x", x, ldx)
+        _check_pieces(what, "w", w, ldw)
+    _check_vector(what, "x_scale", x_scale, M, torch.float32, device)
+    _check_vector(what, "w_scale", w_scale, N, torch.float32, device)
     if bias is not None:
-        _check_vector(what, "bias", bias, N, torch.bfloat16, x.device)
+        _check_vector(what, "bias", bias, N, torch.bfloat16, device)
     if out is None:
         out = _empty_rows(M, N, out_dtype or torch.bfloat16, x.device)
-    _check_rows(what, "out", out, (M, N), None, x.device)
-    p = dit_linear_params(M, N, K, x.stride(0), w.stride(0), out.stride(0), _dtype_code(out), 0)
+    code = _dtype_code(out)
+    p = dit_linear_params(M, N, K, ldx, ldw, _row_stride(what, "out", out, (M, N), out.dtype, device), code, 0)
     st = lib().dit_linear_quant_forward(x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
                                         bias.data_ptr() if bias is not None else None, out.data_ptr(), ctypes.byref(p),
                                         _stream_ptr(stream))

@@ -97,5 +97,5 @@ def test_binding_refusals():
             f()
     # a row that ends inside its last 16-byte piece, at the end of its storage
     with pytest.raises(ValueError):
-        B._check_pieces("f", "x", torch.zeros(2 * 16 + 7, dtype=torch.int8).as_strided((3, 7), (16, 1)))
-    B._check_pieces("f", "x", torch.zeros(3 * 16, dtype=torch.int8).as_strided((3, 7), (16, 1)))
+        B._check_pieces("f", "x", torch.zeros(2 * 16 + 7, dtype=torch.int8).as_strided((3, 7), (16, 1)), 16)
+    B._check_pieces("f", "x", torch.zeros(3 * 16, dtype=torch.int8).as_strided((3, 7), (16, 1)), 16)
