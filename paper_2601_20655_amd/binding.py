@@ -277,8 +277,8 @@ def _stream_ptr(stream):
         return stream.cuda_stream
     # (the raw handle: building the Stream object around it took 2.5 us, a seventh of what a small call takes the host)
     try:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    except AttributeError:  # not public functions: this torch may not have them
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    except AttributeError:  # not a public function: this torch may not have it
         return torch.cuda.current_stream().cuda_stream
 
 

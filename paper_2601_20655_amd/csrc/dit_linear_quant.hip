@@ -1,9 +1,6 @@
 // Projection of 8-bit rows: y[m, n] = (sum_k x[m, k] w[n, k]) * (x_scale[m] * w_scale[n]) + bias[n], the sum an exact 32-bit
 // integer on the matrix cores.  Few token rows are done here, straight from memory; more by the tiles of dit_linear.hip and
 // dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
-#ifdef SWEEP
-#include <stdlib.h>
-#endif
 #include "dit_attn_device.h"
 #include "dit_attn_internal.h"
 
@@ -187,29 +184,34 @@ hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
 
 }  // namespace
 
+// Few rows: as many workgroups as there are compute units, or twice as many, so that all of them pull the weights in at the same
+// rate, and at most 32 features each.  Past 16 rows, and with more features, the tiles read the token rows fewer times.
+// Measured, us, this kernel and the best tile: 1 x 20,480 x 5,120 (three workgroups a unit) 22 and 26; 1 x 15,360 x 5,120 16 and 18;
+// 16 x 5,120 x 20,480 25 and 41; 32 x 5,120 x 5,120 7.8 and 10.5; 64 x 5,120 x 20,480 39 and 44; but 32 x 15,360 x 5,120 22 and 20,
+// 64 x 15,360 x 5,120 29 and 24.
+int choose_linear_quant(int M, int N, int K, int cus, int* features) {
+    const int64_t per = ((int64_t)N + 32 * cus - 1) / (32 * cus);  // workgroups a compute unit
+    *features = 0;
+    if (M <= 16 ? per <= 3 : M <= 64 && per == 1) {
+        const int f = (int)((N + per * cus - 1) / (per * cus));
+        *features = f < 8 ? 8 : f;
+        return 0;
+    }
+    return choose_linear_form_i8(M, N, K, N >= 8, cus);
+}
+
 hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     int cus = 0;
     hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
-#ifdef SWEEP
-    const char* force = getenv("DIT_FORM");
-    const int forced = force ? atoi(force) : -1;
-#endif
-    {
-        const int per = (q.N + 32 * cus - 1) / (32 * cus);  // workgroups a compute unit, 32 features each at most
-        int F = (q.N + per * cus - 1) / (per * cus);
-        if (F < 8) F = 8;
-#ifdef SWEEP
-        const bool few = forced < 0 ? q.M <= 16 : forced == 99 && q.M <= 64;
-#else
-        const bool few = q.M <= 16 ? per <= 2 : q.M <= 64 && per == 1;
-#endif
-        if (few) {
-            if (q.M <= 8) return launch_few<1, 4, 3>(q, F, s);
-            if (q.M <= 16) return launch_few<2, 4, 3>(q, F, s);
-            if (q.M <= 32) return launch_few<4, 4, 2>(q, F, s);
-            return launch_few<8, 4, 2>(q, F, s);
-        }
+    int features;
+    const int form = choose_linear_quant(q.M, q.N, q.K, cus, &features);
+    if (features) {
+        // (3 stages are level with 4 and better than 2 at 16 rows: 25 and 26 us; with more rows 2 leave room for two workgroups)
+        if (q.M <= 8) return launch_few<1, 4, 3>(q, features, s);
+        if (q.M <= 16) return launch_few<2, 4, 3>(q, features, s);
+        if (q.M <= 32) return launch_few<4, 4, 2>(q, features, s);
+        return launch_few<8, 4, 2>(q, features, s);
     }
     LinearArgs a{};
     a.x = reinterpret_cast<const uint16_t*>(q.x);
@@ -226,12 +228,6 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     a.ldw = q.ldw / 2;
     a.ldy = q.ldy;
     a.out_f32 = q.out_f32;
-    const bool big_too = a.N >= 8;
-#ifdef SWEEP
-    const int form = forced >= 0 && (forced > 0 || big_too) && forced != 99 ? forced : choose_linear_form_i8(q.M, q.N, q.K, big_too, cus);
-#else
-    const int form = choose_linear_form_i8(q.M, q.N, q.K, big_too, cus);
-#endif
     if (form) return launch_linear_small_i8(a, form, s);
     // 256 x 256 tiles store whole 16-byte pieces: the last N % 8 features are a call of their own
     const int rest = a.N % 8;

@@ -65,6 +65,19 @@ def test_shapes(M, N, K, out):
     R.check_linear(y, x, xs, w, ws, use, out == "bf16", "%dx%dx%d" % (M, N, K))
 
 
+@pytest.mark.parametrize("i", range(len(R.KERNELS)), ids=["%s_%dx%dx%d" % k for k in R.KERNELS])
+def test_every_kernel(i):
+    """Each kernel on more blocks of K than its stages hold (test_quant_host.py checks that the shapes run on these kernels),
+    in both output types; unit scales and integers, so that a fragment read before its stage has arrived cannot hide."""
+    _, M, N, K = R.KERNELS[i]
+    x, xs, w, ws, bias = operands(M, N, K, seed=i, lo=-8, hi=9)
+    for out in ("f32", "bf16"):
+        y = run(x, xs, w, ws, bias, out, pad=i % 3)
+        R.check_linear(y, x, xs, w, ws, bias, out == "bf16", R.KERNELS[i][0])
+    ones = [np.ones(n, np.float32) for n in (M, N)]
+    assert np.array_equal(run(x, ones[0], w, ones[1], None, "f32"), x.astype(np.float32) @ w.astype(np.float32).T)
+
+
 @pytest.mark.parametrize("M", [1, 4, 16, 17, 40, 64, 300])
 @pytest.mark.parametrize("K", [5120, 20480])
 def test_long_sums(M, K):

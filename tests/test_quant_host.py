@@ -4,6 +4,7 @@ import ctypes
 
 import pytest
 
+import quant_ref as R
 from paper_2601_20655_amd import binding as B
 
 FAKE = 0x1000
@@ -99,3 +100,33 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         B._check_pieces("f", "x", torch.zeros(2 * 16 + 7, dtype=torch.int8).as_strided((3, 7), (16, 1)), 16)
     B._check_pieces("f", "x", torch.zeros(3 * 16, dtype=torch.int8).as_strided((3, 7), (16, 1)), 16)
+
+
+def kernel_of(M, N, K, cus=256):
+    """The kernel of a projection as quant_ref.KERNELS names it."""
+    f = B.lib()._ZN3dit19choose_linear_quantEiiiiPi
+    f.restype = ctypes.c_int
+    features = ctypes.c_int(-1)
+    form = f(M, N, K, cus, ctypes.byref(features))
+    if features.value:
+        assert form == 0 and 8 <= features.value <= 32
+        groups = next(g for g in (1, 2, 4, 8) if M <= 8 * g)
+        return "few%d/%d" % (groups, (features.value + 7) // 8)
+    if form:
+        return "%d%s" % (form, " any" if K % 128 or N % 8 else "")
+    return "big%s%s" % (" tail" if K % 128 else "", " rest" if N % 8 else "")
+
+
+@pytest.mark.parametrize("kernel,M,N,K", R.KERNELS)
+def test_every_kernel_has_a_shape(kernel, M, N, K):
+    assert kernel_of(M, N, K) == kernel
+
+
+def test_kernels_follow_rows_and_compute_units():
+    """Few rows are streamed, a clip goes to 256 x 256 tiles; where a workgroup for each compute unit is not enough for the
+    features, rows past 16 go to tiles; narrow outputs have no 256 x 256 form."""
+    assert kernel_of(1, 15360, 5120) == "few1/4" and kernel_of(16, 5120, 20480) == "few2/3"
+    assert kernel_of(17, 15360, 5120).startswith("11") and kernel_of(64, 8192, 5120) == "few8/4"
+    assert kernel_of(32760, 15360, 5120) == "big" and kernel_of(32760, 15360, 5121) == "big tail"
+    assert not kernel_of(1, 40960, 5120).startswith("few") and kernel_of(1, 1920, 5120, cus=32) == "few1/4"
+    assert kernel_of(100000, 7, 512) not in ("big", "big rest")
