@@ -281,11 +281,11 @@ struct LinearArgs {
     int tail;              // 8-bit integers of a row behind the whole steps, 0 .. 127 (tiles of dit_linear_small.hip only)
 };
 hipError_t launch_linear(const LinearArgs& a, hipStream_t s);
-hipError_t launch_linear_i8(const LinearArgs& a, hipStream_t s);  // 256 x 256 tiles, 8-bit operands
+hipError_t launch_linear_i8(LinearArgs a, int rows, hipStream_t s);  // tiles of 256 or 192 rows x 256 features, 8-bit operands
 // plain projections that 256 x 256 tiles would leave most of the chip idle for (dit_linear_small.hip): which tile, 0 = none
 int choose_linear_form(int M, int N, int K, int cus);
 hipError_t launch_linear_small(const LinearArgs& a, int form, hipStream_t s);
-int choose_linear_form_i8(int M, int N, int K, bool big_too, int cus);  // 0 only with big_too
+int choose_linear_form_i8(int M, int N, int K, int cus);  // (64: the big kernel's, 192 rows; that one and 0 only from 8 features on)
 hipError_t launch_linear_small_i8(const LinearArgs& a, int form, hipStream_t s);
 
 // Second half of the per-token normalisation of the fused q/k/v projection: the projection's epilogue left, in the

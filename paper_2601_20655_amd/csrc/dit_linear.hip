@@ -62,19 +62,22 @@ __device__ __forceinline__ void static_for(F&& f) {
 // 8-bit operands.  TAIL: integers are left behind the whole steps (a.tail), and make one more.  PAST: the rows are stored past
 // the caches (exceeds_caches; a branch in the store instead costs the step loop registers, 1,830 -> 2,010 us at 32,760 x
 // 15,360 x 5,120).
-template <int OP, bool OUT_F32, int QKV, bool TAIL = false, bool PAST = false>
+// 192-token tiles (TB = 6): where they fill the last round of workgroups better.
+template <int OP, bool OUT_F32, int QKV, bool TAIL = false, bool PAST = false, int TB = 8>
 __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearArgs a) {
     // QKV: 0 plain rows; 1 the fused q/k/v form; 2 the same with the k rows RMS-normalised per head; 3 with the
     // per-token normalisation's first half (weights applied, sums of squares left for k_rescale_kernel)
-    static_assert(OP == OP_BF16 ? !TAIL && !PAST : OP == OP_I8 && !QKV, "operand types");
+    static_assert(OP == OP_BF16 ? !TAIL && !PAST && TB == 8 : OP == OP_I8 && !QKV, "operand types");
     static_assert(!(OUT_F32 && QKV), "the fused q/k/v form writes 16-bit rows and tiles");
     static_assert(kLinBM == 256 && kLinBN == 256 && kLinBK == 64, "tile shape");
     constexpr int SX = kLinSX;
     constexpr int BR = 16;       // rows of an MFMA block
     constexpr int FB = 4;        // 16-feature blocks per wavefront
-    constexpr int TB = 8;        // 16-token blocks per wavefront
+    static_assert(TB == 8 || TB == 6, "16-token blocks per wavefront");
+    constexpr int BM = 32 * TB;   // tokens of a tile
     constexpr int NLW = 4;        // wavefronts that issue the loads (the first four: see below)
-    constexpr int NCH = 32 / NLW;  // 1 KiB chunks (8 rows) per loading wavefront and tile
+    constexpr int NCH = 32 / NLW;  // 1 KiB chunks (8 rows) per loading wavefront and w tile
+    constexpr int NCHX = TB;       // and x tile
     constexpr int ROWB = 128;  // bytes per row of a tile
     constexpr int NKS = 2;     // contraction slices (32 indices) per step
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -139,9 +142,9 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     auto set_load_tile = [&](int i) __attribute__((always_inline)) {
         int tm, tn;
         tile_coords(i, tm, tn);
-        xrow_max = a.M - 1 - tm * kLinBM;
+        xrow_max = a.M - 1 - tm * BM;
         wrow_max = a.N - 1 - tn * kLinBN;
-        xtile = reinterpret_cast<const uint8_t*>(a.x + (int64_t)tm * kLinBM * a.ldx);
+        xtile = reinterpret_cast<const uint8_t*>(a.x + (int64_t)tm * BM * a.ldx);
         wtile = reinterpret_cast<const uint8_t*>(a.w + (int64_t)tn * kLinBN * a.ldw);
     };
     set_load_tile(0);
@@ -176,7 +179,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     auto dma_x = [&](int buf) {
         if (!loader) return;
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) dma_x_chunk(buf, i);
+        for (int i = 0; i < NCHX; ++i) dma_x_chunk(buf, i);
     };
     auto dma_w = [&](int buf) {
         if (!loader) return;
@@ -239,7 +242,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     // load in flight -- vmcnt(0) -- in front of the barrier, and the x tile that is meant to stay in
     // flight across it would be waited for after all)
     auto sync_point = [&]() __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NCH) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NCHX) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         asm volatile("" : "+v"(l));
         const int r = 8 * ((wave & (NLW - 1)) + NLW * (l >> 3)) + (l & 7);
         uint8_t* const row = smem + kWBase + buf * kLinTileBytes + r * ROWB;
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NCH) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NCHX) : "memory");
         for (int p = a.tail >> 4; p < 8; ++p) {
             u32x4* const at = reinterpret_cast<u32x4*>(row + 16 * (p ^ ((r >> 1) & 7)));
             u32x4 v = mk4(0u, 0u, 0u, 0u);
@@ -317,7 +320,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
             else *at = v;
         };
         // (16-bit output only: with fp32 output the extra path costs the step loop a register)
-        const bool full = !OUT_F32 && (tm + 1) * kLinBM <= a.M && (tn + 1) * kLinBN <= a.N;  // uniform
+        const bool full = !OUT_F32 && (tm + 1) * BM <= a.M && (tn + 1) * kLinBN <= a.N;  // uniform
 #pragma unroll
         for (int pass = 0; pass < TB / TBP; ++pass) {
             if constexpr (REREAD) {
@@ -331,7 +334,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 const int row = BR * h + lr;
                 float xs = 1.f;
                 if constexpr (OP == OP_I8) {
-                    const int m = tm * kLinBM + (wt * TB + tb) * BR + lr;
+                    const int m = tm * BM + (wt * TB + tb) * BR + lr;
                     xs = a.x_scale[m < a.M ? m : a.M - 1];
                 }
 #pragma unroll
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 return *reinterpret_cast<const u32x4*>(region + row * RB + ((rp ^ (row & (PR - 1))) << 4));
             };
             auto put = [&](int k, u32x4 v) __attribute__((always_inline)) {
-                const int m = tm * kLinBM + wt * BR * TB + pass * RP + k * (64 / PR) + rrow;
+                const int m = tm * BM + wt * BR * TB + pass * RP + k * (64 / PR) + rrow;
                 // N is a multiple of 8: a piece of a row is inside or outside as a whole
                 if (m < a.M && n < a.N)
                     store_piece(reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES), v);
@@ -379,7 +382,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3])::"memory");
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int m = tm * kLinBM + wt * BR * TB + pass * RP + k * (64 / PR) + rrow;
+                    const int m = tm * BM + wt * BR * TB + pass * RP + k * (64 / PR) + rrow;
                     store_piece(reinterpret_cast<u32x4*>(static_cast<uint8_t*>(a.y) + ((int64_t)m * a.ldy + n) * ES), v[k]);
                 }
             } else {
@@ -477,7 +480,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         const int tok_end = a.qkv_nKT * kBK;  // slots of the sequence's tiles
 #pragma unroll
         for (int pass = 0; pass < TB / TBP; ++pass) {
-            const int tok0 = tm * kLinBM + wt * BR * TB + pass * RP;  // a multiple of 32: half a key tile
+            const int tok0 = tm * BM + wt * BR * TB + pass * RP;  // a multiple of 32: half a key tile
             float rs2[TBP] = {1.f, 1.f};
             if (normed) {
                 float* const mine = reinterpret_cast<float*>(region);
@@ -663,11 +666,12 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
             // reads issued behind the youngest fragment this pair needs (its second x fragment), from the issue order
             // below: the x fragments of the pairs behind it and, from the second pair on, the next slice's w fragments
             if constexpr (P == 0) {
-                asm volatile("s_waitcnt lgkmcnt(4)"
+                asm volatile("s_waitcnt lgkmcnt(%6)"
                              : "+v"(W[cur][0]), "+v"(W[cur][1]), "+v"(W[cur][2]), "+v"(W[cur][3]), "+v"(X[T]),
-                               "+v"(X[T + 1]));
+                               "+v"(X[T + 1])
+                             : "n"(TB - 4));
             } else {
-                asm volatile("s_waitcnt lgkmcnt(8)" : "+v"(X[T]), "+v"(X[T + 1]));
+                asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(X[T]), "+v"(X[T + 1]) : "n"(TB));
             }
             static_for<0, 2 * FB>([&](auto mc) __attribute__((always_inline)) {
                 constexpr int m = decltype(mc)::value, fb = m >> 1, tb = T + (m & 1);
@@ -738,9 +742,9 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last steps
 }
 
-template <int OP, bool OUT_F32, int QKV, bool TAIL = false, bool PAST = false>
+template <int OP, bool OUT_F32, int QKV, bool TAIL = false, bool PAST = false, int TB = 8>
 hipError_t launch_linear_inst(const LinearArgs& a, int cus, hipStream_t s) {
-    auto kern = linear_kernel<OP, OUT_F32, QKV, TAIL, PAST>;
+    auto kern = linear_kernel<OP, OUT_F32, QKV, TAIL, PAST, TB>;
     constexpr int smem = (kLinSX + kLinSW) * kLinTileBytes;
     static std::atomic<uint64_t> attr_set{0};
     hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
@@ -769,19 +773,23 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t s) {
 namespace {
 
 template <bool OUT_F32, bool TAIL>
-hipError_t launch_linear_i8(const LinearArgs& a, int cus, hipStream_t s) {
+hipError_t launch_linear_i8(const LinearArgs& a, int rows, int cus, hipStream_t s) {
+    if (rows == 192) return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false, 6>(a, cus, s);
     if (exceeds_caches((int64_t)a.M * a.N * (OUT_F32 ? 4 : 2))) return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, true>(a, cus, s);
     return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false>(a, cus, s);
 }
 
 }  // namespace
 
-hipError_t launch_linear_i8(const LinearArgs& a, hipStream_t s) {
+hipError_t launch_linear_i8(LinearArgs a, int rows, hipStream_t s) {
     int cus = 0;
     const hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
-    if (a.tail > 0) return a.out_f32 ? launch_linear_i8<true, true>(a, cus, s) : launch_linear_i8<false, true>(a, cus, s);
-    return a.out_f32 ? launch_linear_i8<true, false>(a, cus, s) : launch_linear_i8<false, false>(a, cus, s);
+    a.nTM = (a.M + rows - 1) / rows;
+    a.nTN = (a.N + kLinBN - 1) / kLinBN;
+    if ((int64_t)a.nTM * a.nTN > 0x7fffffff) return hipErrorInvalidValue;
+    if (a.tail > 0) return a.out_f32 ? launch_linear_i8<true, true>(a, rows, cus, s) : launch_linear_i8<false, true>(a, rows, cus, s);
+    return a.out_f32 ? launch_linear_i8<true, false>(a, rows, cus, s) : launch_linear_i8<false, false>(a, rows, cus, s);
 }
 
 }  // namespace dit

@@ -197,7 +197,7 @@ int choose_linear_quant(int M, int N, int K, int cus, int* features) {
         *features = f < 8 ? 8 : f;
         return 0;
     }
-    return choose_linear_form_i8(M, N, K, N >= 8, cus);
+    return choose_linear_form_i8(M, N, K, cus);
 }
 
 hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
@@ -228,21 +228,18 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     a.ldw = q.ldw / 2;
     a.ldy = q.ldy;
     a.out_f32 = q.out_f32;
-    if (form) return launch_linear_small_i8(a, form, s);
+    if (form && form != 64) return launch_linear_small_i8(a, form, s);
     // 256 x 256 tiles store whole 16-byte pieces: the last N % 8 features are a call of their own
     const int rest = a.N % 8;
     a.N -= rest;
-    a.nTM = (a.M + kLinBM - 1) / kLinBM;
-    a.nTN = (a.N + kLinBN - 1) / kLinBN;
-    if ((int64_t)a.nTM * a.nTN > 0x7fffffff) return hipErrorInvalidValue;
-    e = launch_linear_i8(a, s);
+    e = launch_linear_i8(a, form == 64 ? 192 : 256, s);
     if (e != hipSuccess || rest == 0) return e;
     a.w += (int64_t)a.N * a.ldw;
     a.w_scale += a.N;
     if (a.bias) a.bias += a.N;
     a.y = static_cast<uint8_t*>(a.y) + (int64_t)a.N * (a.out_f32 ? 4 : 2);
     a.N = rest;
-    return launch_linear_small_i8(a, choose_linear_form_i8(a.M, a.N, q.K, false, cus), s);
+    return launch_linear_small_i8(a, choose_linear_form_i8(a.M, a.N, q.K, cus), s);
 }
 
 }  // namespace dit

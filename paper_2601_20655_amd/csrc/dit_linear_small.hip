@@ -183,21 +183,30 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     // ---- what is left of K: one more step, staged through registers, the bytes behind the rows' ends zeros
     if constexpr (ANY) {
         if (a.tail > 0) {
-            for (int p = tid; p < (T::BN + T::BM) * 8; p += 512) {
-                const int line = p >> 3, r = line < T::BN ? line : line - T::BN;
+            constexpr int PIECES = (T::BN + T::BM) * 8, TURNS = (PIECES + 511) / 512;
+            u32x4 v[TURNS];
+#pragma unroll
+            for (int i = 0; i < TURNS; ++i) {  // (all are asked for before the first is waited for)
+                const int p = tid + 512 * i, line = p >> 3, r = line < T::BN ? line : line - T::BN;
                 const int at = 16 * ((p & 7) ^ ((r >> 1) & 7));
                 const bool is_w = line < T::BN;
                 const int row0 = is_w ? tn * T::BN : tm * T::BM, end = is_w ? a.N : a.M;
                 const int row = row0 + r < end ? row0 + r : end - 1;
                 const uint16_t* const from = (is_w ? a.w + (int64_t)row * a.ldw : a.x + (int64_t)row * a.ldx) + a.K;
-                u32x4 v = mk4(0u, 0u, 0u, 0u);
-                if (at < a.tail) v = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(from) + at);
+                v[i] = mk4(0u, 0u, 0u, 0u);
+                if (p < PIECES && at < a.tail)
+                    v[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(from) + at);
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int bits = 8 * (a.tail - at - 4 * i);  // of this dword, those that count
-                    v[i] = bits <= 0 ? 0u : bits < 32 ? v[i] & ((1u << bits) - 1u) : v[i];
+            for (int i = 0; i < TURNS; ++i) {
+                const int p = tid + 512 * i, line = p >> 3, r = line < T::BN ? line : line - T::BN;
+                const int at = 16 * ((p & 7) ^ ((r >> 1) & 7));
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int bits = 8 * (a.tail - at - 4 * d);  // of this dword, those that count
+                    v[i][d] = bits <= 0 ? 0u : bits < 32 ? v[i][d] & ((1u << bits) - 1u) : v[i][d];
                 }
-                *reinterpret_cast<u32x4*>(smem + 16 * p) = v;
+                if (p < PIECES) *reinterpret_cast<u32x4*>(smem + 16 * p) = v[i];
             }
             __syncthreads();
 #pragma unroll
@@ -318,13 +327,18 @@ struct Form {
 constexpr Form kForms[] = {{1, 1, 0.20, 0.35, 2.5}, {2, 1, 0.215, 0.36, 2.5}, {2, 2, 0.33, 0.55, 3.0}, {4, 2, 0.47, 0.0, 3.0},
                            {3, 4, 0.74, 0.0, 3.5},  {4, 4, 0.76, 0.0, 4.0},   {5, 4, 1.05, 0.0, 4.0}};
 
-// The tile the estimate says is fastest for nK steps (10 TB + FB), 0 for the big kernel, which keeps what is not 5 % slower
-// there (and is left out of it without `big_too`).
-int best_form(int M, int N, double nK, int cus, bool big_too) {
+}  // namespace
+
+// The tile the estimate says is fastest (10 TB + FB), 0 for the big kernel, which keeps what is not 5 % slower there.
+// Measured, us a call one after the other on the same operands: M x N x K = 769 x 10,240 x 5,120: 98 in 256 x 256 tiles
+// (160 of them), 80 in 160 x 256 (with other work between the calls 98 and 88); 769 x 5,120 x 5,120: 82 and 56 (96 x 256);
+// 512 x 3,072 x 1,536: 28 and 9 (64 x 128); 172 x 3,664 x 3,072: 51 and 11 (64 x 64); 1 x 15,360 x 5,120: 80 and 23;
+// 3,600 x 5,120 x 5,120: 193 and 161 (160 x 256); kept: 14,040 x 1,536 x 1,536 (66), 3,600 x 15,360 x 5,120 (430).
+int choose_linear_form(int M, int N, int K, int cus) {
+    const double nK = K / kLinBK;
     auto tiles_of = [&](int bm, int bn) { return (int64_t)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     const int64_t big = tiles_of(kLinBM, kLinBN), full = big / cus, rest = big % cus;
     double best = 0.95 * (7.0 + full * (1.2 * nK + 3.5) + (rest == 0 ? 0.0 : (rest <= cus / 2 ? 1.0 : 1.2) * nK + 3.5));
-    if (!big_too) best = 1e30;
     int form = 0;
     for (const Form& f : kForms) {
         const int64_t tiles = tiles_of(32 * f.tb, 64 * f.fb);
@@ -341,14 +355,6 @@ int best_form(int M, int N, double nK, int cus, bool big_too) {
     return form;
 }
 
-}  // namespace
-
-// Measured, us a call one after the other on the same operands: M x N x K = 769 x 10,240 x 5,120: 98 in 256 x 256 tiles
-// (160 of them), 80 in 160 x 256 (with other work between the calls 98 and 88); 769 x 5,120 x 5,120: 82 and 56 (96 x 256);
-// 512 x 3,072 x 1,536: 28 and 9 (64 x 128); 172 x 3,664 x 3,072: 51 and 11 (64 x 64); 1 x 15,360 x 5,120: 80 and 23;
-// 3,600 x 5,120 x 5,120: 193 and 161 (160 x 256); kept: 14,040 x 1,536 x 1,536 (66), 3,600 x 15,360 x 5,120 (430).
-int choose_linear_form(int M, int N, int K, int cus) { return best_form(M, N, K / kLinBK, cus, true); }
-
 hipError_t launch_linear_small(const LinearArgs& a, int form, hipStream_t s) {
 #define DIT_TILE(TB, FB) \
     if (form == 10 * TB + FB)       \
@@ -364,10 +370,43 @@ hipError_t launch_linear_small(const LinearArgs& a, int form, hipStream_t s) {
     return hipErrorInvalidValue;
 }
 
-// A step of 8-bit operands is the same bytes and the same number of matrix instructions of the same length as one of 16-bit
-// operands, of twice the contraction indices: the same estimates.
-int choose_linear_form_i8(int M, int N, int K, bool big_too, int cus) {
-    return best_form(M, N, (K + 127) / 128, cus, big_too);
+namespace {
+
+// The same for 8-bit operands, whose steps are as many bytes and matrix instructions for twice the contraction indices:
+// microseconds of a step where less than 0.8 of the compute units work, and where all do (by then the board's power limit holds
+// them back), fitted to runs over 40 shapes (M 17 .. 32,760, N 1,536 .. 20,480, K 700 .. 20,480); tiles of 192 and 256 rows
+// are the big kernel's.
+struct FormI8 {
+    int tb, fb, slots;
+    double light, full, ends, start;
+};
+constexpr FormI8 kFormsI8[] = {{1, 1, 2, 0.16, 0.31, 2.5, 3.0}, {2, 1, 2, 0.16, 0.50, 2.5, 3.0},  {2, 2, 2, 0.275, 0.70, 3.0, 3.0},
+                               {4, 2, 1, 0.38, 0.60, 3.5, 3.0}, {3, 4, 1, 0.58, 0.78, 4.0, 3.0},  {4, 4, 1, 0.66, 0.88, 5.0, 3.0},
+                               {5, 4, 1, 0.88, 1.04, 6.0, 3.0}, {6, 4, 1, 0.85, 1.13, 3.5, 7.0},  {8, 4, 1, 1.00, 1.40, 5.5, 7.0}};
+
+}  // namespace
+
+// Measured, us, 256, 192 and the best of fewer rows: 7,800 x 4,608 x 1,536 65, 58 and 77; 14,040 x 1,536 x 1,536 43, 38 and 47;
+// 3,600 x 5,120 x 5,120 108, 89 and 91; 14,040 x 4,608 x 1,536 98, 110 and 127; 32,760 x 5,120 x 5,120 636, 680 and 793.
+int choose_linear_form_i8(int M, int N, int K, int cus) {
+    const double nK = (K + 127) / 128;
+    double best = 1e30;
+    int form = 0;
+    for (const FormI8& f : kFormsI8) {
+        if (f.tb > 5 && N < 8) continue;  // (stored in whole pieces)
+        const int64_t tiles = (int64_t)((M + 32 * f.tb - 1) / (32 * f.tb)) * ((N + 64 * f.fb - 1) / (64 * f.fb));
+        const int64_t rounds = tiles / (f.slots * cus), left = tiles % (f.slots * cus);
+        // (workgroups in pairs: a first pair on a compute unit takes half of what all pairs add)
+        const double step = f.slots == 2 ? left <= cus ? f.light : f.light + (f.full - f.light) * (0.45 + 0.55 * (left - cus) / cus)
+                                         : left <= 0.8 * cus ? f.light : 0.5 * (f.light + f.full);
+        const double ends = f.ends + (f.tb < 6 && K % 128 ? 2.0 : 0.0);  // (the rest of K: a step that nothing hides)
+        const double t = f.start + rounds * (f.full * nK + ends) + (left == 0 ? 0.0 : step * nK + ends);
+        if (t < best) {
+            best = t;
+            form = f.tb == 8 ? 0 : 10 * f.tb + f.fb;
+        }
+    }
+    return form;
 }
 
 hipError_t launch_linear_small_i8(const LinearArgs& a, int form, hipStream_t s) {
