@@ -496,12 +496,13 @@ dit_status dit_dequant_rows_forward(const int8_t *q, const float *scale, void *y
 
 /*
  * The projection of dit_linear_forward on 8-bit rows, a scale for each token and one for each output channel:
- *     y[m, n] = (sum_k x[m, k] w[n, k]) * (x_scale[m] * w_scale[n]) + bias[n].
+ *     y[m, n] = (sum_k x[m, k] w[n, k]) * x_scale[m] * w_scale[n] + bias[n].
  * x: [M, K] int8, x_scale: [M] fp32; w: [N, K] int8, w_scale: [N] fp32; bias: [N] bf16 or NULL; y: [M, N] bf16 or fp32
  * (out_dtype).  Strides in ELEMENTS.  The sum is an exact 32-bit integer, so results do not depend on the order of the
  * sum nor on the tiles: a row of y depends on its own x row alone, bit for bit.  It is rounded to fp32 (a relative 2^-24),
- * scaled and biased in fp32, and rounded once if y is bf16.  M, N and K need not be multiples of anything (K a
- * multiple of 128 is fastest); M = 1 is a pass over the weights.  Every 8-bit value counts, -128 too.
+ * scaled by the token's and then by the channel's scale and biased in fp32, and rounded once if y is bf16.  M, N and K need
+ * not be multiples of anything; K and row strides that are multiples of 128 are fastest (8,192 x 5,120 x 5,100 on rows 5,104
+ * bytes apart 237 us, 5,120 apart 186).  M = 1 is a pass over the weights.  Every 8-bit value counts, -128 too.
  * x and w are read in whole 16-byte pieces: the bytes between the end of a row and the next multiple of 16 are read
  * (also behind the last row) and not used.  x and w may not overlap y.  No workspace.
  * Errors: NULL x, x_scale, w, w_scale, y or p, M, N or K < 1, a stride shorter than its row, bad out_dtype or nonzero

@@ -275,7 +275,7 @@ struct LinearArgs {
     float qkv_eps;
     const float* qkv_kgamma;     // nullable [H*128]
     // 8-bit operands: x and w hold pairs of signed 8-bit integers (K, ldx and ldw count pairs; K the whole steps only), the
-    // sums are integers, and y = sum * (x_scale * w_scale) + bias
+    // sums are integers, and y = sum * x_scale * w_scale + bias
     const float* x_scale;  // [M]
     const float* w_scale;  // [N]
     int tail;              // 8-bit integers of a row behind the whole steps, 0 .. 127 (tiles of dit_linear_small.hip only)

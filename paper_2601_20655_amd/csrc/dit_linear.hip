@@ -295,9 +295,11 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         const int n = tn * kLinBN + wf * BR * FB + rp * (16 / ES);
         uint2 bb[FB];
         f32x4 ws[FB];  // (8-bit operands)
-        // (read again in every pass where holding them through all of them costs spills)
-        constexpr bool REREAD = OP == OP_I8 && (OUT_F32 || TAIL);
-        [[maybe_unused]] auto load_features = [&](int lgp) __attribute__((always_inline)) {
+        // (read again in every pass: held through all of them they cost spills, and 1,845 us become 2,000 at 32,760 x 15,360 x
+        // 5,120)
+        [[maybe_unused]] auto load_features = [&]() __attribute__((always_inline)) {
+            int lgp = lg;
+            asm volatile("" : "+v"(lgp));
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
                 const int n0 = tn * kLinBN + wf * BR * FB + fb * BR + 4 * lgp;
@@ -305,9 +307,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                 ws[fb] = scales_of_4<false>(a.w_scale, n0, a.N);
             }
         };
-        if constexpr (OP == OP_I8) {
-            if constexpr (!REREAD) load_features(lg);
-        } else {
+        if constexpr (OP != OP_I8) {
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
                 const int n0 = tn * kLinBN + wf * BR * FB + fb * BR + 4 * lg;
@@ -323,11 +323,7 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
         const bool full = !OUT_F32 && (tm + 1) * BM <= a.M && (tn + 1) * kLinBN <= a.N;  // uniform
 #pragma unroll
         for (int pass = 0; pass < TB / TBP; ++pass) {
-            if constexpr (REREAD) {
-                int lgp = lg;
-                asm volatile("" : "+v"(lgp));
-                load_features(lgp);
-            }
+            if constexpr (OP == OP_I8) load_features();
 #pragma unroll
             for (int h = 0; h < TBP; ++h) {
                 const int tb = pass * TBP + h;
@@ -343,11 +339,12 @@ __global__ void __launch_bounds__(64 * kLinWaves, 1) linear_kernel(const LinearA
                     const float b2 = __uint_as_float(bb[fb].y << 16), b3 = __uint_as_float(bb[fb].y & 0xffff0000u);
                     float y0, y1, y2, y3;
                     if constexpr (OP == OP_I8) {
-                        // (the sum is rounded to fp32 here, a relative 2^-24)
-                        y0 = fmaf((float)acc[fb][tb][0], xs * ws[fb][0], b0);
-                        y1 = fmaf((float)acc[fb][tb][1], xs * ws[fb][1], b1);
-                        y2 = fmaf((float)acc[fb][tb][2], xs * ws[fb][2], b2);
-                        y3 = fmaf((float)acc[fb][tb][3], xs * ws[fb][3], b3);
+                        // (the sum is rounded to fp32 here, a relative 2^-24; scaled one by one, so that the scales' product need not be
+                        // a normal number)
+                        y0 = fmaf((float)acc[fb][tb][0] * xs, ws[fb][0], b0);
+                        y1 = fmaf((float)acc[fb][tb][1] * xs, ws[fb][1], b1);
+                        y2 = fmaf((float)acc[fb][tb][2] * xs, ws[fb][2], b2);
+                        y3 = fmaf((float)acc[fb][tb][3] * xs, ws[fb][3], b3);
                     } else {
                         y0 = acc[fb][tb][0] + b0;
                         y1 = acc[fb][tb][1] + b1;

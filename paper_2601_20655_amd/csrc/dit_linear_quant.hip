@@ -1,4 +1,4 @@
-// Projection of 8-bit rows: y[m, n] = (sum_k x[m, k] w[n, k]) * (x_scale[m] * w_scale[n]) + bias[n], the sum an exact 32-bit
+// Projection of 8-bit rows: y[m, n] = (sum_k x[m, k] w[n, k]) * x_scale[m] * w_scale[n] + bias[n], the sum an exact 32-bit
 // integer on the matrix cores.  Few token rows are done here, straight from memory; more by the tiles of dit_linear.hip and
 // dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
 #include "dit_attn_device.h"
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantAr
         int sum = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += part[(w * FB * TB + at) * 64 + l][f & 3];
-        const float y = fmaf((float)sum, a.x_scale[m] * a.w_scale[n], a.bias ? __uint_as_float((uint32_t)a.bias[n] << 16) : 0.f);
+        const float y = fmaf((float)sum * a.x_scale[m], a.w_scale[n], a.bias ? __uint_as_float((uint32_t)a.bias[n] << 16) : 0.f);
         const int64_t o = (int64_t)m * a.ldy + n;
         if constexpr (OUT_F32) static_cast<float*>(a.y)[o] = y;
         else static_cast<uint16_t*>(a.y)[o] = (uint16_t)pack2<OP_BF16>(y, 0.f);

@@ -261,11 +261,12 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
         for (int fb = 0; fb < FB; ++fb) {
             float y0, y1, y2, y3;
             if constexpr (OP == OP_I8) {
-                // (the sum is rounded to fp32 here, a relative 2^-24)
-                y0 = fmaf((float)acc[fb][tb][0], xs * ws[fb][0], b[fb][0]);
-                y1 = fmaf((float)acc[fb][tb][1], xs * ws[fb][1], b[fb][1]);
-                y2 = fmaf((float)acc[fb][tb][2], xs * ws[fb][2], b[fb][2]);
-                y3 = fmaf((float)acc[fb][tb][3], xs * ws[fb][3], b[fb][3]);
+                // (the sum is rounded to fp32 here, a relative 2^-24; scaled one by one, so that the scales' product need not be a
+                // normal number)
+                y0 = fmaf((float)acc[fb][tb][0] * xs, ws[fb][0], b[fb][0]);
+                y1 = fmaf((float)acc[fb][tb][1] * xs, ws[fb][1], b[fb][1]);
+                y2 = fmaf((float)acc[fb][tb][2] * xs, ws[fb][2], b[fb][2]);
+                y3 = fmaf((float)acc[fb][tb][3] * xs, ws[fb][3], b[fb][3]);
             } else {
                 y0 = acc[fb][tb][0] + b[fb][0];
                 y1 = acc[fb][tb][1] + b[fb][1];

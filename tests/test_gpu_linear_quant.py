@@ -154,6 +154,18 @@ def test_scales_that_are_not_numbers(M):
     assert np.array_equal(y[2][cols], bias[cols])
 
 
+@pytest.mark.parametrize("M", [2, 40, 300, 3000])
+def test_scales_whose_product_is_no_normal_number(M):
+    """Scales of 2^-75 and 2^-60: their product underflows fp32, sums of a million times as much do not."""
+    x, xs, w, ws, _ = operands(M, 520, 640, seed=M)
+    xs, ws = np.full(M, 2.0 ** -75, np.float32), np.full(520, 2.0 ** -60, np.float32)
+    x[0] = w[0] = 127
+    y = run(x, xs, w, ws, None, "f32")
+    keep = np.abs(x.astype(np.float64) @ w.astype(np.float64).T) >= 2.0 ** 14  # (normal results)
+    ref = (x.astype(np.float64) @ w.astype(np.float64).T) * 2.0 ** -135
+    assert np.all(np.abs(y[keep] - ref[keep]) <= 4 * R.U * np.abs(ref[keep])) and y[0, 0] > 0
+
+
 def test_offsets_beyond_32_bits():
     """Rows of x and y 2^17 bytes and elements apart, 33,000 of them; rows of w as far apart."""
     import torch
