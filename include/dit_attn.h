@@ -422,8 +422,9 @@ dit_status dit_qkv_proj_forward(const void *x, const void *w, const void *bias, 
  *
  * A QUANTISED ROW is N signed 8-bit integers q and one fp32 scale, and stands for the numbers q[n] * scale.  The
  * quantisation is symmetric, one scale a row: with amax the largest magnitude of the row's numbers t,
- *     scale = amax / 127,   q[n] = round to nearest even (t[n] * (127 / amax)),   in [-127, 127],
- * so the largest number is kept, and every other is off by at most half a scale.  All of it is computed in fp32.
+ *     scale = amax / 127,   q[n] = round to nearest even (t[n] * (127 * (1 / amax))),   in [-127, 127],
+ * so the largest number is kept, and every other is off by at most half a scale.  All of it is computed in
+ * fp32, operation by operation as written.
  *   - A row whose amax is below 2^-120 (a row of zeros) gets scale 0 and q 0.
  *   - A row with a NaN or an infinity gets scale NaN and q 0: whatever reads the row yields NaN, and no other row is touched.
  * 8-bit rows start on multiples of 16 bytes, like every row; exactly N bytes of a row are written.  Scales are dense:

@@ -4,7 +4,7 @@
 // A row has to be seen whole before its first integer is known, and is read once: W wavefronts hold it in registers, C
 // chunks of eight columns a lane, exchange its largest magnitude (and sum of squares) and write its integers.  The
 // normalisation's factor 1 / sqrt(mean + eps) is common to the row, so it cancels in the integers
-// q = rint(t * 127 / max|t|), t = h * gamma, and appears in the scale alone: the integers do not wait for the sum.
+// q = rint(t * (127 * (1 / max|t|))), t = h * gamma, and appears in the scale alone: the integers do not wait for the sum.
 //
 // What bounds it: memory.  32,760 x 5,120, new rows at every call: norm with 16-bit residual 194 us (6.0 TB/s of reads and
 // writes), with a 32-bit one 332 (5.6), without 104 (4.8), 16-bit rows to 8 bits 82 (6.1), back to 16 bits 82 (6.1) and 32 bits
@@ -88,8 +88,13 @@ __device__ __forceinline__ void store_number(void* row, int i, float v) {
 }
 
 // v * inverse, rounded to the nearest even integer of magnitude 127 or less, in the low byte: 1.5 * 2^23 puts the integer's
-// two's complement into the last bits of the significand
-__device__ __forceinline__ uint32_t to_byte(float v, float inverse) { return __float_as_uint(fmaf(v, inverse, 12582912.0f)); }
+// two's complement into the last bits of the significand.  (Product and sum are rounded one after the other, as the formula
+// has them: fused, one number in ten million fell to the other side of a tie.)
+__device__ __forceinline__ uint32_t to_byte(float v, float inverse) {
+#pragma clang fp contract(off)
+    const float p = v * inverse;
+    return __float_as_uint(p + 12582912.0f);
+}
 __device__ __forceinline__ uint32_t to_bytes(const float v[4], float inverse) {
     const uint32_t lo = __builtin_amdgcn_perm(to_byte(v[1], inverse), to_byte(v[0], inverse), 0x0c0c0400u);
     const uint32_t hi = __builtin_amdgcn_perm(to_byte(v[3], inverse), to_byte(v[2], inverse), 0x04000c0cu);
@@ -269,7 +274,7 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
         factor = 1.0f / (sqrtf(sum / (float)a.N + a.eps) * kQuantTop);
     }
     const bool some = good && top >= kQuantZero;
-    const float inverse = some ? kQuantTop / top : 0.f;
+    const float inverse = some ? kQuantTop * (1.0f / top) : 0.f;
     if (part == 0 && lane == 0) a.scale[m] = !good ? NAN : some ? top * factor : 0.f;
     int8_t* const q = a.q + m * a.ldq;
 #pragma unroll

@@ -21,9 +21,9 @@ def norm_rows(x, gamma, residual, eps):
 def check_rows(q, scale, t, factor, q_slack=0.0, scale_rel=0.0, what=""):
     """8-bit rows against t (numbers that are quantised, but for a positive factor of the row, which is in the scale alone).
 
-    q = rint(t * (127 / amax)): t carries at most two roundings (the sum, the product with the weight), amax the same two,
-    the quotient and the product one each: six units of 2^-24 of at most 127, 4.6e-5, by which a number next to a tie may
-    fall to the other side.  So q is within 1/2 + 1e-4 (+ q_slack, one number a row) of the unrounded 64-bit number.
+    q = rint(t * (127 * (1 / amax))): t carries at most two roundings (the sum, the product with the weight), amax the same
+    two, the quotient and the products one each: seven units of 2^-24 of at most 127, 5.3e-5, by which a number next to a tie
+    may fall to the other side.  So q is within 1/2 + 1e-4 (+ q_slack, one number a row) of the unrounded 64-bit number.
     scale = amax * factor / 127: the two roundings of amax and three of its own, and scale_rel for the factor."""
     amax = np.abs(t).max(axis=1)
     with np.errstate(divide="ignore", invalid="ignore"):
