@@ -296,7 +296,8 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
 template <bool OUT_F32, int C, bool CUT, bool PAST>
 __global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, int parts) {
     constexpr int V = OUT_F32 ? 4 : 8;
-    typedef std::conditional_t<OUT_F32, uint32_t, uint2> piece_t;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef std::conditional_t<OUT_F32, uint32_t, u32x2> piece_t;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t id = (int64_t)blockIdx.x * 4 + wave;
@@ -312,7 +313,14 @@ __global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, 
     for (int c = 0; c < C; ++c) {
         const int at = first + c * 64;
         b[c] = piece_t();
-        if (at < whole) b[c] = *reinterpret_cast<const piece_t*>(q + V * (int64_t)at);
+        if (at < whole) {
+            const piece_t* const p = reinterpret_cast<const piece_t*>(q + V * (int64_t)at);
+            // (past the caches too with 16-bit rows: GELU and reading back, 32,760 x 20,480, 690 -> 642 us; with 32-bit ones
+            // 128 -> 130.  The 8-bit rows' own stores stay: this call finds them there, 148 us for rows to 8 bits and back at
+            // 32,760 x 5,120, 162 with stores past the caches)
+            if constexpr (PAST && !OUT_F32) b[c] = __builtin_nontemporal_load(p);
+            else b[c] = *p;
+        }
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
