@@ -23,10 +23,10 @@ __device__ __forceinline__ u32x4 load_cut_piece(const int8_t* row, int at, int e
 typedef const __attribute__((address_space(1))) void* gptr_t;
 typedef __attribute__((address_space(3))) void* lptr_t;
 
-// Few token rows: XI groups of 8.  A workgroup takes all of them and F features, WI groups of 8 (the last one may be cut); its
-// NW wavefronts share K in blocks of 128 bytes, one after the other, and add their sums at the end.  A wavefront streams its
-// blocks through S stages of LDS of its own: the load-to-LDS DMA moves 8 rows of a block an instruction, whole lines, and no
-// wavefront waits for another before the end.
+// Few token rows, or few tiles of a long sum: a workgroup takes 8 XI rows and F features, WI groups of 8 (the last one may be
+// cut); its NW wavefronts share K in blocks of 128 bytes, one after the other, and add their sums at the end.  A wavefront
+// streams its blocks through S stages of LDS of its own: the load-to-LDS DMA moves 8 rows of a block an instruction, whole
+// lines, and no wavefront waits for another before the end.
 template <int XI, int WI, int NW, int S>
 struct FewTile {
     static constexpr int TB = (XI + 1) / 2, FB = (WI + 1) / 2;  // 16-token and 16-feature blocks
@@ -71,6 +71,7 @@ __global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantAr
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 15, lg = lane >> 4;
     const int n0 = blockIdx.x * F, n1 = n0 + F < a.N ? n0 + F : a.N;  // its features
+    const int m0 = blockIdx.y * (8 * XI), m1 = m0 + 8 * XI < a.M ? m0 + 8 * XI : a.M;  // and token rows
 
     // DMA sources: 8 rows of 128 bytes an instruction.  LDS is filled in lane order, so the bank swizzle (piece p of row r in slot
     // p ^ ((r >> 1) & 7)) is in which piece a lane fetches.  Rows past the end are the last one again (their sums are not
@@ -79,7 +80,7 @@ __global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantAr
 #pragma unroll
     for (int i = 0; i < T::LOADS; ++i) {
         const int r = 8 * (i < WI ? i : i - WI) + (lane >> 3);
-        const int row = i < WI ? (n0 + r < n1 ? n0 + r : n1 - 1) : (r < a.M ? r : a.M - 1);
+        const int row = i < WI ? (n0 + r < n1 ? n0 + r : n1 - 1) : (m0 + r < m1 ? m0 + r : m1 - 1);
         src[i] = (i < WI ? a.w + (int64_t)row * a.ldw : a.x + (int64_t)row * a.ldx) + 16 * ((lane & 7) ^ ((r >> 1) & 7));
     }
     const int whole = a.K >> 7;
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantAr
             u32x4 x[TB];
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb)
-                x[tb] = load_cut_piece(a.x + (int64_t)(16 * tb + lr < a.M ? 16 * tb + lr : a.M - 1) * a.ldx, at, a.K);
+                x[tb] = load_cut_piece(a.x + (int64_t)(m0 + 16 * tb + lr < m1 ? m0 + 16 * tb + lr : m1 - 1) * a.ldx, at, a.K);
 #pragma unroll
             for (int fb = 0; fb < FB; ++fb) {
                 const int n = n0 + 16 * fb + lr;
@@ -146,10 +147,10 @@ __global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantAr
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) part[((wave * FB + fb) * TB + tb) * 64 + lane] = acc[fb][tb];
     __syncthreads();
-    for (int i = tid; i < 16 * FB * a.M; i += 64 * NW) {
-        const int m = i / (16 * FB), f = i % (16 * FB), n = n0 + f;
+    for (int i = tid; i < 16 * FB * (m1 - m0); i += 64 * NW) {
+        const int r = i / (16 * FB), f = i % (16 * FB), m = m0 + r, n = n0 + f;
         if (n >= n1) continue;
-        const int at = (f >> 4) * TB + (m >> 4), l = 16 * ((f & 15) >> 2) + (m & 15);
+        const int at = (f >> 4) * TB + (r >> 4), l = 16 * ((f & 15) >> 2) + (r & 15);
         int sum = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += part[(w * FB * TB + at) * 64 + l][f & 3];
@@ -167,7 +168,7 @@ hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
     const hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + F - 1) / F)), dim3(64 * NW), smem, s, a, F);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + F - 1) / F), (unsigned)((a.M + 8 * XI - 1) / (8 * XI))), dim3(64 * NW), smem, s, a, F);
     return hipGetLastError();
 }
 
@@ -189,12 +190,20 @@ hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
 // Measured, us, this kernel and the best tile: 1 x 20,480 x 5,120 (three workgroups a unit) 22 and 26; 1 x 15,360 x 5,120 16 and 18;
 // 16 x 5,120 x 20,480 25 and 41; 32 x 5,120 x 5,120 7.8 and 10.5; 64 x 5,120 x 20,480 39 and 44; but 32 x 15,360 x 5,120 22 and 20,
 // 64 x 15,360 x 5,120 29 and 24.
+// More rows go there too, in blocks of 32 rows x 32 features, where those are no more than the compute units: a long sum is then
+// shared by four wavefronts and streams deeper than in a tile.  300 x 300 x 300 4.1 and 4.7, 298 x 768 x 5,376 7.6 and 11.2,
+// 1,049 x 26 x 9,426 10 and 17, 191 x 640 x 18,048 16 and 27; of 90 drawn sizes none loses more than 4 %.  Past that number the
+// tiles win: 859 x 320 x 2,688 (270 blocks) 9.1 and 7.2, 1,863 x 129 x 3,368 (295) 12.7 and 10.3.
 int choose_linear_quant(int M, int N, int K, int cus, int* features) {
     const int64_t per = ((int64_t)N + 32 * cus - 1) / (32 * cus);  // workgroups a compute unit
     *features = 0;
     if (M <= 16 ? per <= 3 : M <= 64 && per == 1) {
         const int f = (int)((N + per * cus - 1) / (per * cus));
         *features = f < 8 ? 8 : f;
+        return 0;
+    }
+    if (M > 64 && (int64_t)((M + 31) / 32) * ((N + 31) / 32) <= cus) {
+        *features = N < 32 ? (N + 7) / 8 * 8 : 32;
         return 0;
     }
     return choose_linear_form_i8(M, N, K, cus);
@@ -210,7 +219,7 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
         // (3 stages are level with 4 and better than 2 at 16 rows: 25 and 26 us; with more rows 2 leave room for two workgroups)
         if (q.M <= 8) return launch_few<1, 4, 3>(q, features, s);
         if (q.M <= 16) return launch_few<2, 4, 3>(q, features, s);
-        if (q.M <= 32) return launch_few<4, 4, 2>(q, features, s);
+        if (q.M <= 32 || q.M > 64) return launch_few<4, 4, 2>(q, features, s);
         return launch_few<8, 4, 2>(q, features, s);
     }
     LinearArgs a{};

@@ -64,17 +64,20 @@ def check_linear(y, xq, xs, wq, ws, bias, bf16_out, what=""):
 
 
 # Every kernel of the projection, with at least twice as many blocks of K as a ring of LDS stages holds: few rows (groups of 8
-# rows / groups of 8 features of a workgroup), the small tiles (10 x 32-row blocks + 64-feature blocks; "any": N cut, or K),
-# tiles of 192 ("64") and 256 ("big") rows x 256 features ("tail": K cut; "rest": the last N % 8 features in a call of their own).
+# rows / groups of 8 features of a workgroup), that kernel in blocks of 32 rows (/ groups of 8 features), the small tiles (10 x
+# 32-row blocks + 64-feature blocks; "any": N cut, or K), tiles of 192 ("64") and 256 ("big") rows x 256 features ("tail": K
+# cut; "rest": the last N % 8 features in a call of their own).
 KERNELS = [
     ("few1/1", 3, 173, 1959), ("few1/2", 2, 3116, 2259), ("few1/3", 7, 4146, 1738), ("few1/4", 4, 7456, 1920),
     ("few2/1", 14, 605, 2141), ("few2/2", 14, 2376, 1664), ("few2/3", 12, 8960, 1920), ("few2/4", 13, 7840, 2432),
     ("few4/1", 28, 8, 2432), ("few4/2", 30, 3234, 1729), ("few4/3", 21, 4368, 2304), ("few4/4", 17, 7752, 1664),
     ("few8/1", 47, 48, 1664), ("few8/2", 52, 2396, 1860), ("few8/3", 33, 4169, 2196), ("few8/4", 33, 6220, 1706),
-    ("11", 95, 432, 1792), ("11 any", 345, 29, 2412), ("21", 34, 8512, 1664), ("21 any", 4332, 66, 1675),
-    ("22", 5738, 136, 1664), ("22 any", 5445, 143, 1687), ("42", 5785, 296, 1664), ("42 any", 5782, 261, 1708),
-    ("34", 544, 6536, 1664), ("34 any", 513, 6555, 1801), ("44", 581, 9344, 1536), ("44 any", 4055, 1300, 1732),
-    ("54", 5409, 1296, 1664), ("54 any", 1051, 7375, 2048), ("64", 5742, 1304, 1792), ("64 tail", 5433, 1352, 1845),
-    ("64 rest", 3654, 2301, 1792), ("64 tail rest", 5405, 1313, 1686), ("big", 2819, 4360, 1536),
-    ("big tail", 1231, 9376, 1800), ("big rest", 1383, 8357, 1664), ("big tail rest", 1177, 9455, 1694),
+    ("blocks/1", 634, 8, 2176), ("blocks/2", 1957, 16, 2048), ("blocks/3", 1149, 24, 1795),
+    ("blocks/4", 95, 432, 1792), ("11", 19, 8360, 1920), ("11 any", 18, 8839, 1919), ("21", 34, 8512, 1664),
+    ("21 any", 4332, 66, 1675), ("22", 5738, 136, 1664), ("22 any", 5445, 143, 1687), ("42", 5785, 296, 1664),
+    ("42 any", 5782, 261, 1708), ("34", 544, 6536, 1664), ("34 any", 513, 6555, 1801), ("44", 581, 9344, 1536),
+    ("44 any", 4055, 1300, 1732), ("54", 5409, 1296, 1664), ("54 any", 1051, 7375, 2048), ("64", 5742, 1304, 1792),
+    ("64 tail", 5433, 1352, 1845), ("64 rest", 3654, 2301, 1792), ("64 tail rest", 5405, 1313, 1686),
+    ("big", 2819, 4360, 1536), ("big tail", 1231, 9376, 1800), ("big rest", 1383, 8357, 1664),
+    ("big tail rest", 1177, 9455, 1694),
 ]

@@ -110,6 +110,8 @@ def kernel_of(M, N, K, cus=256):
     form = f(M, N, K, cus, ctypes.byref(features))
     if features.value:
         assert form == 0 and 8 <= features.value <= 32
+        if M > 64:
+            return "blocks/%d" % ((features.value + 7) // 8)
         groups = next(g for g in (1, 2, 4, 8) if M <= 8 * g)
         return "few%d/%d" % (groups, (features.value + 7) // 8)
     if form not in (0, 64):
