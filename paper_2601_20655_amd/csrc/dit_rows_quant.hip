@@ -122,6 +122,28 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
     // is loaded number by number, by its one lane.
     const int whole = a.N >> 3, rest = CUT ? a.N & 7 : 0;
     const int first = part * 64 + lane, step = W * 64;
+    // (asked for ahead of everything: 7,800 x 1,537 with a 16-bit residual 19.0 us if the whole chunks are waited for first, 17.2
+    // this way)
+    float end_x[7] = {}, end_r[7] = {}, end_g[7] = {};
+    if (CUT && (whole & 63) == lane && (whole >> 6) % W == part) {
+#pragma unroll
+        for (int i = 0; i < 7; ++i) end_x[i] = load_number<X_F32>(x, 8 * whole + (i < rest ? i : 0));
+        if constexpr (RES != ROW_NONE) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i) end_r[i] = load_number<R_F32>(r, 8 * whole + (i < rest ? i : 0));
+        }
+        if (MODE == ROW_NORM && a.gamma) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i) end_g[i] = a.gamma[8 * whole + (i < rest ? i : 0)];
+        }
+    }
+    // Weights are asked for with the row, where they and it take no more than 60 registers (and the rows are not past the caches:
+    // norm of 32,760 x 5,120 with a 16-bit residual 193 us behind the row, 201 with it).  With them, and behind: 7,800 x 5,120
+    // without a residual 26 and 31, 7,800 x 1,536 9.0 and 10.1, with a 16-bit one 15.0 and 16.3, with a 32-bit one 26.6 and 28.5;
+    // but 3,600 x 5,120 with a 32-bit one, of more registers, 66 and 43.
+    constexpr bool AHEAD = MODE == ROW_NORM && !PAST && C > 1 &&
+                           C * (8 + (X_F32 ? 8 : 4) + (RES == ROW_NONE ? 0 : R_F32 ? 8 : 4)) + (CUT ? 21 : 0) <= 60;
+    [[maybe_unused]] Chunk<true> kg[C];
     float t[C][8];
     if constexpr (C == 1) {
 #pragma unroll
@@ -149,6 +171,15 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
             for (int c = 0; c < C; ++c) {
                 const int at = first + c * step;
                 kr[c] = load_chunk<R_F32, PAST>(r, 8 * (at < whole ? at : whole - 1));
+            }
+        }
+        if constexpr (AHEAD) {
+            if (a.gamma) {
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int at = first + c * step;
+                    kg[c] = load_chunk<true, false>(a.gamma, 8 * (at < whole ? at : whole - 1));
+                }
             }
         }
         // (All are asked for before the first is used.  Left to the compiler, loads sank behind the test for the row's end and
@@ -180,18 +211,8 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (first + c * step != whole) continue;
-            float v[7], w[7];
 #pragma unroll
-            for (int i = 0; i < 7; ++i) v[i] = load_number<X_F32>(x, 8 * whole + (i < rest ? i : 0));
-            if constexpr (RES != ROW_NONE) {
-#pragma unroll
-                for (int i = 0; i < 7; ++i) w[i] = load_number<R_F32>(r, 8 * whole + (i < rest ? i : 0));
-            }
-#pragma unroll
-            for (int i = 0; i < 7; ++i) {
-                if constexpr (RES != ROW_NONE) v[i] += w[i];
-                t[c][i] = i < rest ? v[i] : 0.f;
-            }
+            for (int i = 0; i < 7; ++i) t[c][i] = i < rest ? RES != ROW_NONE ? end_x[i] + end_r[i] : end_x[i] : 0.f;
         }
     }
 
@@ -223,15 +244,13 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
                 const int at = first + c * step;
                 if (at < whole) {
                     float g[8];
-                    load8(a.gamma, 8 * at, 1, g);
+                    if constexpr (AHEAD) to_numbers<true>(kg[c], g);
+                    else load8(a.gamma, 8 * at, 1, g);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) t[c][i] *= g[i];
                 } else if (CUT && at == whole) {
-                    float g[7];
 #pragma unroll
-                    for (int i = 0; i < 7; ++i) g[i] = a.gamma[8 * whole + (i < rest ? i : 0)];
-#pragma unroll
-                    for (int i = 0; i < 7; ++i) t[c][i] = i < rest ? t[c][i] * g[i] : t[c][i];
+                    for (int i = 0; i < 7; ++i) t[c][i] = i < rest ? t[c][i] * end_g[i] : t[c][i];
                 }
             }
         }
