@@ -271,3 +271,59 @@ def test_own_stream_and_graph():
             t.zero_()
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(results(), want[i]))
+
+
+# rows enough that a lane takes several chunks and a workgroup several rows, the last workgroup not full
+MANY = [(1101, 203), (1027, 520), (1030, 1001), (1050, 1537), (1026, 2567), (1025, 3333), (1041, 4999), (1024, 5120),
+        (521, 7777), (1100, 5121)]
+
+
+@pytest.mark.parametrize("M,N", MANY)
+@pytest.mark.parametrize("bf16", [True, False])
+def test_quant_many_rows(M, N, bf16):
+    test_quant_rows(M, N, bf16)
+    test_quant_rows_gelu(M, N, bf16)
+
+
+@pytest.mark.parametrize("M,N", MANY)
+@pytest.mark.parametrize("x_bf16,residual,gamma", [(True, "bf16", True), (True, "f32", True), (False, "f32", True),
+                                                   (False, "bf16", True), (True, "none", True), (False, "none", True)])
+def test_norm_quant_many_rows(M, N, x_bf16, residual, gamma):
+    test_norm_quant(M, N, x_bf16, residual, gamma)
+
+
+@pytest.mark.parametrize("N", [5120, 5121])
+@pytest.mark.parametrize("residual", ["none", "bf16", "f32"])
+def test_rows_larger_than_the_caches(N, residual):
+    """61 rows over and over, more than the caches hold: the results of a call on the 61 alone, but for the order in which
+    a row's squares are added up, which is in the scale."""
+    import torch
+
+    M, base = 27500, 61  # 282 MB of x
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    of = torch.arange(M, device="cuda") % base
+
+    def rows(dt):
+        r = torch.empty((M, (N + 15) // 16 * 16), dtype=dt, device="cuda")[:, :N]
+        few = torch.empty((base, (N + 15) // 16 * 16), dtype=dt, device="cuda")[:, :N]
+        few.copy_(torch.randn((base, N), generator=gen, device="cuda"))
+        r.copy_(few[of])
+        return r, few
+
+    x, x0 = rows(torch.bfloat16)
+    g = 1 + 0.25 * torch.randn(N, generator=gen, device="cuda")
+    r, r0 = (None, None) if residual == "none" else rows(torch.bfloat16 if residual == "bf16" else torch.float32)
+    got = B.dit_rms_norm_quant_forward(x, g, residual=r)
+    want = B.dit_rms_norm_quant_forward(x0, g, residual=r0)
+    assert torch.equal(got[0], want[0][of])
+    rel = ((got[1].double() - want[1].double()[of]) / want[1].double()[of]).abs().max().item()
+    assert rel <= 2 * (6 * R.U + R.norm_scale_rel(N)), rel
+    if r is not None:
+        assert torch.equal(got[2], want[2][of])
+    for act in ("none", "gelu"):
+        q, scale = B.dit_quant_rows_forward(x, act=act)
+        q0, scale0 = B.dit_quant_rows_forward(x0, act=act)
+        assert torch.equal(q, q0[of]) and torch.equal(scale, scale0[of])
+    for dt in (torch.bfloat16, torch.float32):
+        y = B.dit_dequant_rows_forward(q, scale, out_dtype=dt)
+        assert torch.equal(y, B.dit_dequant_rows_forward(q0, scale0, out_dtype=dt)[of])

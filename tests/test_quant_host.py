@@ -1,6 +1,9 @@
 """Refusals of the 8-bit row operators: every argument is checked before anything is launched, so these calls never touch
 the HIP runtime (no accepted call is made: the pointers are fake)."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 
@@ -100,6 +103,20 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         B._check_pieces("f", "x", torch.zeros(2 * 16 + 7, dtype=torch.int8).as_strided((3, 7), (16, 1)), 16)
     B._check_pieces("f", "x", torch.zeros(3 * 16, dtype=torch.int8).as_strided((3, 7), (16, 1)), 16)
+
+
+@pytest.mark.parametrize("compiler,std", [("gcc", "-std=c99"), ("g++", "-std=c++17")])
+def test_structs_as_c_lays_them_out(compiler, std, tmp_path):
+    if shutil.which(compiler) is None:
+        pytest.skip(compiler + " not found")
+    structs = ["dit_quant_rows_params", "dit_norm_quant_params", "dit_dequant_rows_params", "dit_linear_params"]
+    src = tmp_path / ("t.c" if compiler == "gcc" else "t.cpp")
+    src.write_text('#include "dit_attn.h"\n#include <stddef.h>\n#include <stdio.h>\nint main(void) {\n' + "".join(
+        '  printf("%%zu %%zu\\n", sizeof(%s), offsetof(%s, flags));\n' % (s, s) for s in structs) + "  return 0;\n}\n")
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.check_call([compiler, std, "-Wall", "-Wextra", "-pedantic", "-Werror", "-I", include, str(src), "-o", str(tmp_path / "t")])
+    got = [int(x) for x in subprocess.check_output([str(tmp_path / "t")]).split()]
+    assert got == [v for s in structs for v in (ctypes.sizeof(getattr(B, s)), getattr(B, s).flags.offset)]
 
 
 def kernel_of(M, N, K, cus=256):
