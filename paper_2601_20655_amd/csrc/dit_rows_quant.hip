@@ -7,11 +7,11 @@
 // q = rint(t * (127 * (1 / max|t|))), t = h * gamma, and appears in the scale alone: the integers do not wait for the sum.
 //
 // What bounds it: memory.  32,760 x 5,120, new rows at every call: norm with 16-bit residual 194 us (6.0 TB/s of reads and
-// writes), with a 32-bit one 332 (5.6), without 104 (4.8), 16-bit rows to 8 bits 82 (6.1), back to 16 bits 82 (6.1) and 32 bits
-// 128 (6.6); GELU, 32,760 x 20,480, 355 (5.7).  (Copying 2 GiB by torch: 4.9 TB/s.)  One row: 3.7 us, launch included.
+// writes), with a 32-bit one 332 (5.6), without 107 (4.7; 85 without weights, which come from the second-level cache twice as
+// wide as the row), 16-bit rows to 8 bits 83 (6.1), back to 16 bits 81 (6.2) and 32 bits 128 (6.5); GELU, 32,760 x 20,480, 335
+// to 359 (5.6 to 6.0; there the vector ALU is busy in 97 % of the clocks).  (A copy of 2 GiB: 4.95 TB/s.)  One row: 3.3 us.
 // Tried without gain: workgroups that walk several rows with the weights in registers (norm 201 -> 219 to 249 us; 105 -> 98
-// without a residual), weights asked for ahead of their use (105 -> 121 without a residual: the registers cost a wavefront a
-// SIMD).
+// without a residual), weights asked for ahead of their use with rows past the caches (105 -> 121 without a residual).
 #include <type_traits>
 
 #include "dit_attn_device.h"
