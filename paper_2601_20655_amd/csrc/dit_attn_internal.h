@@ -349,8 +349,8 @@ struct LinearQuantArgs {
     int out_f32;
 };
 hipError_t launch_linear_quant(const LinearQuantArgs& a, hipStream_t s);
-// Which kernel: *features > 0: the few rows' one, so many features a workgroup (past 64 rows in blocks of 32 rows); else the tile
-// as choose_linear_form names it (the host tests read it).
-int choose_linear_quant(int M, int N, int K, int cus, int* features);
+// Which kernel: *rows > 0: the few rows' one, in blocks of so many rows and *features features; else the tile as
+// choose_linear_form names it (the host tests read it).
+int choose_linear_quant(int M, int N, int K, int cus, int* rows, int* features);
 
 }  // namespace dit

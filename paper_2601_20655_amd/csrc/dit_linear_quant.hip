@@ -30,8 +30,14 @@ typedef __attribute__((address_space(3))) void* lptr_t;
 // cut); its NW wavefronts share K in blocks of 128 bytes, one after the other, and add their sums at the end.  A wavefront
 // streams its blocks through S stages of LDS of its own: the load-to-LDS DMA moves 8 rows of a block an instruction, whole
 // lines, and no wavefront waits for another before the end.
-template <int XI, int WI, int NW, int S>
+// Eight wavefronts where a workgroup streams so few bytes that its own trips to memory are what it waits for: 1 x 40 x 16,912
+// 4.9 us and with four 6.6, 113 x 96 x 12,928 5.8 and 6.4; with more features four are level or better (119 x 547 x 16,978
+// in 16-row blocks 12.1 and 13.0).  (3 stages are level with 4 and better than 2 at 16 rows: 16 x 5,120 x 20,480 25 and 26; with
+// more rows 2 leave room for two workgroups.)
+template <int XI, int WI>
 struct FewTile {
+    static constexpr int NW = XI <= 2 && WI == 1 ? 8 : 4;
+    static constexpr int S = XI == 1 || (XI == 2 && WI > 1) ? 3 : 2;
     static constexpr int TB = (XI + 1) / 2, FB = (WI + 1) / 2;  // 16-token and 16-feature blocks
     static constexpr int LOADS = WI + XI;                       // DMA instructions of a block
     static constexpr int STAGE = 2048 * (FB + TB);
@@ -65,16 +71,36 @@ __device__ __forceinline__ void read_fragments(u32x4 (&f)[N], uint32_t at) {
     }
 }
 
-template <int XI, int WI, int NW, int S, bool OUT_F32>
-__global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantArgs a, int F) {
-    using T = FewTile<XI, WI, NW, S>;
-    constexpr int TB = T::TB, FB = T::FB;
+// How the blocks of F features and 8 XI rows lie over the workgroups.  One row block: a feature block each.  Several: each XCD
+// (workgroups go round them one by one) takes `share` neighbours, along the shorter operand first, so that its L2 fetches the
+// longer one once: 799 x 96 x 18,816 in blocks of 16 x 20 11.4 us and 16.0 without, 363 x 275 x 11,204 11.9 and 13.9, 41 x 1,974 x
+// 3,622 5.8 and 7.4.
+struct FewGrid {
+    int F, blocks, share;
+    int along;       // blocks along the shorter operand
+    uint32_t magic;  // 2^20 / along, rounded up: i * magic >> 20 is i / along for numbers below 2^10
+    int rows_longer;
+};
+
+template <int XI, int WI, bool OUT_F32>
+__global__ void __launch_bounds__((64 * FewTile<XI, WI>::NW)) linear_few_kernel(const LinearQuantArgs a, const FewGrid g) {
+    using T = FewTile<XI, WI>;
+    constexpr int TB = T::TB, FB = T::FB, NW = T::NW, S = T::S;
+    const int F = g.F;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 15, lg = lane >> 4;
-    const int n0 = blockIdx.x * F, n1 = n0 + F < a.N ? n0 + F : a.N;  // its features
-    const int m0 = blockIdx.y * (8 * XI), m1 = m0 + 8 * XI < a.M ? m0 + 8 * XI : a.M;  // and token rows
+    int bn = blockIdx.x, bm = 0;
+    if (g.share) {
+        const int i = (blockIdx.x & 7) * g.share + (blockIdx.x >> 3);
+        if (i >= g.blocks) return;
+        const int far = (int)(i * g.magic >> 20), near = i - far * g.along;
+        bm = g.rows_longer ? far : near;
+        bn = g.rows_longer ? near : far;
+    }
+    const int n0 = bn * F, n1 = n0 + F < a.N ? n0 + F : a.N;  // its features
+    const int m0 = bm * (8 * XI), m1 = m0 + 8 * XI < a.M ? m0 + 8 * XI : a.M;  // and token rows
 
     // DMA sources: 8 rows of 128 bytes an instruction.  LDS is filled in lane order, so the bank swizzle (piece p of row r in slot
     // p ^ ((r >> 1) & 7)) is in which piece a lane fetches.  Rows past the end are the last one again (their sums are not
@@ -164,50 +190,64 @@ __global__ void __launch_bounds__(64 * NW) linear_few_kernel(const LinearQuantAr
     }
 }
 
-template <int XI, int WI, int NW, int S, bool OUT_F32>
+template <int XI, int WI, bool OUT_F32>
 hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
-    constexpr int smem = FewTile<XI, WI, NW, S>::LDS;
-    const auto kern = linear_few_kernel<XI, WI, NW, S, OUT_F32>;
+    using T = FewTile<XI, WI>;
+    const auto kern = linear_few_kernel<XI, WI, OUT_F32>;
     static std::atomic<uint64_t> attr_set{0};
-    const hipError_t e = allow_dynamic_lds(kern, smem, attr_set);
+    const hipError_t e = allow_dynamic_lds(kern, T::LDS, attr_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + F - 1) / F), (unsigned)((a.M + 8 * XI - 1) / (8 * XI))), dim3(64 * NW), smem, s,
-                       a, F);
+    const int row_blocks = (a.M + 8 * XI - 1) / (8 * XI), feature_blocks = (a.N + F - 1) / F;
+    FewGrid g{F, feature_blocks, 0, 1, 0, 0};
+    if (row_blocks > 1) {
+        g.blocks = row_blocks * feature_blocks;
+        if (g.blocks >= 1 << 10) return hipErrorInvalidValue;
+        g.share = (g.blocks + 7) / 8;
+        g.rows_longer = a.M > a.N;
+        g.along = g.rows_longer ? feature_blocks : row_blocks;
+        g.magic = ((1u << 20) + g.along - 1) / g.along;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)(g.share ? 8 * g.share : g.blocks)), dim3(64 * T::NW), T::LDS, s, a, g);
     return hipGetLastError();
 }
 
-template <int XI, int NW, int S>
+template <int XI>
 hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
     switch ((F + 7) / 8) {
-        case 1: return a.out_f32 ? launch_few<XI, 1, NW, S, true>(a, F, s) : launch_few<XI, 1, NW, S, false>(a, F, s);
-        case 2: return a.out_f32 ? launch_few<XI, 2, NW, S, true>(a, F, s) : launch_few<XI, 2, NW, S, false>(a, F, s);
-        case 3: return a.out_f32 ? launch_few<XI, 3, NW, S, true>(a, F, s) : launch_few<XI, 3, NW, S, false>(a, F, s);
-        case 4: return a.out_f32 ? launch_few<XI, 4, NW, S, true>(a, F, s) : launch_few<XI, 4, NW, S, false>(a, F, s);
+        case 1: return a.out_f32 ? launch_few<XI, 1, true>(a, F, s) : launch_few<XI, 1, false>(a, F, s);
+        case 2: return a.out_f32 ? launch_few<XI, 2, true>(a, F, s) : launch_few<XI, 2, false>(a, F, s);
+        case 3: return a.out_f32 ? launch_few<XI, 3, true>(a, F, s) : launch_few<XI, 3, false>(a, F, s);
+        case 4: return a.out_f32 ? launch_few<XI, 4, true>(a, F, s) : launch_few<XI, 4, false>(a, F, s);
     }
     return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-// Few rows: as many workgroups as there are compute units, or twice as many, so that all of them pull the weights in at the same
-// rate, and at most 32 features each.  Past 16 rows, and with more features, the tiles read the token rows fewer times.
-// Measured, us, this kernel and the best tile: 1 x 20,480 x 5,120 (three workgroups a unit) 22 and 26; 1 x 15,360 x 5,120 16 and 18;
-// 16 x 5,120 x 20,480 25 and 41; 32 x 5,120 x 5,120 7.8 and 10.5; 64 x 5,120 x 20,480 39 and 44; but 32 x 15,360 x 5,120 22 and 20,
-// 64 x 15,360 x 5,120 29 and 24.
-// More rows go there too, in blocks of 32 rows x 32 features, where those are no more than the compute units: a long sum is then
-// shared by four wavefronts and streams deeper than in a tile.  300 x 300 x 300 4.1 and 4.7, 298 x 768 x 5,376 7.6 and 11.2,
-// 1,049 x 26 x 9,426 10 and 17, 191 x 640 x 18,048 16 and 27; of 90 drawn sizes none loses more than 4 %.  Past that number the
-// tiles win: 859 x 320 x 2,688 (270 blocks) 9.1 and 7.2, 1,863 x 129 x 3,368 (295) 12.7 and 10.3.
-int choose_linear_quant(int M, int N, int K, int cus, int* features) {
-    const int64_t per = ((int64_t)N + 32 * cus - 1) / (32 * cus);  // workgroups a compute unit
-    *features = 0;
-    if (M <= 16 ? per <= 3 : M <= 64 && per == 1) {
-        const int f = (int)((N + per * cus - 1) / (per * cus));
+// The few rows' kernel: a workgroup a compute unit, of at most 32 features, so that all of them pull in the weights at the
+// same rate; its row block the smallest that leaves so few.  Up to 16 rows two or three workgroups a unit pay too.  Else the
+// tiles, which read the rows fewer times.  Measured, us, this kernel and the best tile: 1 x 20,480 x 5,120 (three workgroups a
+// unit) 22 and 26; 1 x 15,360 x 5,120 16 and 18; 16 x 5,120 x 20,480 25 and 41; 32 x 5,120 x 5,120 7.8 and 10.5; 64 x 5,120 x
+// 20,480 39 and 44; but 32 x 15,360 x 5,120 22 and 20, 64 x 15,360 x 5,120 29 and 24.  Blocks of 16 rows and up to 16 features:
+// 113 x 96 x 12,928 5.8 and 18, 428 x 128 x 3,712 4.6 and 7.0, 33 x 41 x 14,220 5.6 and 22; with more features those of 32 rows
+// are level or better (41 x 1,974 x 3,622 5.5 and 5.3, tile 9.1).  Of 32: 298 x 768 x 5,376 7.6 and 11, 37 x 2,775 x 18,763 18
+// and 31.  Of 64, where K is long enough: 113 x 4,000 x 17,280 22 and 30, 1,281 x 237 x 3,155 9.2 and 9.7, but 782 x 544 x 1,792
+// 6.9 and 6.2, 48 x 5,376 x 2,176 7.3 and 6.5.  Over 250 drawn sizes it takes 0.64 of the tiles' time, at most 1.05 of it.
+int choose_linear_quant(int M, int N, int K, int cus, int* rows, int* features) {
+    *rows = *features = 0;
+    for (int r = M <= 8 ? 8 : 16; r <= 64; r *= 2) {
+        const int row_blocks = (int)(((int64_t)M + r - 1) / r);
+        if (row_blocks > cus || (r == 64 && K < 3000)) continue;
+        const int each = cus / row_blocks, f = (int)(((int64_t)N + each - 1) / each);
+        if (f > (r == 16 && row_blocks > 1 ? 16 : 32)) continue;
+        *rows = r;
         *features = f < 8 ? 8 : f;
         return 0;
     }
-    if (M > 64 && (int64_t)((M + 31) / 32) * ((N + 31) / 32) <= cus) {
-        *features = N < 32 ? (N + 7) / 8 * 8 : 32;
+    const int64_t per = ((int64_t)N + 32 * cus - 1) / (32 * cus);  // workgroups a compute unit
+    if (M <= 16 && per <= 3) {
+        *rows = M <= 8 ? 8 : 16;
+        *features = (int)((N + per * cus - 1) / (per * cus));
         return 0;
     }
     return choose_linear_form_i8(M, N, K, cus);
@@ -217,14 +257,13 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     int cus = 0;
     hipError_t e = compute_units(&cus);
     if (e != hipSuccess) return e;
-    int features;
-    const int form = choose_linear_quant(q.M, q.N, q.K, cus, &features);
-    if (features) {
-        // (3 stages are level with 4 and better than 2 at 16 rows: 25 and 26 us; with more rows 2 leave room for two workgroups)
-        if (q.M <= 8) return launch_few<1, 4, 3>(q, features, s);
-        if (q.M <= 16) return launch_few<2, 4, 3>(q, features, s);
-        if (q.M <= 32 || q.M > 64) return launch_few<4, 4, 2>(q, features, s);
-        return launch_few<8, 4, 2>(q, features, s);
+    int rows, features;
+    const int form = choose_linear_quant(q.M, q.N, q.K, cus, &rows, &features);
+    switch (rows) {
+        case 8: return launch_few<1>(q, features, s);
+        case 16: return launch_few<2>(q, features, s);
+        case 32: return launch_few<4>(q, features, s);
+        case 64: return launch_few<8>(q, features, s);
     }
     LinearArgs a{};
     a.x = reinterpret_cast<const uint16_t*>(q.x);

@@ -64,20 +64,21 @@ def check_linear(y, xq, xs, wq, ws, bias, bf16_out, what=""):
 
 
 # Every kernel of the projection, with at least twice as many blocks of K as a ring of LDS stages holds: few rows (groups of 8
-# rows / groups of 8 features of a workgroup), that kernel in blocks of 32 rows (/ groups of 8 features), the small tiles (10 x
-# 32-row blocks + 64-feature blocks; "any": N cut, or K), tiles of 192 ("64") and 256 ("big") rows x 256 features ("tail": K
-# cut; "rest": the last N % 8 features in a call of their own).
+# rows / groups of 8 features of a workgroup), that kernel with several row blocks ("blocks"), the small tiles (10 x 32-row blocks
+# + 64-feature blocks; "any": N cut, or K), tiles of 192 ("64") and 256 ("big") rows x 256 features ("tail": K cut; "rest":
+# the last N % 8 features in a call of their own).
 KERNELS = [
-    ("few1/1", 3, 173, 1959), ("few1/2", 2, 3116, 2259), ("few1/3", 7, 4146, 1738), ("few1/4", 4, 7456, 1920),
-    ("few2/1", 14, 605, 2141), ("few2/2", 14, 2376, 1664), ("few2/3", 12, 8960, 1920), ("few2/4", 13, 7840, 2432),
-    ("few4/1", 28, 8, 2432), ("few4/2", 30, 3234, 1729), ("few4/3", 21, 4368, 2304), ("few4/4", 17, 7752, 1664),
-    ("few8/1", 47, 48, 1664), ("few8/2", 52, 2396, 1860), ("few8/3", 33, 4169, 2196), ("few8/4", 33, 6220, 1706),
-    ("blocks/1", 634, 8, 2176), ("blocks/2", 1957, 16, 2048), ("blocks/3", 1149, 24, 1795),
-    ("blocks/4", 95, 432, 1792), ("11", 19, 8360, 1920), ("11 any", 18, 8839, 1919), ("21", 34, 8512, 1664),
-    ("21 any", 4332, 66, 1675), ("22", 5738, 136, 1664), ("22 any", 5445, 143, 1687), ("42", 5785, 296, 1664),
-    ("42 any", 5782, 261, 1708), ("34", 544, 6536, 1664), ("34 any", 513, 6555, 1801), ("44", 581, 9344, 1536),
-    ("44 any", 4055, 1300, 1732), ("54", 5409, 1296, 1664), ("54 any", 1051, 7375, 2048), ("64", 5742, 1304, 1792),
-    ("64 tail", 5433, 1352, 1845), ("64 rest", 3654, 2301, 1792), ("64 tail rest", 5405, 1313, 1686),
-    ("big", 2819, 4360, 1536), ("big tail", 1231, 9376, 1800), ("big rest", 1383, 8357, 1664),
-    ("big tail rest", 1177, 9455, 1694),
+    ("few1/1", 3, 173, 6423), ("few1/2", 6, 2873, 3146), ("few1/3", 7, 4146, 2067), ("few1/4", 5, 7952, 1664),
+    ("few2/1", 14, 605, 6528), ("few2/2", 15, 3164, 2124), ("few2/3", 10, 4512, 3456), ("few2/4", 11, 7456, 2304),
+    ("few4/2", 23, 3384, 2192), ("few4/3", 21, 4369, 3247), ("few4/4", 18, 7699, 2207), ("few8/3", 34, 4312, 3164),
+    ("few8/4", 34, 6252, 3013), ("blocks2/1", 54, 350, 6401), ("blocks2/2", 30, 1395, 3534),
+    ("blocks4/1", 4361, 8, 2304), ("blocks4/2", 2602, 31, 3029), ("blocks4/3", 7007, 19, 2258),
+    ("blocks4/4", 5478, 31, 1787), ("blocks8/1", 10337, 8, 3200), ("blocks8/2", 8425, 10, 3565),
+    ("blocks8/3", 8267, 17, 3187), ("blocks8/4", 8337, 25, 3069), ("11", 33, 5128, 1792), ("11 any", 36, 4408, 1898),
+    ("21", 10472, 16, 1792), ("21 any", 8227, 19, 1944), ("22", 8498, 72, 1664), ("22 any", 8394, 66, 1706),
+    ("42", 9519, 136, 1792), ("42 any", 9628, 139, 1691), ("34", 11202, 264, 1664), ("34 any", 11084, 281, 1774),
+    ("44", 12301, 264, 1664), ("44 any", 12247, 269, 1791), ("54", 8218, 784, 1664), ("54 any", 1418, 5465, 1792),
+    ("64", 11060, 536, 1792), ("64 tail", 8497, 784, 1708), ("64 rest", 8205, 871, 1792),
+    ("64 tail rest", 10901, 551, 1667), ("big", 12594, 800, 1664), ("big tail", 13681, 808, 1683),
+    ("big rest", 12405, 1101, 1664), ("big tail rest", 12403, 769, 1678),
 ]

@@ -121,16 +121,15 @@ def test_structs_as_c_lays_them_out(compiler, std, tmp_path):
 
 def kernel_of(M, N, K, cus=256):
     """The kernel of a projection as quant_ref.KERNELS names it."""
-    f = B.lib()._ZN3dit19choose_linear_quantEiiiiPi
+    f = B.lib()._ZN3dit19choose_linear_quantEiiiiPiS0_
     f.restype = ctypes.c_int
-    features = ctypes.c_int(-1)
-    form = f(M, N, K, cus, ctypes.byref(features))
-    if features.value:
-        assert form == 0 and 8 <= features.value <= 32
-        if M > 64:
-            return "blocks/%d" % ((features.value + 7) // 8)
-        groups = next(g for g in (1, 2, 4, 8) if M <= 8 * g)
-        return "few%d/%d" % (groups, (features.value + 7) // 8)
+    rows, features = ctypes.c_int(-1), ctypes.c_int(-1)
+    form = f(M, N, K, cus, ctypes.byref(rows), ctypes.byref(features))
+    if rows.value:
+        assert form == 0 and 8 <= features.value <= 32 and rows.value in (8, 16, 32, 64)
+        name = "few%d" if M <= rows.value else "blocks%d"
+        assert M <= rows.value or -(-M // rows.value) * -(-N // features.value) <= cus
+        return (name + "/%d") % (rows.value // 8, (features.value + 7) // 8)
     if form not in (0, 64):
         return "%d%s" % (form, " any" if K % 128 or N % 8 else "")
     return "%s%s%s" % ("64" if form else "big", " tail" if K % 128 else "", " rest" if N % 8 else "")
