@@ -624,9 +624,12 @@ def dit_qkv_proj_forward(x, w, bias, grid, split, H, q_out=None, origin=(0, 0, 0
     return q_out, workspace
 
 
-def _empty_rows(M, N, dtype, device, multiple=16):
-    """An [M, N] tensor whose rows start on multiples of so many bytes."""
-    per = multiple // dtype.itemsize
+def _empty_rows(M, N, dtype, device, lines=False):
+    """An [M, N] tensor whose rows start on multiples of 16 bytes: dense where its rows do by themselves, else (or if asked
+    to) on multiples of 128, so that no two rows share a memory line."""
+    per = 128 // dtype.itemsize
+    if not lines and N * dtype.itemsize % 16 == 0:
+        return torch.empty((M, N), dtype=dtype, device=device)
     return torch.empty((M, (N + per - 1) // per * per), dtype=dtype, device=device)[:, :N]
 
 
@@ -665,7 +668,7 @@ def _quant_outputs(what, x, q, scale):
     ldx = _row_stride(what, "x", x, shape, x.dtype, device)
     if q is None:
         # (lines of 128 bytes to themselves: the projection reads rows of such strides a quarter faster)
-        q = _empty_rows(shape[0], shape[1], torch.int8, x.device, 128)
+        q = _empty_rows(shape[0], shape[1], torch.int8, x.device, True)
     ldq = _row_stride(what, "q", q, shape, torch.int8, device)
     if scale is None:
         scale = torch.empty(shape[0], dtype=torch.float32, device=x.device)

@@ -778,9 +778,16 @@ namespace {
 
 template <bool OUT_F32, bool TAIL>
 hipError_t launch_linear_i8(const LinearArgs& a, int rows, int cus, hipStream_t s) {
-    if (rows == 192) return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false, 6>(a, cus, s);
-    if (exceeds_caches((int64_t)a.M * a.N * (OUT_F32 ? 4 : 2))) return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, true>(a, cus, s);
-    return launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false>(a, cus, s);
+    // (16-bit rows by halves of 128-byte lines: 25,978 x 12,353 x 384 with rows of 64-byte multiples 197 us past the caches and
+    // 221 through them, of 32-byte ones 321 and 239.  32-bit rows always: 27,223 x 16,309 x 1,664 on any rows 760 to 806 past
+    // and 930 to 1,036 through)
+    const int64_t row = a.ldy * (OUT_F32 ? 4 : 2);
+    const bool past = exceeds_caches((int64_t)a.M * a.N * (OUT_F32 ? 4 : 2)) &&
+                      (OUT_F32 || (reinterpret_cast<uintptr_t>(a.y) | (uintptr_t)row) % 64 == 0);
+    if (rows == 192)
+        return past ? launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, true, 6>(a, cus, s)
+                    : launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false, 6>(a, cus, s);
+    return past ? launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, true>(a, cus, s) : launch_linear_inst<OP_I8, OUT_F32, 0, TAIL, false>(a, cus, s);
 }
 
 }  // namespace

@@ -244,3 +244,31 @@ def test_quantised_rows_through_the_projection(M):
     h = (x.double() + r.double()).cpu().numpy()
     ref = (h / np.sqrt((h * h).mean(1, keepdims=True))) @ wf.double().cpu().numpy().T
     assert np.sqrt(np.mean((y.cpu().numpy() - ref) ** 2)) < 2 * 4.5 / 254 / 3 ** 0.5
+
+
+@pytest.mark.parametrize("M,N,K,bf16,ld", [(27500, 5120, 384, True, 5120), (27500, 5120, 384, True, 5128), (27500, 5121, 200, True, None),
+                                           (27500, 5120, 2048, True, 5120), (27500, 5121, 2040, True, None),
+                                           (13800, 5120, 384, False, 5124), (13800, 5121, 200, False, None),
+                                           (27500, 5128, 2000, False, None)])
+def test_output_larger_than_the_caches(M, N, K, bf16, ld):
+    """61 rows over and over: integer sums are exact and the rest is done number by number, so the bits are those of a call on
+    the 61 alone (another kernel)."""
+    import torch
+
+    gen = torch.Generator(device="cuda").manual_seed(N + K)
+    of = torch.arange(M, device="cuda") % 61
+
+    def rows(n):
+        r = torch.empty((n, (K + 15) // 16 * 16), dtype=torch.int8, device="cuda")[:, :K]
+        return r.copy_(torch.randint(-127, 128, (n, K), generator=gen, device="cuda", dtype=torch.int8))
+
+    few, w = rows(61), rows(N)
+    x = torch.empty((M, few.stride(0)), dtype=torch.int8, device="cuda")[:, :K].copy_(few[of])
+    xs, ws = torch.rand(61, generator=gen, device="cuda"), torch.rand(N, generator=gen, device="cuda")
+    bias = torch.randn(N, generator=gen, device="cuda").bfloat16()
+    dt = torch.bfloat16 if bf16 else torch.float32
+    buf = None if ld is None else torch.full((M, ld), 7.0, dtype=dt, device="cuda")
+    y = B.dit_linear_quant_forward(x, xs[of], w, ws, bias, out=None if buf is None else buf[:, :N], out_dtype=dt if buf is None else None)
+    want = B.dit_linear_quant_forward(few, xs, w, ws, bias, out_dtype=dt)
+    assert torch.equal(y, want[of])
+    assert buf is None or torch.all(buf[:, N:] == 7.0)
