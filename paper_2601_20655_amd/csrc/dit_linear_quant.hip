@@ -2,8 +2,8 @@
 // integer on the matrix cores.  Few token rows are done here, straight from memory; more by the tiles of dit_linear.hip and
 // dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
 //
-// What bounds the few rows' kernel: the stream of the weights.  1 x 15,360 x 5,120 12.6 us, 6.2 TB/s; 16 x 5,120 x 20,480
-// 21.9 us, 4.8 TB/s (a copy: 4.95).
+// What bounds the few rows' kernel: the stream of the weights.  1 x 15,360 x 5,120 12.6 to 13.0 us, 6.1 TB/s; 16 x 5,120 x
+// 20,480 21.8 us, 4.8 TB/s (a copy: 4.95).
 #include "dit_attn_device.h"
 #include "dit_attn_internal.h"
 
