@@ -627,8 +627,8 @@ def dit_qkv_proj_forward(x, w, bias, grid, split, H, q_out=None, origin=(0, 0, 0
 def _empty_rows(M, N, dtype, device, lines=False):
     """An [M, N] tensor whose rows start on multiples of 16 bytes: dense where its rows do by themselves, else (or if asked
     to) on multiples of 128, so that no two rows share a memory line."""
-    per = 128 // dtype.itemsize
-    if not lines and N * dtype.itemsize % 16 == 0:
+    per = (128 if lines or N * dtype.itemsize % 16 else 16) // dtype.itemsize
+    if N % per == 0:
         return torch.empty((M, N), dtype=dtype, device=device)
     return torch.empty((M, (N + per - 1) // per * per), dtype=dtype, device=device)[:, :N]
 
@@ -669,10 +669,13 @@ def _quant_outputs(what, x, q, scale):
     if q is None:
         # (lines of 128 bytes to themselves: the projection reads rows of such strides a quarter faster)
         q = _empty_rows(shape[0], shape[1], torch.int8, x.device, True)
-    ldq = _row_stride(what, "q", q, shape, torch.int8, device)
+        ldq = q.stride(0)
+    else:
+        ldq = _row_stride(what, "q", q, shape, torch.int8, device)
     if scale is None:
         scale = torch.empty(shape[0], dtype=torch.float32, device=x.device)
-    _check_vector(what, "scale", scale, shape[0], torch.float32, device)
+    else:
+        _check_vector(what, "scale", scale, shape[0], torch.float32, device)
     return shape, device, code, ldx, q, ldq, scale
 
 
@@ -707,7 +710,9 @@ def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=Non
         ldr = _row_stride(what, "residual", residual, shape, residual.dtype, device)
         if h_out is None:
             h_out = _empty_rows(shape[0], shape[1], residual.dtype, x.device)
-        ldh = _row_stride(what, "h_out", h_out, shape, residual.dtype, device)
+            ldh = h_out.stride(0)
+        else:
+            ldh = _row_stride(what, "h_out", h_out, shape, residual.dtype, device)
     elif h_out is not None:
         raise ValueError("%s: h_out needs a residual" % what)
     p = dit_norm_quant_params(shape[0], shape[1], ldx, ldr, ldh, ldq, eps, code, r_code, 0)
@@ -730,8 +735,10 @@ def dit_dequant_rows_forward(q, scale, out=None, out_dtype=None, stream=None):
     _check_vector(what, "scale", scale, shape[0], torch.float32, device)
     if out is None:
         out = _empty_rows(shape[0], shape[1], out_dtype or torch.bfloat16, q.device)
-    code = _dtype_code(out)
-    p = dit_dequant_rows_params(shape[0], shape[1], ldq, _row_stride(what, "out", out, shape, out.dtype, device), code, 0)
+        ldy = out.stride(0)
+    else:
+        ldy = _row_stride(what, "out", out, shape, out.dtype, device)
+    p = dit_dequant_rows_params(shape[0], shape[1], ldq, ldy, _dtype_code(out), 0)
     st = lib().dit_dequant_rows_forward(q.data_ptr(), scale.data_ptr(), out.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
     if st != DIT_OK:
         raise DitError(st, what)
@@ -764,8 +771,10 @@ def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dt
         _check_vector(what, "bias", bias, N, torch.bfloat16, device)
     if out is None:
         out = _empty_rows(M, N, out_dtype or torch.bfloat16, x.device)
-    code = _dtype_code(out)
-    p = dit_linear_params(M, N, K, ldx, ldw, _row_stride(what, "out", out, (M, N), out.dtype, device), code, 0)
+        ldy = out.stride(0)
+    else:
+        ldy = _row_stride(what, "out", out, (M, N), out.dtype, device)
+    p = dit_linear_params(M, N, K, ldx, ldw, ldy, _dtype_code(out), 0)
     st = lib().dit_linear_quant_forward(x.data_ptr(), x_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(),
                                         bias.data_ptr() if bias is not None else None, out.data_ptr(), ctypes.byref(p),
                                         _stream_ptr(stream))
