@@ -34,7 +34,7 @@
 //
 // The same kernel multiplies 8-bit integers (v_mfma_i32_16x16x64_i8): a step's tiles are as many bytes, for 128
 // contraction indices in place of 64, and everything above holds.  The scales of rows and features are applied on the
-// way out.  32,760 x 15,360 x 5,120: 1,810 to 1,920 us by box, 2,680 to 2,850 TOP/s, the matrix cores busy in 75 to
+// way out.  32,760 x 15,360 x 5,120: 1,810 to 2,000 us by box, 2,570 to 2,850 TOP/s, the matrix cores busy in 75 to
 // 77 % of the clocks of a chip that its power limit holds at 1.6 to 1.75 GHz; a loop of such instructions alone sustains
 // 3,530 on random operands.  192-token tiles (TB 6) take what 256-token ones would fill the last round of workgroups
 // badly with: 7,800 x 4,608 x 1,536 65 -> 58 us, of twelve steps a tile, so that starts and stores show.

@@ -2,8 +2,8 @@
 // integer on the matrix cores.  Few token rows are done here, straight from memory; more by the tiles of dit_linear.hip and
 // dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
 //
-// What bounds the few rows' kernel: the stream of the weights.  1 x 15,360 x 5,120 12.6 to 13.0 us, 6.1 TB/s; 16 x 5,120 x
-// 20,480 21.8 us, 4.8 TB/s (a copy: 4.95).
+// What bounds the few rows' kernel: the stream of the weights.  1 x 15,360 x 5,120 12.6 to 12.9 us, 6.2 TB/s; 16 x 5,120 x
+// 20,480 21.6 us, 4.8 TB/s (a copy: 4.95).
 #include "dit_attn_device.h"
 #include "dit_attn_internal.h"
 
@@ -77,8 +77,9 @@ __device__ __forceinline__ void read_fragments(u32x4 (&f)[N], uint32_t at) {
 // 3,622 5.8 and 7.4.
 struct FewGrid {
     int F, blocks, share;
-    int along;       // blocks along the shorter operand
-    uint32_t magic;  // 2^20 / along, rounded up: i * magic >> 20 is i / along for numbers below 2^10
+    int xcds, shift;  // 7 and 3, or 0 and 0 for one row block
+    int along;        // blocks along the shorter operand
+    uint32_t magic;   // 2^20 / along, rounded up: i * magic >> 20 is i / along for numbers below 2^10; 0 for one row block
     int rows_longer;
 };
 
@@ -91,10 +92,13 @@ __global__ void __launch_bounds__((64 * FewTile<XI, WI>::NW)) linear_few_kernel(
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 15, lg = lane >> 4;
+    // (Without a branch: the arguments behind one would be loaded behind it, 0.2 us.)
     int bn = blockIdx.x, bm = 0;
-    if (g.share) {
-        const int i = (blockIdx.x & 7) * g.share + (blockIdx.x >> 3);
-        if (i >= g.blocks) return;
+    bool surplus = false;
+    if constexpr (XI > 1) {
+        const int own = (blockIdx.x & g.xcds) * g.share + (blockIdx.x >> g.shift);
+        surplus = own >= g.blocks;  // (the last block again, for nobody)
+        const int i = surplus ? g.blocks - 1 : own;
         const int far = (int)(i * g.magic >> 20), near = i - far * g.along;
         bm = g.rows_longer ? far : near;
         bn = g.rows_longer ? near : far;
@@ -176,7 +180,7 @@ __global__ void __launch_bounds__((64 * FewTile<XI, WI>::NW)) linear_few_kernel(
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb) part[((wave * FB + fb) * TB + tb) * 64 + lane] = acc[fb][tb];
     __syncthreads();
-    for (int i = tid; i < 16 * FB * (m1 - m0); i += 64 * NW) {
+    for (int i = tid; i < (surplus ? 0 : 16 * FB * (m1 - m0)); i += 64 * NW) {
         const int r = i / (16 * FB), f = i % (16 * FB), m = m0 + r, n = n0 + f;
         if (n >= n1) continue;
         const int at = (f >> 4) * TB + (r >> 4), l = 16 * ((f & 15) >> 2) + (r & 15);
@@ -198,11 +202,13 @@ hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
     const hipError_t e = allow_dynamic_lds(kern, T::LDS, attr_set);
     if (e != hipSuccess) return e;
     const int row_blocks = (a.M + 8 * XI - 1) / (8 * XI), feature_blocks = (a.N + F - 1) / F;
-    FewGrid g{F, feature_blocks, 0, 1, 0, 0};
+    FewGrid g{F, feature_blocks, 0, 0, 0, 1, 0, 1};
     if (row_blocks > 1) {
         g.blocks = row_blocks * feature_blocks;
         if (g.blocks >= 1 << 10) return hipErrorInvalidValue;
         g.share = (g.blocks + 7) / 8;
+        g.xcds = 7;
+        g.shift = 3;
         g.rows_longer = a.M > a.N;
         g.along = g.rows_longer ? feature_blocks : row_blocks;
         g.magic = ((1u << 20) + g.along - 1) / g.along;
