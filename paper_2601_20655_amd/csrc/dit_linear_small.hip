@@ -11,7 +11,7 @@
 // three stages of so large a tile, and a step has one barrier.  So a small tile costs more per flop than a big one, and
 // is taken only where it fills the chip better (choose_linear_form).  8-bit operands (v_mfma_i32_16x16x64_i8, twice the contraction
 // indices a step) leave half the steps, so starts and stores weigh more: 769 x 2,311 x 1,001 with 32-bit rows, eight
-// steps, 8.8 us where the operations take 1.5 and the bytes 2.1.
+// steps, 8.1 us where the operations take 1.5 and the bytes 2.1.
 #include <type_traits>
 
 #include "dit_attn_device.h"
@@ -114,13 +114,24 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     };
 
     const int nK = a.K / kLinBK;
+    // ANY: what is left of K is one more step.  Of its pieces those past the rows' ends are not read (piece 0 in their place), and
+    // the bytes past K count as zeros of x when it is multiplied.  (Staged through registers behind the whole steps it was
+    // waited for on its own: 769 x 2,311 x 1,001 8.1 -> 7.4 us, 17 x 15,360 x 5,100 18.6 -> 17.4, 544 x 6,536 x 1,700 16.1 -> 15.1.)
+    const int steps = nK + (ANY && a.tail > 0 ? 1 : 0);
+    auto behind = [&](int chunk) __attribute__((always_inline)) {  // how far such a piece lies behind piece 0
+        const int at = 16 * ((lane & 7) ^ ((4 * chunk + (r8 >> 1)) & 7));
+        return at < a.tail ? 0 : at;
+    };
     // S - 1 stages are requested ahead; past the end of K the last step is requested again (into a stage nobody reads
     // any more), so that the number of loads in flight stays the constant the waits count on
     int requested = 0;
     auto request_piece = [&](auto i, int stage) __attribute__((always_inline)) {
         constexpr int I = decltype(i)::value;
         uint8_t* const dst = smem + stage * T::STAGE;
-        src[I] += requested > 0 && requested < nK ? 128 : 0;  // on from the step requested before
+        src[I] += requested > 0 && requested < steps ? 128 : 0;  // on from the step requested before
+        if constexpr (ANY) {
+            if (requested == nK && steps > nK) src[I] -= behind(I < FULL ? wave : wave >> 1);
+        }
         if constexpr (I < FULL) {
             __builtin_amdgcn_global_load_lds((gptr_t)src[I], (lptr_t)(dst + (wave + 8 * I) * 1024), 16, 0, 0);
         } else {
@@ -136,15 +147,13 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     // behind the MFMAs and were waited for there: 641 x 3,320 x 1,664 14.6 -> 12.8 us, 3,600 x 5,120 x 5,120 166 -> 159.)
     constexpr int GAPS = TB > 2 ? TB - 2 : 1, PER = (R + GAPS - 1) / GAPS, LPER = (T::LOADS + GAPS - 1) / GAPS;
     int stage = 0, free_stage = S - 1;
-    if (!ANY || nK > 0) {
 #pragma unroll
-        for (int s = 0; s < S - 1; ++s) {
-            static_for<0, T::LOADS>([&](auto i) __attribute__((always_inline)) { request_piece(i, s); });
-            ++requested;
-        }
-        sync_stage();
-        static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W0, X0, i, 0, 0); });
+    for (int s = 0; s < S - 1; ++s) {
+        static_for<0, T::LOADS>([&](auto i) __attribute__((always_inline)) { request_piece(i, s); });
+        ++requested;
     }
+    sync_stage();
+    static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W0, X0, i, 0, 0); });
     for (int k = 0; k < nK; ++k) {
         const int next = stage + 1 == S ? 0 : stage + 1;
         auto slice = [&](u32x4 (&W)[FB], u32x4 (&X)[TB], u32x4 (&Wn)[FB], u32x4 (&Xn)[TB], int nstage, auto ksn) __attribute__((always_inline)) {
@@ -179,49 +188,29 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
         free_stage = stage;
         stage = next;
     }
+    if constexpr (ANY) {
+        if (steps > nK) {
+            // (its first slice has been read behind the whole steps)
+            auto last = [&](u32x4 (&W)[FB], u32x4 (&X)[TB], int ks) __attribute__((always_inline)) {
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const int bits = 8 * (a.tail - 64 * ks - 16 * lg - 4 * d);  // of this dword, those that count
+                        X[tb][d] = bits <= 0 ? 0u : bits < 32 ? X[tb][d] & ((1u << bits) - 1u) : X[tb][d];
+                    }
+#pragma unroll
+                    for (int fb = 0; fb < FB; ++fb) acc[fb][tb] = LinAcc<OP>::mfma(W[fb], X[tb], acc[fb][tb]);
+                }
+            };
+            static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W1, X1, i, stage, 1); });
+            last(W0, X0, 0);
+            last(W1, X1, 1);
+        }
+    }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    // ---- what is left of K: one more step, staged through registers, the bytes behind the rows' ends zeros
-    if constexpr (ANY) {
-        if (a.tail > 0) {
-            constexpr int PIECES = (T::BN + T::BM) * 8, TURNS = (PIECES + 511) / 512;
-            u32x4 v[TURNS];
-#pragma unroll
-            for (int i = 0; i < TURNS; ++i) {  // (all are asked for before the first is waited for)
-                const int p = tid + 512 * i, line = p >> 3, r = line < T::BN ? line : line - T::BN;
-                const int at = 16 * ((p & 7) ^ ((r >> 1) & 7));
-                const bool is_w = line < T::BN;
-                const int row0 = is_w ? tn * T::BN : tm * T::BM, end = is_w ? a.N : a.M;
-                const int row = row0 + r < end ? row0 + r : end - 1;
-                const uint16_t* const from = (is_w ? a.w + (int64_t)row * a.ldw : a.x + (int64_t)row * a.ldx) + a.K;
-                v[i] = mk4(0u, 0u, 0u, 0u);
-                if (p < PIECES && at < a.tail)
-                    v[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint8_t*>(from) + at);
-            }
-#pragma unroll
-            for (int i = 0; i < TURNS; ++i) {
-                const int p = tid + 512 * i, line = p >> 3, r = line < T::BN ? line : line - T::BN;
-                const int at = 16 * ((p & 7) ^ ((r >> 1) & 7));
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int bits = 8 * (a.tail - at - 4 * d);  // of this dword, those that count
-                    v[i][d] = bits <= 0 ? 0u : bits < 32 ? v[i][d] & ((1u << bits) - 1u) : v[i][d];
-                }
-                if (p < PIECES) *reinterpret_cast<u32x4*>(smem + 16 * p) = v[i];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                static_for<0, R>([&](auto i) __attribute__((always_inline)) { read_fragment(W0, X0, i, 0, ks); });
-#pragma unroll
-                for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                    for (int fb = 0; fb < FB; ++fb) acc[fb][tb] = LinAcc<OP>::mfma(W0[fb], X0[tb], acc[fb][tb]);
-            }
-            __syncthreads();
-        }
-    }
 
     // ---- store: 16 token rows at a time through an area of the wavefront's own, so that rows leave in 16-byte pieces
     // (Tried: non-temporal stores.  769 x 10,240 x 5,120 72.1 -> 70.6 us on the operands of the call before, 89.4 ->
@@ -402,7 +391,7 @@ int choose_linear_form_i8(int M, int N, int K, int cus) {
         // (workgroups in pairs: a first pair on a compute unit takes half of what all pairs add)
         const double step = f.slots == 2 ? left <= cus ? f.light : f.light + (f.full - f.light) * (0.45 + 0.55 * (left - cus) / cus)
                                          : left <= 0.8 * cus ? f.light : 0.5 * (f.light + f.full);
-        const double ends = f.ends + (f.tb < 6 && K % 128 ? 2.0 : 0.0);  // (the rest of K: a step that nothing hides)
+        const double ends = f.ends + (f.tb < 6 && K % 128 ? 0.5 : 0.0);  // (the rest of K: 769 x 2,312 x 1,024 7.1, x 1,001 7.6)
         const double t = f.start + rounds * (f.full * nK + ends) + (left == 0 ? 0.0 : step * nK + ends);
         if (t < best) {
             best = t;
