@@ -363,6 +363,20 @@ __global__ void __launch_bounds__(256) dequant_rows_kernel(const DequantArgs a, 
     }
 }
 
+// A launch has fewer than 2^32 work items: a longer one is not refused, its workgroups are counted modulo that, and rows are
+// left out.  So calls of more rows are several launches, of as many groups of `rows` rows (`threads` work items each) as one takes.
+template <class F>
+hipError_t launch_slices(int M, int rows, int64_t threads, F&& launch) {
+    const int64_t most = 0xffffffff / threads * rows;
+    for (int64_t m = 0; m < M; m += most) {
+        const int some = (int)(M - m < most ? M - m : most);
+        launch(m, some, (unsigned)(((int64_t)some + rows - 1) / rows));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // How rows lie over wavefronts.  Where there are wavefronts enough to keep the memory busy, `most` chunks a lane; where there
 // are not, one, the row over as many wavefronts as it takes (at most 16, a workgroup).  (A wavefront a SIMD is enough: norm of
 // 769 x 5,120 9.3 us if four are asked for, 8.1 with one, 1,560 x 5,120 without a residual 11.2 and 8.5; 1,560 x 5,000 with a
@@ -387,9 +401,16 @@ hipError_t launch_quant(const QuantArgs& a, const RowLayout& l, hipStream_t s) {
     const bool past = SOME_16 && exceeds_caches((int64_t)a.M * a.N * ((X_F32 ? 4 : 2) + (RES == ROW_F32 ? 4 : RES == ROW_BF16 ? 2 : 0)));
     const auto kern = a.N % 8 ? past ? quant_rows_kernel<MODE, X_F32, RES, C, true, SOME_16> : quant_rows_kernel<MODE, X_F32, RES, C, true, false>
                               : past ? quant_rows_kernel<MODE, X_F32, RES, C, false, SOME_16> : quant_rows_kernel<MODE, X_F32, RES, C, false, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)a.M + l.rows - 1) / l.rows)),
-                       dim3(64 * l.waves * l.rows), 0, s, a, l.waves);
-    return hipGetLastError();
+    return launch_slices(a.M, l.rows, 64 * l.waves * l.rows, [&](int64_t m, int rows, unsigned groups) {
+        QuantArgs b = a;
+        b.x = static_cast<const uint8_t*>(a.x) + m * a.ldx * (X_F32 ? 4 : 2);
+        if (a.residual) b.residual = static_cast<const uint8_t*>(a.residual) + m * a.ldr * (RES == ROW_F32 ? 4 : 2);
+        if (a.h_out) b.h_out = static_cast<uint8_t*>(a.h_out) + m * a.ldh * (RES == ROW_F32 ? 4 : 2);
+        b.q = a.q + m * a.ldq;
+        b.scale = a.scale + m;
+        b.M = rows;
+        hipLaunchKernelGGL(kern, dim3(groups), dim3(64 * l.waves * l.rows), 0, s, b, l.waves);
+    });
 }
 
 template <int MODE, bool X_F32, int RES>
@@ -415,13 +436,18 @@ template <bool OUT_F32, int C>
 hipError_t launch_dequant(const DequantArgs& a, int need, hipStream_t s) {
     constexpr int V = OUT_F32 ? 4 : 8;
     const int parts = (need + C - 1) / C;
-    const int64_t groups = ((int64_t)a.M * parts + 3) / 4;
-    if (groups > 0x7fffffff) return hipErrorInvalidValue;
     const bool past = exceeds_caches((int64_t)a.M * a.N * (OUT_F32 ? 4 : 2));
     const auto kern = a.N % V ? past ? dequant_rows_kernel<OUT_F32, C, true, true> : dequant_rows_kernel<OUT_F32, C, true, false>
                               : past ? dequant_rows_kernel<OUT_F32, C, false, true> : dequant_rows_kernel<OUT_F32, C, false, false>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(256), 0, s, a, parts);
-    return hipGetLastError();
+    // (four wavefronts a workgroup; four rows, so that any number of parts makes whole workgroups)
+    return launch_slices(a.M, 4, 256 * parts, [&](int64_t m, int rows, unsigned) {
+        DequantArgs b = a;
+        b.q = a.q + m * a.ldq;
+        b.scale = a.scale + m;
+        b.y = static_cast<uint8_t*>(a.y) + m * a.ldy * (OUT_F32 ? 4 : 2);
+        b.M = rows;
+        hipLaunchKernelGGL(kern, dim3((unsigned)(((int64_t)rows * parts + 3) / 4)), dim3(256), 0, s, b, parts);
+    });
 }
 
 template <bool OUT_F32>
