@@ -259,10 +259,7 @@ int choose_linear_quant(int M, int N, int K, int cus, int* rows, int* features) 
     return choose_linear_form_i8(M, N, K, cus);
 }
 
-hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
-    int cus = 0;
-    hipError_t e = compute_units(&cus);
-    if (e != hipSuccess) return e;
+static hipError_t launch_slice(const LinearQuantArgs& q, int cus, hipStream_t s) {
     int rows, features;
     const int form = choose_linear_quant(q.M, q.N, q.K, cus, &rows, &features);
     switch (rows) {
@@ -290,7 +287,7 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     // 256 x 256 tiles store whole 16-byte pieces: the last N % 8 features are a call of their own
     const int rest = a.N % 8;
     a.N -= rest;
-    e = launch_linear_i8(a, form == 64 ? 192 : 256, s);
+    const hipError_t e = launch_linear_i8(a, form == 64 ? 192 : 256, s);
     if (e != hipSuccess || rest == 0) return e;
     a.w += (int64_t)a.N * a.ldw;
     a.w_scale += a.N;
@@ -298,6 +295,29 @@ hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
     a.y = static_cast<uint8_t*>(a.y) + (int64_t)a.N * (a.out_f32 ? 4 : 2);
     a.N = rest;
     return launch_linear_small_i8(a, choose_linear_form_i8(a.M, a.N, q.K, cus), s);
+}
+
+// In slices of 2^30 rows and features: the kernels count both in 32 bits, to the ends of their tiles, and the narrowest outputs
+// (under 8 features, 160 rows a tile) have no more tiles than a launch takes.
+hipError_t launch_linear_quant(const LinearQuantArgs& q, hipStream_t s) {
+    constexpr int kSlice = 1 << 30;
+    int cus = 0;
+    hipError_t e = compute_units(&cus);
+    for (int64_t m = 0; m < q.M && e == hipSuccess; m += kSlice) {
+        for (int64_t n = 0; n < q.N && e == hipSuccess; n += kSlice) {
+            LinearQuantArgs a = q;
+            a.x += m * q.ldx;
+            a.x_scale += m;
+            a.w += n * q.ldw;
+            a.w_scale += n;
+            if (a.bias) a.bias += n;
+            a.y = static_cast<uint8_t*>(a.y) + (m * q.ldy + n) * (q.out_f32 ? 4 : 2);
+            a.M = (int)(q.M - m < kSlice ? q.M - m : kSlice);
+            a.N = (int)(q.N - n < kSlice ? q.N - n : kSlice);
+            e = launch_slice(a, cus, s);
+        }
+    }
+    return e;
 }
 
 }  // namespace dit

@@ -292,6 +292,10 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     }
 }
 
+// A launch has fewer than 2^32 work items (a larger one is not refused: its workgroups are counted modulo that): outputs of
+// more tiles go to larger ones, and to the big kernel, whose workgroups walk over theirs.
+constexpr int64_t kMostTiles = 0xffffffff / 512;
+
 template <int OP, int TB, int FB, bool OUT_F32, bool ANY>
 hipError_t launch_tile(LinearArgs a, hipStream_t s) {
     using T = LinTile<TB, FB>;
@@ -302,7 +306,7 @@ hipError_t launch_tile(LinearArgs a, hipStream_t s) {
     if (e != hipSuccess) return e;
     a.nTM = (a.M + T::BM - 1) / T::BM;
     a.nTN = (a.N + T::BN - 1) / T::BN;
-    if ((int64_t)a.nTM * a.nTN > 0x7fffffff) return hipErrorInvalidValue;
+    if ((int64_t)a.nTM * a.nTN > kMostTiles) return hipErrorInvalidValue;
     hipLaunchKernelGGL(kern, dim3((unsigned)((int64_t)a.nTM * a.nTN)), dim3(512), smem, s, a);
     return hipGetLastError();
 }
@@ -334,6 +338,7 @@ int choose_linear_form(int M, int N, int K, int cus) {
     int form = 0;
     for (const Form& f : kForms) {
         const int64_t tiles = tiles_of(32 * f.tb, 64 * f.fb);
+        if (tiles > kMostTiles) continue;
         const int slots = f.step2 > 0.0 ? 2 * cus : cus;
         const int64_t rounds = tiles / slots, left = tiles % slots;
         const double full_step = f.step2 > 0.0 ? f.step2 : f.step;
@@ -387,6 +392,7 @@ int choose_linear_form_i8(int M, int N, int K, int cus) {
     for (const FormI8& f : kFormsI8) {
         if (f.tb > 5 && N < 8) continue;  // (stored in whole pieces)
         const int64_t tiles = (int64_t)((M + 32 * f.tb - 1) / (32 * f.tb)) * ((N + 64 * f.fb - 1) / (64 * f.fb));
+        if (f.tb < 6 && tiles > kMostTiles) continue;
         const int64_t rounds = tiles / (f.slots * cus), left = tiles % (f.slots * cus);
         // (workgroups in pairs: a first pair on a compute unit takes half of what all pairs add)
         const double step = f.slots == 2 ? left <= cus ? f.light : f.light + (f.full - f.light) * (0.45 + 0.55 * (left - cus) / cus)
