@@ -466,7 +466,11 @@ dit_status dit_quant_rows_forward(const void *x, int8_t *q, float *scale, const 
  *   h_out     [M, N] of r_dtype (ldh); NULL if the sum is not wanted.  Without residual it must be NULL.  It may be the
  *             residual itself, or x, if type and strides are the same too (the sum replaces it); else it may not overlap
  *             either.
- *   q, scale  as above.  A row whose sum of squares overflows fp32 counts as one with an infinity.
+ *   q, scale  as above.  A row whose sum of squares overflows fp32 counts as one with an infinity.  One of zeros is a row
+ *             whose largest |h * gamma| is below 2^-120.  eps may be 0 or any small number: below 2^-100 h is scaled by a
+ *             power of two first, so that no square underflows; the limit of 2^-120 then holds for the scaled numbers, of
+ *             which the largest |h|, or sqrt(eps) where that is larger, is between 1/2 and 2 (rows above that stay as
+ *             they are).
  * No workspace.  Errors: as dit_quant_rows_forward; eps negative or not finite, h_out without residual -> DIT_ERR_INVALID_ARG.
  */
 typedef struct {

@@ -309,6 +309,7 @@ inline bool exceeds_caches(int64_t bytes) { return bytes > (int64_t)256 << 20; }
 // ---- 8-bit rows: N signed 8-bit integers and one fp32 scale a row (dit_rows_quant.hip) ----
 constexpr float kQuantTop = 127.0f;            // the largest magnitude of a row becomes this integer
 constexpr float kQuantZero = 0x1p-120f;        // rows whose largest magnitude is below count as zero (127 / amax stays finite)
+constexpr float kNormSmallEps = 0x1p-100f;     // a smaller eps does not outweigh what small squares lose
 constexpr int kQuantMaxColumns = 65536;
 struct QuantArgs {
     const void* x;         // [M, N] bf16 or fp32

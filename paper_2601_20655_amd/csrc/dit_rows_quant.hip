@@ -6,6 +6,10 @@
 // normalisation's factor 1 / sqrt(mean + eps) is common to the row, so it cancels in the integers
 // q = rint(t * (127 * (1 / max|t|))), t = h * gamma, and appears in the scale alone: the integers do not wait for the sum.
 //
+// Squares below 2^-126 lose digits and below 2^-150 vanish.  An eps of 2^-100 or more outweighs what is lost; with a smaller one (0 is
+// allowed) the row is first scaled by a power of two that brings its largest number, or sqrt(eps), near 1.  It rounds nothing and
+// cancels in the integers and in the scale.
+//
 // What bounds it: memory.  32,760 x 5,120, new rows at every call: norm with 16-bit residual 194 us (6.0 TB/s of reads and
 // writes), with a 32-bit one 332 (5.6), without 107 (4.7; 85 without weights, which come from the second-level cache twice as
 // wide as the row), 16-bit rows to 8 bits 83 (6.1), back to 16 bits 81 (6.2) and 32 bits 128 (6.5); GELU, 32,760 x 20,480, 335
@@ -232,8 +236,33 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
             }
         }
     }
-    float top = 0.f, sum = 0.f;
+    float top = 0.f, sum = 0.f, eps = a.eps;
     if constexpr (MODE == ROW_NORM) {
+        if (eps < kNormSmallEps) {  // (uniform)
+            float big = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) big = fmaxf(big, __builtin_fabsf(t[c][i]));
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
+            if (W > 1) {
+                if (lane == 0) s_top[wave] = big;
+                __syncthreads();
+                for (int w = 0; w < W; ++w) big = fmaxf(big, s_top[sub * W + w]);
+                __syncthreads();  // (s_top is written again below)
+            }
+            // up by 2^k, k >= 0: the larger of the row's largest number and sqrt(eps) to about 1.  (The exponent of 0, of an
+            // infinity and of a NaN reads as 0.)
+            const int of_row = big > 0.f ? __builtin_amdgcn_frexp_expf(big) : -1000;
+            const int of_eps = eps > 0.f ? __builtin_amdgcn_frexp_expf(eps) >> 1 : -1000;
+            const int e = of_row > of_eps ? of_row : of_eps, k = e < 0 ? -e : 0;
+            eps = ldexpf(eps, 2 * k);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[c][i] = ldexpf(t[c][i], k);
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -290,7 +319,7 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
     float factor = 1.0f / kQuantTop;
     if constexpr (MODE == ROW_NORM) {
         good = good && sum < INFINITY;
-        factor = 1.0f / (sqrtf(sum / (float)a.N + a.eps) * kQuantTop);
+        factor = 1.0f / (sqrtf(sum / (float)a.N + eps) * kQuantTop);
     }
     const bool some = good && top >= kQuantZero;
     const float inverse = some ? kQuantTop * (1.0f / top) : 0.f;
