@@ -423,8 +423,8 @@ dit_status dit_qkv_proj_forward(const void *x, const void *w, const void *bias, 
  * A QUANTISED ROW is N signed 8-bit integers q and one fp32 scale, and stands for the numbers q[n] * scale.  The
  * quantisation is symmetric, one scale a row: with amax the largest magnitude of the row's numbers t,
  *     scale = amax / 127,   q[n] = round to nearest even (t[n] * (127 * (1 / amax))),   in [-127, 127],
- * so the largest number is kept, and every other is off by at most half a scale.  All of it is computed in
- * fp32, operation by operation as written.
+ * so the largest number is kept, and every other is off by at most half a scale.  Both are computed from t in
+ * fp32, operation by operation as written: the bits are those of the formula.
  *   - A row whose amax is below 2^-120 (a row of zeros) gets scale 0 and q 0.
  *   - A row with a NaN or an infinity gets scale NaN and q 0: whatever reads the row yields NaN, and no other row is touched.
  * 8-bit rows start on multiples of 16 bytes, like every row; exactly N bytes of a row are written.  Scales are dense:
@@ -434,7 +434,8 @@ dit_status dit_qkv_proj_forward(const void *x, const void *w, const void *bias, 
 /*
  * t = act(x) to 8-bit rows.  x: [M, N] bf16 or fp32, row stride ldx.  q: [M, N] int8, row stride ldq (bytes).
  * scale: [M] fp32.  The weights w [N, K] of a projection are quantised by this call too: a scale for each output channel.
- * act: DIT_ACT_NONE, or DIT_ACT_GELU_TANH: t = x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))), in fp32.
+ * act: DIT_ACT_NONE, or DIT_ACT_GELU_TANH: t = x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))), in fp32 by the chip's exponential
+ * and reciprocal: within 2^-20 |x| of the formula.
  * No workspace.  q may not overlap x.
  * Errors: NULL x/q/scale/p, M or N < 1, a stride shorter than its row, a bad dtype or act, nonzero flags ->
  * DIT_ERR_INVALID_ARG; N above DIT_QUANT_MAX_COLUMNS -> DIT_ERR_UNSUPPORTED; a base pointer or row stride that breaks
@@ -460,6 +461,7 @@ dit_status dit_quant_rows_forward(const void *x, int8_t *q, float *scale, const 
  *     h = x + residual,   y = h * gamma / sqrt(mean over the N columns of h^2 + eps),   q, scale = 8-bit rows of y.
  * The sum h is used unrounded (fp32); h_out gets it rounded once to r_dtype.  Since 1 / sqrt(...) is common to a row, q is
  * computed from h * gamma, and the factor goes into the scale alone: q does not depend on how the squares are summed.
+ * scale = max |h * gamma| / (127 * sqrt(mean + eps)) in fp32; the order of the sum depends on M, N and the types.
  *   x         [M, N] bf16 or fp32 (x_dtype, ldx)
  *   residual  [M, N] of r_dtype (ldr), or NULL: h = x
  *   gamma     [N] fp32, 16-byte aligned, or NULL: all 1

@@ -316,14 +316,14 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
     if (!live) return;
 
     bool good = top < INFINITY;
-    float factor = 1.0f / kQuantTop;
+    float divisor = kQuantTop;  // the scale is top / divisor
     if constexpr (MODE == ROW_NORM) {
         good = good && sum < INFINITY;
-        factor = 1.0f / (sqrtf(sum / (float)a.N + eps) * kQuantTop);
+        divisor *= sqrtf(sum / (float)a.N + eps);
     }
     const bool some = good && top >= kQuantZero;
     const float inverse = some ? kQuantTop * (1.0f / top) : 0.f;
-    if (part == 0 && lane == 0) a.scale[m] = !good ? NAN : some ? top * factor : 0.f;
+    if (part == 0 && lane == 0) a.scale[m] = !good ? NAN : some ? top / divisor : 0.f;
     int8_t* const q = a.q + m * a.ldq;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
