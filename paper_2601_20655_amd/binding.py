@@ -649,6 +649,12 @@ def _row_stride(what, name, t, shape, dtype, device):
     return s[0]
 
 
+def _check_counts(what, *counts):
+    """Rows and columns are 32-bit integers in the library; ctypes would cut larger ones off without a word."""
+    if max(counts) > 0x7fffffff:
+        raise ValueError("%s: more than %d rows or columns" % (what, 0x7fffffff))
+
+
 def _check_vector(what, name, t, n, dtype, device):
     if t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s: %s must be a dense tensor of %d elements" % (what, name, n))
@@ -663,6 +669,7 @@ def _quant_outputs(what, x, q, scale):
     shape = x.shape
     if len(shape) != 2:
         raise ValueError("%s: x must be [M, N]" % what)
+    _check_counts(what, *shape)
     device = x.get_device()
     code = _dtype_code(x)
     ldx = _row_stride(what, "x", x, shape, x.dtype, device)
@@ -731,6 +738,7 @@ def dit_dequant_rows_forward(q, scale, out=None, out_dtype=None, stream=None):
     shape, device = q.shape, q.get_device()
     if len(shape) != 2:
         raise ValueError("%s: q must be [M, N]" % what)
+    _check_counts(what, *shape)
     ldq = _row_stride(what, "q", q, shape, torch.int8, device)
     _check_vector(what, "scale", scale, shape[0], torch.float32, device)
     if out is None:
@@ -760,6 +768,7 @@ def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dt
     if len(xshape) != 2 or len(wshape) != 2 or wshape[1] != xshape[1]:
         raise ValueError("%s: shapes do not fit y[M, N] = x[M, K] w[N, K]^T" % what)
     (M, K), N = xshape, wshape[0]
+    _check_counts(what, M, N, K)
     ldx = _row_stride(what, "x", x, xshape, torch.int8, device)
     ldw = _row_stride(what, "w", w, wshape, torch.int8, device)
     if K % 16 and M and N:
