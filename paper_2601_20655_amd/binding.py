@@ -703,10 +703,11 @@ def dit_quant_rows_forward(x, act="none", q=None, scale=None, stream=None):
     return q, scale
 
 
-def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=None, q=None, scale=None, stream=None):
+def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=None, q=None, scale=None, stream=None, want_h=True):
     """h = x + residual, y = h * gamma / sqrt(mean(h^2) + eps) and y's 8-bit rows: x [M, N] bf16 or float32, gamma [N]
     float32 or None, residual [M, N] bf16 or float32 or None.  Returns (q, scale), and with a residual (q, scale, h): h in
-    residual's type, in h_out if given (residual itself: the sum replaces it)."""
+    residual's type, in h_out if given (residual itself: the sum replaces it).  want_h=False: the sum is not written, and
+    (q, scale) returned with a residual too."""
     what = "dit_rms_norm_quant_forward"
     shape, device, code, ldx, q, ldq, scale = _quant_outputs(what, x, q, scale)
     if gamma is not None:
@@ -715,7 +716,10 @@ def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=Non
     if residual is not None:
         r_code = _dtype_code(residual)
         ldr = _row_stride(what, "residual", residual, shape, residual.dtype, device)
-        if h_out is None:
+        if not want_h:
+            if h_out is not None:
+                raise ValueError("%s: h_out is given, and want_h is False" % what)
+        elif h_out is None:
             h_out = _empty_rows(shape[0], shape[1], residual.dtype, x.device)
             ldh = h_out.stride(0)
         else:
@@ -729,7 +733,7 @@ def dit_rms_norm_quant_forward(x, gamma=None, eps=1e-6, residual=None, h_out=Non
                                           scale.data_ptr(), ctypes.byref(p), _stream_ptr(stream))
     if st != DIT_OK:
         raise DitError(st, what)
-    return (q, scale) if residual is None else (q, scale, h_out)
+    return (q, scale) if h_out is None else (q, scale, h_out)
 
 
 def dit_dequant_rows_forward(q, scale, out=None, out_dtype=None, stream=None):
