@@ -278,7 +278,7 @@ struct LinearArgs {
     // sums are integers, and y = sum * x_scale * w_scale + bias
     const float* x_scale;  // [M]
     const float* w_scale;  // [N]
-    int tail;              // 8-bit integers of a row behind the whole steps, 0 .. 127 (tiles of dit_linear_small.hip only)
+    int tail;              // 8-bit integers of a row behind the whole steps, 0 .. 127
 };
 hipError_t launch_linear(const LinearArgs& a, hipStream_t s);
 hipError_t launch_linear_i8(LinearArgs a, int rows, hipStream_t s);  // tiles of 256 or 192 rows x 256 features, 8-bit operands

@@ -1,9 +1,10 @@
 // Projection of 8-bit rows: y[m, n] = (sum_k x[m, k] w[n, k]) * x_scale[m] * w_scale[n] + bias[n], the sum an exact 32-bit
-// integer on the matrix cores.  Few token rows are done here, straight from memory; more by the tiles of dit_linear.hip and
-// dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
+// integer on the matrix cores.  Few token rows are done here, through LDS rings of each wavefront's own; more by the tiles of
+// dit_linear.hip and dit_linear_small.hip, which take 8-bit operands at twice the contraction indices a step.
 //
-// What bounds the few rows' kernel: the stream of the weights.  1 x 15,360 x 5,120 12.6 to 12.9 us, 6.2 TB/s; 16 x 5,120 x
-// 20,480 21.6 us, 4.8 TB/s (a copy: 4.95).
+// What bounds the few rows' kernel: the stream of the weights.  From memory (as where a model's layers follow each other)
+// 1 x 15,360 x 5,120 15 to 16.3 us, 4.8 to 5.2 TB/s, 16 x 5,120 x 20,480 25 us, 4.2 TB/s (a copy: 4.95); weights that the 256 MB
+// cache still holds 12.6 to 13.2 us and 17.7 to 22.
 #include "dit_attn_device.h"
 #include "dit_attn_internal.h"
 
@@ -232,13 +233,15 @@ hipError_t launch_few(const LinearQuantArgs& a, int F, hipStream_t s) {
 
 // The few rows' kernel: a workgroup a compute unit, of at most 32 features, so that all of them pull in the weights at the
 // same rate; its row block the smallest that leaves so few.  Up to 16 rows two or three workgroups a unit pay too.  Else the
-// tiles, which read the rows fewer times.  Measured, us, this kernel and the best tile: 1 x 20,480 x 5,120 (three workgroups a
+// tiles, which read the rows fewer times.  Measured, us, operands that change from call to call and come from memory, this
+// kernel and the best tile: 1 x 20,480 x 5,120 (three workgroups a
 // unit) 22 and 26; 1 x 15,360 x 5,120 16 and 18; 16 x 5,120 x 20,480 25 and 41; 32 x 5,120 x 5,120 7.8 and 10.5; 64 x 5,120 x
 // 20,480 39 and 44; but 32 x 15,360 x 5,120 22 and 20, 64 x 15,360 x 5,120 29 and 24.  Blocks of 16 rows and up to 16 features:
 // 113 x 96 x 12,928 5.8 and 18, 428 x 128 x 3,712 4.6 and 7.0, 33 x 41 x 14,220 5.6 and 22; with more features those of 32 rows
 // are level or better (41 x 1,974 x 3,622 5.5 and 5.3, tile 9.1).  Of 32: 298 x 768 x 5,376 7.6 and 11, 37 x 2,775 x 18,763 18
 // and 31.  Of 64, where K is long enough: 113 x 4,000 x 17,280 22 and 30, 1,281 x 237 x 3,155 9.2 and 9.7, but 782 x 544 x 1,792
-// 6.9 and 6.2, 48 x 5,376 x 2,176 7.3 and 6.5.  Over 250 drawn sizes it takes 0.64 of the tiles' time, at most 1.05 of it.
+// 6.9 and 6.2, 48 x 5,376 x 2,176 7.3 and 6.5.  Over 250 drawn sizes that it is chosen for (M 1 .. 2,900, N 16 .. 8,192, K 512 ..
+// 20,000) it takes 0.46 of the tiles' time in the geometric mean, 0.15 at best and 1.00 at worst.
 int choose_linear_quant(int M, int N, int K, int cus, int* rows, int* features) {
     *rows = *features = 0;
     for (int r = M <= 8 ? 8 : 16; r <= 64; r *= 2) {

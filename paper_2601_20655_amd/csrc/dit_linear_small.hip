@@ -11,7 +11,9 @@
 // three stages of so large a tile, and a step has one barrier.  So a small tile costs more per flop than a big one, and
 // is taken only where it fills the chip better (choose_linear_form).  8-bit operands (v_mfma_i32_16x16x64_i8, twice the contraction
 // indices a step) leave half the steps, so starts and stores weigh more: 769 x 2,311 x 1,001 with 32-bit rows, eight
-// steps, 8.1 us where the operations take 1.5 and the bytes 2.1.
+// steps, 7.9 us on the same operands and 9.1 on new ones, where the operations take 1.0 and the bytes 1.3.  Behind the last
+// product bias and scales are asked for and waited for one after the other, and the next rows' scales behind the stores of the
+// rows before: known leads, not taken.
 #include <type_traits>
 
 #include "dit_attn_device.h"
@@ -116,7 +118,8 @@ __global__ void __launch_bounds__(512, (LinTile<TB, FB>::PAIR ? 4 : 2)) linear_t
     const int nK = a.K / kLinBK;
     // ANY: what is left of K is one more step.  Of its pieces those past the rows' ends are not read (piece 0 in their place), and
     // the bytes past K count as zeros of x when it is multiplied.  (Staged through registers behind the whole steps it was
-    // waited for on its own: 769 x 2,311 x 1,001 8.1 -> 7.4 us, 17 x 15,360 x 5,100 18.6 -> 17.4, 544 x 6,536 x 1,700 16.1 -> 15.1.)
+    // waited for on its own: 769 x 2,311 x 1,001 with 16-bit rows 8.1 -> 7.4 us, 17 x 15,360 x 5,100 18.6 -> 17.4, 544 x 6,536 x
+    // 1,700 16.1 -> 15.1, on the same operands.)
     const int steps = nK + (ANY && a.tail > 0 ? 1 : 0);
     auto behind = [&](int chunk) __attribute__((always_inline)) {  // how far such a piece lies behind piece 0
         const int at = 16 * ((lane & 7) ^ ((4 * chunk + (r8 >> 1)) & 7));
@@ -383,6 +386,8 @@ constexpr FormI8 kFormsI8[] = {{1, 1, 2, 0.16, 0.31, 2.5, 3.0}, {2, 1, 2, 0.16, 
 
 }  // namespace
 
+// (The second launch that N % 8 features cost behind tiles of 192 and 256 rows is not in the estimate: 8,654 x 1,781 x 34 goes to
+// those and takes 18.7 us on the same operands, 8,654 x 1,784 x 34 13.8.)
 // Measured, us, 256, 192 and the best of fewer rows: 7,800 x 4,608 x 1,536 65, 58 and 77; 14,040 x 1,536 x 1,536 43, 38 and 47;
 // 3,600 x 5,120 x 5,120 108, 89 and 91; 14,040 x 4,608 x 1,536 98, 110 and 127; 32,760 x 5,120 x 5,120 636, 680 and 793.
 int choose_linear_form_i8(int M, int N, int K, int cus) {
@@ -397,7 +402,7 @@ int choose_linear_form_i8(int M, int N, int K, int cus) {
         // (workgroups in pairs: a first pair on a compute unit takes half of what all pairs add)
         const double step = f.slots == 2 ? left <= cus ? f.light : f.light + (f.full - f.light) * (0.45 + 0.55 * (left - cus) / cus)
                                          : left <= 0.8 * cus ? f.light : 0.5 * (f.light + f.full);
-        const double ends = f.ends + (f.tb < 6 && K % 128 ? 0.5 : 0.0);  // (the rest of K: 769 x 2,312 x 1,024 7.1, x 1,001 7.6)
+        const double ends = f.ends + (f.tb < 6 && K % 128 ? 0.5 : 0.0);  // (the rest of K: 769 x 2,312 x 1,024 6.0, x 1,001 7.6)
         const double t = f.start + rounds * (f.full * nK + ends) + (left == 0 ? 0.0 : step * nK + ends);
         if (t < best) {
             best = t;

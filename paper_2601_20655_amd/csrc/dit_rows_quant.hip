@@ -14,6 +14,9 @@
 // writes), with a 32-bit one 332 (5.6), without 107 (4.7; 85 without weights, which come from the second-level cache twice as
 // wide as the row), 16-bit rows to 8 bits 83 (6.1), back to 16 bits 81 (6.2) and 32 bits 128 (6.5); GELU, 32,760 x 20,480, 335
 // to 359 (5.6 to 6.0; there the vector ALU is busy in 97 % of the clocks).  (A copy of 2 GiB: 4.95 TB/s.)  One row: 3.3 us.
+// The norm of rows beyond 49,152 columns takes seven or eight chunks a lane, which spill 12 to 120 bytes a lane: 2,048 x 65,536
+// with a 16-bit residual 203 us (4.6 TB/s), 2,048 x 40,960 102 (5.7).  Rows of 65,536 to 8 bits, no spill: 80 us, 32-bit ones 131
+// (5.0 to 5.1).
 // Tried without gain: workgroups that walk several rows with the weights in registers (norm 201 -> 219 to 249 us; 105 -> 98
 // without a residual), weights asked for ahead of their use with rows past the caches (105 -> 121 without a residual).
 #include <type_traits>
@@ -123,11 +126,11 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
 
     // Chunk c of lane l is chunk (c W + part) 64 + l of the row.  Whole chunks are loaded without a branch: behind the last
     // one it is loaded again, and counts as zeros.  (One chunk a lane: there may be no whole one.)  A last chunk that N cuts
-    // is loaded number by number, by its one lane.
+    // is loaded number by number, by its one lane, ahead of the row: widening waits for it inside its branch, so that the wavefront
+    // that has it asks for the row behind that.  (Behind the row, the whole chunks were waited for first: 7,800 x 1,537 with a
+    // 16-bit residual 19.0 us, 17.2 this way.)
     const int whole = a.N >> 3, rest = CUT ? a.N & 7 : 0;
     const int first = part * 64 + lane, step = W * 64;
-    // (asked for ahead of everything: 7,800 x 1,537 with a 16-bit residual 19.0 us if the whole chunks are waited for first, 17.2
-    // this way)
     float end_x[7] = {}, end_r[7] = {}, end_g[7] = {};
     if (CUT && (whole & 63) == lane && (whole >> 6) % W == part) {
 #pragma unroll
@@ -144,7 +147,8 @@ __global__ void __launch_bounds__(1024) quant_rows_kernel(const QuantArgs a, int
     // Weights are asked for with the row, where they and it take no more than 60 registers (and the rows are not past the caches:
     // norm of 32,760 x 5,120 with a 16-bit residual 193 us behind the row, 201 with it).  With them, and behind: 7,800 x 5,120
     // without a residual 26 and 31, 7,800 x 1,536 9.0 and 10.1, with a 16-bit one 15.0 and 16.3, with a 32-bit one 26.6 and 28.5;
-    // but 3,600 x 5,120 with a 32-bit one, of more registers, 66 and 43.
+    // but 3,600 x 5,120 with a 32-bit one, of more registers, 66 and 43.  (Behind the row they come chunk by chunk, each waited for,
+    // and the first wait is for the stores of h too: a known lead, not taken.)
     constexpr bool AHEAD = MODE == ROW_NORM && !PAST && C > 1 &&
                            C * (8 + (X_F32 ? 8 : 4) + (RES == ROW_NONE ? 0 : R_F32 ? 8 : 4)) + (CUT ? 21 : 0) <= 60;
     [[maybe_unused]] Chunk<true> kg[C];

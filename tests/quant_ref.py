@@ -50,8 +50,8 @@ def half_ulp_bf16(x):
 
 
 def check_linear(y, xq, xs, wq, ws, bias, bf16_out, what=""):
-    """The sum of products is an integer below 2^53: exact in float64, whatever the order.  fp32 rounds it once, the product
-    of the scales once, their product once and the sum with the bias once."""
+    """The sum of products is an integer below 2^53: exact in float64, whatever the order.  fp32 rounds it once, its product
+    with the token's scale once, and that times the channel's scale plus the bias once: three of the four units."""
     acc = xq.astype(np.float64) @ wq.astype(np.float64).T
     part = acc * (xs.astype(np.float64)[:, None] * ws.astype(np.float64)[None, :])
     ref = part if bias is None else part + bias.astype(np.float64)[None, :]
