@@ -77,6 +77,21 @@ hipError_t launch_row_stats(const TableArgs* t, const RstdArgs* q, const RstdArg
     const int64_t tb = ((int64_t)ta.total + 255) / 256;
     const int64_t qb = ((int64_t)qa.B * qa.L + 3) / 4, kb = ((int64_t)ka.B * ka.L + 3) / 4;
     if (tb + qb + kb == 0) return hipSuccess;
+    if ((tb + qb + kb) * 256 > 0xffffffff) {
+        // A launch has fewer than 2^32 work items (a larger one is not refused: its workgroups are counted modulo that).  The
+        // table in one of its own, then a batch entry each, of at most 2^24 rows.
+        hipError_t e = launch_row_stats(t, nullptr, nullptr, s);
+        for (const RstdArgs* of : {q, k}) {
+            for (int b = 0; of && b < of->B && e == hipSuccess; ++b) {
+                RstdArgs one = *of;
+                one.x = static_cast<const uint8_t*>(of->x) + b * of->s_b * (of->in_f32 ? 4 : 2);
+                one.rstd = of->rstd + (int64_t)b * of->L;
+                one.B = 1;
+                e = launch_row_stats(nullptr, &one, nullptr, s);
+            }
+        }
+        return e;
+    }
     hipLaunchKernelGGL(row_stats_kernel, dim3((unsigned)(tb + qb + kb)), dim3(256), 0, s, ta, qa, ka, (int)tb, (int)qb);
     return hipGetLastError();
 }
