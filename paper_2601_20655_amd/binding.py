@@ -649,10 +649,12 @@ def _row_stride(what, name, t, shape, dtype, device):
     return s[0]
 
 
-def _check_counts(what, *counts):
-    """Rows and columns are 32-bit integers in the library; ctypes would cut larger ones off without a word."""
-    if max(counts) > 0x7fffffff:
-        raise ValueError("%s: more than %d rows or columns" % (what, 0x7fffffff))
+# Rows and columns are 32-bit integers in the library; ctypes would cut larger ones off without a word.
+_MOST_COUNT = 0x7fffffff
+
+
+def _too_many(what):
+    raise ValueError("%s: more than %d rows or columns" % (what, _MOST_COUNT))
 
 
 def _check_vector(what, name, t, n, dtype, device):
@@ -669,7 +671,8 @@ def _quant_outputs(what, x, q, scale):
     shape = x.shape
     if len(shape) != 2:
         raise ValueError("%s: x must be [M, N]" % what)
-    _check_counts(what, *shape)
+    if shape[0] > _MOST_COUNT or shape[1] > _MOST_COUNT:
+        _too_many(what)
     device = x.get_device()
     code = _dtype_code(x)
     ldx = _row_stride(what, "x", x, shape, x.dtype, device)
@@ -742,7 +745,8 @@ def dit_dequant_rows_forward(q, scale, out=None, out_dtype=None, stream=None):
     shape, device = q.shape, q.get_device()
     if len(shape) != 2:
         raise ValueError("%s: q must be [M, N]" % what)
-    _check_counts(what, *shape)
+    if shape[0] > _MOST_COUNT or shape[1] > _MOST_COUNT:
+        _too_many(what)
     ldq = _row_stride(what, "q", q, shape, torch.int8, device)
     _check_vector(what, "scale", scale, shape[0], torch.float32, device)
     if out is None:
@@ -772,7 +776,8 @@ def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dt
     if len(xshape) != 2 or len(wshape) != 2 or wshape[1] != xshape[1]:
         raise ValueError("%s: shapes do not fit y[M, N] = x[M, K] w[N, K]^T" % what)
     (M, K), N = xshape, wshape[0]
-    _check_counts(what, M, N, K)
+    if M > _MOST_COUNT or N > _MOST_COUNT or K > _MOST_COUNT:
+        _too_many(what)
     ldx = _row_stride(what, "x", x, xshape, torch.int8, device)
     ldw = _row_stride(what, "w", w, wshape, torch.int8, device)
     if K % 16 and M and N:
