@@ -58,7 +58,8 @@ typedef enum {
     DIT_ERR_HIP = -5          /* a HIP runtime call failed; see dit_last_hip_error() */
 } dit_status;
 
-typedef enum { DIT_BF16 = 0, DIT_F32 = 1 } dit_dtype;
+/* DIT_F16: pages of a key/value cache and the rows that come from or go to them (the last section); elsewhere refused. */
+typedef enum { DIT_BF16 = 0, DIT_F32 = 1, DIT_F16 = 2 } dit_dtype;
 
 /*
  * flags: precision of the 16-bit MFMA operands and the K/V staging strategy.
@@ -519,6 +520,131 @@ dit_status dit_dequant_rows_forward(const int8_t *q, const float *scale, void *y
  */
 dit_status dit_linear_quant_forward(const int8_t *x, const float *x_scale, const int8_t *w, const float *w_scale,
                                     const void *bias, void *y, const dit_linear_params *p, void *stream);
+
+/*
+ * ---- Chunk-wise generation over a paged key/value cache ----
+ * The Diffusion stage (Sec. 2.4) in its causal form generates a clip a few frames at a time, each attending to itself and to what
+ * is there; a text model that writes its prompts does so a token at a time.  The keys (normalised and rotated) and values of what
+ * is there stay in the pages of a cache, and three calls serve a chunk of new tokens:
+ *   dit_qk_rope_forward      q and k rows normalised and rotated by positions given for each token, to rows
+ *   dit_kv_append_forward    the same, k and v to the pages, q to rows
+ *   dit_attn_paged_forward   the attention of the chunk over the pages, its own tokens among them
+ * None allocates, synchronises or reads a count on the host: the counts are DEVICE arrays, so that a captured graph serves
+ * every step.  What the host tells besides (max_q, max_kv) is for planning only.
+ *
+ * Tokens of all requests are packed: rows [N, heads, D] (dit_strides, batch ignored).  Positions: int32 [N, 3] DEVICE, dense,
+ * (t, h, w) of every token, any integer; rotation as in dit_self_attn_params.  cos and sin are within 2^-22 of the formula's at
+ * every position; the arithmetic is fp32, rounded once to the type that is written.  fp16 saturates at +-65504.
+ * Normalisation: dit_qk_norm as above (q_gamma: H*D weights, k_gamma: Hk*D; DIT_NORM_TOKEN: over the H*D, or Hk*D, channels of
+ * the token), ahead of the rotation.  Rows whose squares fp32 does not hold are scaled by a power of two first.
+ */
+
+/*
+ * q_out = rotate(normalise(q)), k_out likewise.  q [N, H, D] and q_out, k [N, Hk, D] and k_out: q or k may be NULL (then H or
+ * Hk is 0).  pos NULL: no rotation (d_t, d_h, d_w, rope_base are ignored).  An output may be its input, if type and strides are
+ * the same; else it may overlap neither input.  No workspace.
+ * Errors: NULL p, q and k both NULL, an output that is NULL where its input is not (or the other way round), N < 0, heads that
+ * are not 1 or more where there are rows and 0 where there are none, a bad dtype, split, rope_base or norm, nonzero flags, rows
+ * that overlap -> DIT_ERR_INVALID_ARG; D other than 64 or 128, DIT_NORM_TOKEN with more heads than 512 of 128 channels or 1,024
+ * of 64 (those of q, k and v together, each rounded up to a multiple of 32 or 64) -> DIT_ERR_UNSUPPORTED; a base pointer or
+ * stride that breaks 16-byte row alignment (4 bytes for pos) -> DIT_ERR_ALIGNMENT.  N = 0 is no error and does nothing.
+ */
+typedef struct {
+    int32_t N;             /* tokens */
+    int32_t H, Hk, D;      /* heads of q and of k, head_dim (64 or 128) */
+    int32_t d_t, d_h, d_w; /* RoPE split */
+    float rope_base;
+    int32_t in_dtype;      /* of q and k: DIT_BF16 or DIT_F32 */
+    int32_t out_dtype;     /* of q_out and k_out: DIT_BF16, DIT_F32 or DIT_F16 */
+    uint32_t flags;        /* reserved, must be 0 */
+    dit_strides sq, sk, sq_out, sk_out;
+    dit_qk_norm norm;
+} dit_qk_rope_params;
+
+dit_status dit_qk_rope_forward(const void *q, const void *k, const int32_t *pos, void *q_out, void *k_out,
+                               const dit_qk_rope_params *p, void *stream);
+
+/*
+ * The cache.  K and V: pages [n_pages, page_size, Hk, D] each, addressed as base + page*stride.page + slot*stride.token +
+ * head*stride.head + channel (strides in ELEMENTS, the same for K and V, any order of pages, slots and heads that overlaps no
+ * rows; rows start on multiples of 16 bytes), bf16 or fp16.  Any page_size.
+ *   page_table  int32 [n_requests, max_pages] DEVICE, dense: token n of request r is in slot n % page_size of page
+ *               page_table[r][n / page_size].  An entry outside 0 .. n_pages-1 stands for a page that is not there (one that
+ *               was dropped to bound the cache, say): nothing is written to it, and its keys attend no more.  Requests may
+ *               share pages.
+ *   q_start     int32 [n_requests + 1] DEVICE, ascending from 0: rows q_start[r] .. q_start[r+1]-1 are request r's new tokens.
+ *               Rows from q_start[n_requests] on are of no request: neither read nor, where they are outputs, written.
+ *   kv_len      int32 [n_requests] DEVICE: tokens of the request, the new ones (its last) included; at most max_pages*page_size count.
+ * Counts that are out of range lead to no access out of range: q_start is clamped to 0 .. N, kv_len to 0 .. max_pages*page_size.
+ */
+typedef struct {
+    int32_t n_pages, page_size, Hk, D;
+    int32_t dtype; /* DIT_BF16 or DIT_F16 */
+    int32_t n_requests, max_pages;
+    int64_t page, token, head; /* element strides */
+} dit_kv_cache;
+
+/*
+ * The new tokens' k rows, normalised and rotated, and their v rows, to the pages; and q rows, normalised and rotated, to rows.
+ * New token i of request r goes to place kv_len[r] - new + i; one whose place is before 0, behind the table or in a page that is not there is not
+ * written (its q row is).  Two tokens may not go to the same slot.
+ *   k, v [N, Hk, D], q [N, H, D] of in_dtype; q and q_out both NULL: no q (H is 0).  pos as above.
+ * Errors: as dit_qk_rope_forward; NULL k, v, cache, page_table, q_start or kv_len, counts of the cache below 1, strides that let
+ * rows overlap -> DIT_ERR_INVALID_ARG; a cache of more than 64 GiB from its first row to its last -> DIT_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    int32_t N, H;          /* tokens, heads of q */
+    int32_t d_t, d_h, d_w; /* RoPE split */
+    float rope_base;
+    int32_t in_dtype;      /* of q, k and v: DIT_BF16 or DIT_F32 */
+    int32_t out_dtype;     /* of q_out: DIT_BF16, DIT_F32 or DIT_F16 */
+    uint32_t flags;        /* reserved, must be 0 */
+    dit_strides sq, sk, sv, sq_out;
+    dit_qk_norm norm;
+    dit_kv_cache cache;
+} dit_kv_append_params;
+
+dit_status dit_kv_append_forward(const void *q, const void *k, const void *v, const int32_t *pos, const int32_t *page_table,
+                                 const int32_t *q_start, const int32_t *kv_len, void *q_out, void *k_cache, void *v_cache,
+                                 const dit_kv_append_params *p, void *stream);
+
+/*
+ * out = softmax(scale * <q, k>) v over the keys of the row's own request that are there and that its token sees; q rows are
+ * (normalised and) rotated already.  H is a multiple of the cache's Hk: query head h reads key head h / (H / Hk).
+ * A token at place n (kv_len - new + i) sees, with frame = 0, every key; with frame > 0 those of its own frame n / frame (rounded down) and of the
+ * frames before it -- frame = 1 is the causal mask, frame = tokens of a video frame the frame-wise one --, with window > 0 only
+ * those of the last `window` frames, its own included.  A row that sees no key: out = 0, lse = -inf.
+ *   q     [N, H, D], DIT_BF16, DIT_F16 or DIT_F32; rounded to the cache's type if it is of another one (fp16 saturates)
+ *   out   [N, H, D], DIT_BF16 or DIT_F32.  It may be q, if type and strides are the same.
+ *   lse   (nullable) fp32 [H, N] dense, natural-log sum of exp(scale * score)
+ *   scale <= 0 selects 1/sqrt(D)
+ *   max_q, max_kv  the most new tokens and the most keys of any request, as far as the host knows (0: not); results are right
+ *         whatever they are, and their bits depend on them: they choose the kernels, and where tiles are few, the pieces that their keys are taken in
+ * Products are exact, scores, softmax and sums in fp32; probabilities are rounded to the cache's type for the product with V, the
+ * sums that divide it and lse are over the unrounded ones.  A masked key may hold anything, an infinity or a NaN too.
+ * Deterministic: the same arguments give the same bits.  A row's bits depend on the other requests' counts too (pieces).
+ * workspace: dit_attn_paged_workspace_bytes(p) bytes (the same for any counts), 256-byte aligned.
+ * Errors: NULL q, caches, page_table, q_start, kv_len, out or p, N < 0, H no multiple of Hk, a negative frame, window, max_q or max_kv, window
+ * without frame, a bad dtype, nonzero flags, rows that overlap -> DIT_ERR_INVALID_ARG; D other than 64 or 128, N * H / Hk of 2^31
+ * or more, a cache of more than 64 GiB -> DIT_ERR_UNSUPPORTED; alignment (4 bytes for counts, table and lse) -> DIT_ERR_ALIGNMENT; DIT_ERR_WORKSPACE.  N = 0 does nothing.
+ */
+typedef struct {
+    int32_t N, H;
+    int32_t frame, window;
+    int32_t max_q, max_kv;
+    float scale;
+    int32_t q_dtype, out_dtype;
+    uint32_t flags; /* reserved, must be 0 */
+    dit_strides sq, so;
+    dit_kv_cache cache;
+} dit_paged_attn_params;
+
+/* Bytes of workspace the call needs (0 on invalid params). */
+size_t dit_attn_paged_workspace_bytes(const dit_paged_attn_params *p);
+
+dit_status dit_attn_paged_forward(const void *q, const void *k_cache, const void *v_cache, const int32_t *page_table,
+                                  const int32_t *q_start, const int32_t *kv_len, void *out, float *lse,
+                                  const dit_paged_attn_params *p, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static strings; never NULL. */
 const char *dit_strerror(dit_status s);

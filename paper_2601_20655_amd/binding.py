@@ -33,6 +33,7 @@ DIT_ERR_HIP = -5
 
 DIT_BF16 = 0
 DIT_F32 = 1
+DIT_F16 = 2
 
 DIT_FLAG_QK_BF16 = 1 << 0
 DIT_FLAG_QK_F16 = 1 << 1
@@ -64,6 +65,10 @@ EXPORTS = (
     "dit_rms_norm_quant_forward",
     "dit_dequant_rows_forward",
     "dit_linear_quant_forward",
+    "dit_qk_rope_forward",
+    "dit_kv_append_forward",
+    "dit_attn_paged_workspace_bytes",
+    "dit_attn_paged_forward",
     "dit_mfma_probe",
     "dit_attn_set_timing_events",
     "dit_strerror",
@@ -168,6 +173,43 @@ class dit_dequant_rows_params(ctypes.Structure):
     ]
 
 
+class dit_qk_rope_params(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("d_t", ctypes.c_int32), ("d_h", ctypes.c_int32), ("d_w", ctypes.c_int32), ("rope_base", ctypes.c_float),
+        ("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("sq", dit_strides), ("sk", dit_strides), ("sq_out", dit_strides), ("sk_out", dit_strides),
+        ("norm", dit_qk_norm),
+    ]
+
+
+class dit_kv_cache(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("Hk", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("n_requests", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("page", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64),
+    ]
+
+
+class dit_kv_append_params(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32),
+        ("d_t", ctypes.c_int32), ("d_h", ctypes.c_int32), ("d_w", ctypes.c_int32), ("rope_base", ctypes.c_float),
+        ("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("sq", dit_strides), ("sk", dit_strides), ("sv", dit_strides), ("sq_out", dit_strides),
+        ("norm", dit_qk_norm), ("cache", dit_kv_cache),
+    ]
+
+
+class dit_paged_attn_params(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32), ("frame", ctypes.c_int32), ("window", ctypes.c_int32),
+        ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("q_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("sq", dit_strides), ("so", dit_strides), ("cache", dit_kv_cache),
+    ]
+
+
 class DitError(RuntimeError):
     def __init__(self, status, what):
         self.status = int(status)
@@ -222,6 +264,14 @@ def lib():
         L.dit_dequant_rows_forward.argtypes = [vp, vp, vp, ctypes.POINTER(dit_dequant_rows_params), vp]
         L.dit_linear_quant_forward.restype = ctypes.c_int
         L.dit_linear_quant_forward.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(dit_linear_params), vp]
+        L.dit_qk_rope_forward.restype = ctypes.c_int
+        L.dit_qk_rope_forward.argtypes = [vp] * 5 + [ctypes.POINTER(dit_qk_rope_params), vp]
+        L.dit_kv_append_forward.restype = ctypes.c_int
+        L.dit_kv_append_forward.argtypes = [vp] * 10 + [ctypes.POINTER(dit_kv_append_params), vp]
+        L.dit_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.dit_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(dit_paged_attn_params)]
+        L.dit_attn_paged_forward.restype = ctypes.c_int
+        L.dit_attn_paged_forward.argtypes = [vp] * 8 + [ctypes.POINTER(dit_paged_attn_params), vp, ctypes.c_size_t, vp]
         L.dit_mfma_probe.restype = ctypes.c_int
         L.dit_mfma_probe.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, vp, ctypes.c_size_t,
                                      ctypes.POINTER(ctypes.c_double), vp]
@@ -799,6 +849,237 @@ def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dt
     if st != DIT_OK:
         raise DitError(st, what)
     return out
+
+
+# ---- chunk-wise generation over a paged cache ----
+
+_DTYPE16_CODES = {}
+
+
+def _dtype16_code(what, name, t):
+    """Type code of rows that may be fp16 too."""
+    if not _DTYPE16_CODES:
+        _DTYPE16_CODES.update({torch.bfloat16: DIT_BF16, torch.float32: DIT_F32, torch.float16: DIT_F16})
+    code = _DTYPE16_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError("%s: %s must be bfloat16, float16 or float32, got %s" % (what, name, t.dtype))
+    return code
+
+
+def _stream_on(what, stream, device):
+    """The stream's handle; the library works on the device that is current, where the tensors have to be too."""
+    current = torch.cuda.current_device()
+    if current != device or (stream is not None and stream.device_index != device):
+        raise ValueError("%s: the tensors are on device %d, the current device%s is %d" % (
+            what, device, "" if current != device else "'s stream", current if current != device else stream.device_index))
+    return _stream_ptr(stream)
+
+
+def _check_range(what, **numbers):
+    """Whole numbers that the library holds in 32 bits; ctypes would cut larger ones off without a word."""
+    for name, n in numbers.items():
+        if not 0 <= n <= _MOST_COUNT:
+            raise ValueError("%s: %s must be 0 .. %d, got %s" % (what, name, _MOST_COUNT, n))
+
+
+def _check_split(what, split, D):
+    if len(split) != 3 or min(split) < 0 or sum(split) != D or any(n % 2 for n in split):
+        raise ValueError("%s: split must be three even numbers whose sum is %d, got %s" % (what, D, tuple(split)))
+
+
+def _token_rows(what, name, t, N, D, device):
+    """dit_strides of t: a [N, heads, D] tensor on that device (its index), contiguous along its channels."""
+    shape, s = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != N or shape[2] != D:
+        raise ValueError("%s: %s has shape %s, expected [%d, heads, %d]" % (what, name, tuple(shape), N, D))
+    if t.get_device() != device or device < 0:
+        raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+    if s[2] != 1:
+        raise ValueError("%s: %s must have contiguous channels" % (what, name))
+    return dit_strides(0, s[0], s[1])
+
+
+def _check_counts(what, device, **tensors):
+    """int32 device tensors, dense: name = (tensor, shape)."""
+    for name, (t, shape) in tensors.items():
+        if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError("%s: %s must be a dense int32 tensor of shape %s" % (what, name, shape))
+        if t.get_device() != device:
+            raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+
+
+def _rope_norm(what, norm, H, Hk, D, device):
+    """norm: None, or (mode, eps, q_gamma, k_gamma) as in qk_norm, with weights of H*D and of Hk*D elements."""
+    if norm is None:
+        return dit_qk_norm()
+    mode, eps, gq, gk = norm
+    if mode not in _NORM_CODES:
+        raise ValueError("%s: norm must be one of %s" % (what, ", ".join(sorted(_NORM_CODES))))
+    for name, g, n in (("q_gamma", gq, H * D), ("k_gamma", gk, Hk * D)):
+        if g is not None and (g.dtype != torch.float32 or g.numel() != n or not g.is_contiguous() or g.get_device() != device):
+            raise ValueError("%s: %s must be a dense float32 tensor of %d elements on the rows' device" % (what, name, n))
+    return dit_qk_norm(_NORM_CODES[mode], eps, gq.data_ptr() if gq is not None else None,
+                       gk.data_ptr() if gk is not None else None)
+
+
+_NORM_CODES = {"head": DIT_NORM_HEAD, "token": DIT_NORM_TOKEN}
+
+
+def dit_qk_rope_forward(q, k, pos, split=(0, 0, 0), q_out=None, k_out=None, out_dtype=None, rope_base=10000.0, norm=None,
+                        stream=None):
+    """q [N, H, D] and k [N, Hk, D] (bf16 or float32; either may be None), normalised (norm: None or (mode, eps, q_gamma,
+    k_gamma), see qk_norm; q_gamma of H*D, k_gamma of Hk*D elements) and rotated by the positions pos, int32 [N, 3] (None: not),
+    whose axes have split channels.  Returns (q_out, k_out), bf16, float32 or float16 rows, allocated in out_dtype (default: that
+    of the input) if not given; they may be q and k themselves."""
+    what = "dit_qk_rope_forward"
+    some = q if q is not None else k
+    if some is None or some.dim() != 3:
+        raise ValueError("%s: q must be [N, H, D] and k [N, Hk, D], one of them at least" % what)
+    N, D, device = some.shape[0], some.shape[2], some.get_device()
+    if N > _MOST_COUNT:
+        _too_many(what)
+    heads, strides, codes, outs = [0, 0], [dit_strides() for _ in range(4)], set(), [q_out, k_out]
+    for i, (name, x) in enumerate((("q", q), ("k", k))):
+        if x is None:
+            if outs[i] is not None:
+                raise ValueError("%s: %s_out needs %s" % (what, name, name))
+            continue
+        if x.dtype != some.dtype:
+            raise TypeError("%s: q and k must share one dtype" % what)
+        strides[i] = _token_rows(what, name, x, N, D, device)
+        heads[i] = x.shape[1]
+        if outs[i] is None:
+            outs[i] = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        strides[2 + i] = _token_rows(what, name + "_out", outs[i], N, D, device)
+        if outs[i].shape != x.shape:
+            raise ValueError("%s: %s_out must have the shape of %s" % (what, name, name))
+        codes.add(_dtype16_code(what, name + "_out", outs[i]))
+    if len(codes) != 1:
+        raise TypeError("%s: q_out and k_out must share one dtype" % what)
+    if pos is not None:
+        _check_counts(what, device, pos=(pos, (N, 3)))
+        _check_split(what, split, D)
+    p = dit_qk_rope_params(N, heads[0], heads[1], D, split[0], split[1], split[2], rope_base, _dtype_code(some), codes.pop(), 0,
+                           strides[0], strides[1], strides[2], strides[3], _rope_norm(what, norm, heads[0], heads[1], D, device))
+    ptr = [t.data_ptr() if t is not None else None for t in (q, k, pos, outs[0], outs[1])]
+    st = lib().dit_qk_rope_forward(*ptr, ctypes.byref(p), _stream_on(what, stream, device))
+    if st != DIT_OK:
+        raise DitError(st, what)
+    return outs[0], outs[1]
+
+
+def kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device):
+    """dit_kv_cache of k_cache and v_cache [pages, page_size, Hk, D] (any strides, the same for both; bf16 or float16),
+    page_table [requests, max_pages], q_start [requests + 1] and kv_len [requests] (int32)."""
+    shape, s = k_cache.shape, k_cache.stride()
+    if len(shape) != 4 or v_cache.shape != shape or v_cache.stride() != s or s[3] != 1:
+        raise ValueError("%s: k_cache and v_cache must be [pages, page_size, heads, D] tensors of the same strides with "
+                         "contiguous channels" % what)
+    if v_cache.dtype != k_cache.dtype or k_cache.dtype == torch.float32:
+        raise TypeError("%s: k_cache and v_cache must both be bfloat16 or both float16" % what)
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if t.get_device() != device or device < 0:
+            raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+    if page_table.dim() != 2:
+        raise ValueError("%s: page_table must be [requests, pages]" % what)
+    R, pages = page_table.shape
+    if max(shape[0], shape[1], R, pages) > _MOST_COUNT:
+        _too_many(what)
+    _check_counts(what, device, page_table=(page_table, (R, pages)), q_start=(q_start, (R + 1,)), kv_len=(kv_len, (R,)))
+    return dit_kv_cache(shape[0], shape[1], shape[2], shape[3], _dtype16_code(what, "k_cache", k_cache), R, pages, s[0], s[1], s[2])
+
+
+def dit_kv_append_forward(k, v, k_cache, v_cache, page_table, q_start, kv_len, pos=None, split=(0, 0, 0), q=None, q_out=None,
+                          out_dtype=None, rope_base=10000.0, norm=None, stream=None):
+    """The new tokens' rows k, v [N, Hk, D] (bf16 or float32), k normalised and rotated as in dit_qk_rope_forward, to the pages of
+    the cache (see kv_cache): rows q_start[r] .. q_start[r+1]-1 are the last of the kv_len[r] tokens that request r then has.
+    With q [N, H, D], its rows normalised and rotated to q_out, which is returned (allocated in out_dtype, default that of q, if
+    not given)."""
+    what = "dit_kv_append_forward"
+    if k.dim() != 3 or v.shape != k.shape:
+        raise ValueError("%s: k and v must be [N, Hk, D]" % what)
+    N, Hk, D = k.shape
+    device = k.get_device()
+    if N > _MOST_COUNT:
+        _too_many(what)
+    sk, sv = _token_rows(what, "k", k, N, D, device), _token_rows(what, "v", v, N, D, device)
+    cache = kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device)
+    if cache.Hk != Hk or cache.D != D:
+        raise ValueError("%s: the cache has rows of %d x %d, k of %d x %d" % (what, cache.Hk, cache.D, Hk, D))
+    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise TypeError("%s: q, k and v must share one dtype" % what)
+    H, sq, sq_out, out_code = 0, dit_strides(), dit_strides(), DIT_BF16
+    if q is not None:
+        sq = _token_rows(what, "q", q, N, D, device)
+        H = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+        sq_out = _token_rows(what, "q_out", q_out, N, D, device)
+        if q_out.shape != q.shape:
+            raise ValueError("%s: q_out must have the shape of q" % what)
+        out_code = _dtype16_code(what, "q_out", q_out)
+    elif q_out is not None:
+        raise ValueError("%s: q_out needs q" % what)
+    if pos is not None:
+        _check_counts(what, device, pos=(pos, (N, 3)))
+        _check_split(what, split, D)
+    p = dit_kv_append_params(N, H, split[0], split[1], split[2], rope_base, _dtype_code(k), out_code, 0, sq, sk, sv, sq_out,
+                             _rope_norm(what, norm, H, Hk, D, device), cache)
+    ptr = [t.data_ptr() if t is not None else None
+           for t in (q, k, v, pos, page_table, q_start, kv_len, q_out, k_cache, v_cache)]
+    st = lib().dit_kv_append_forward(*ptr, ctypes.byref(p), _stream_on(what, stream, device))
+    if st != DIT_OK:
+        raise DitError(st, what)
+    return q_out
+
+
+def dit_attn_paged_workspace_bytes(params):
+    return int(lib().dit_attn_paged_workspace_bytes(ctypes.byref(params)))
+
+
+def dit_attn_paged_forward(q, k_cache, v_cache, page_table, q_start, kv_len, frame=0, window=0, max_q=0, max_kv=0, out=None,
+                           lse=None, scale=0.0, out_dtype=None, workspace=None, stream=None, want_lse=False):
+    """Attention of the new tokens' rows q [N, H, D] (bf16, float16 or float32, rotated already) over the pages of the cache (see
+    kv_cache).  frame: 0, a token sees every key of its request; else those of its own frame of so many tokens and of the frames
+    before it (1: the causal mask), with window > 0 of the last `window` frames only.  max_q, max_kv: the most new tokens and keys
+    of any request, if the host knows them (for planning).  Returns out (bf16 or float32; rows of no request are left as they
+    are), and with want_lse or lse (out, lse), lse float32 [H, N]."""
+    what = "dit_attn_paged_forward"
+    if q.dim() != 3:
+        raise ValueError("%s: q must be [N, H, D]" % what)
+    N, H, D = q.shape
+    device = q.get_device()
+    if N > _MOST_COUNT or H > _MOST_COUNT:
+        _too_many(what)
+    _check_range(what, frame=frame, window=window, max_q=max_q, max_kv=max_kv)
+    sq = _token_rows(what, "q", q, N, D, device)
+    cache = kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device)
+    if cache.D != D or cache.Hk < 1 or H % cache.Hk:
+        raise ValueError("%s: q's %d heads of %d channels do not fit the cache's %d of %d" % (what, H, D, cache.Hk, cache.D))
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or (torch.bfloat16 if q.dtype == torch.float16 else q.dtype), device=q.device)
+    so = _token_rows(what, "out", out, N, D, device)
+    if out.shape != q.shape:
+        raise ValueError("%s: out must have the shape of q" % what)
+    if lse is None and want_lse:
+        lse = torch.empty((H, N), dtype=torch.float32, device=q.device)
+    elif lse is not None:
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (H, N) or not lse.is_contiguous() or lse.get_device() != device:
+            raise ValueError("%s: lse must be a dense float32 tensor of shape %s on q's device" % (what, (H, N)))
+    p = dit_paged_attn_params(N, H, frame, window, max_q, max_kv, scale, _dtype16_code(what, "q", q), _dtype_code(out), 0, sq, so,
+                              cache)
+    need = dit_attn_paged_workspace_bytes(p)
+    if workspace is None:
+        workspace = _workspace(need, q.device)
+    else:
+        _check_workspace(what, workspace, need, q.device)
+    st = lib().dit_attn_paged_forward(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
+                                      q_start.data_ptr(), kv_len.data_ptr(), out.data_ptr(),
+                                      lse.data_ptr() if lse is not None else None, ctypes.byref(p), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), _stream_on(what, stream, device))
+    if st != DIT_OK:
+        raise DitError(st, what)
+    return (out, lse) if lse is not None else out
 
 
 DIT_PROBE_BF16 = 0

@@ -7,6 +7,7 @@
 
 #include "../../include/dit_attn.h"
 #include "dit_attn_internal.h"
+#include "dit_paged.h"
 
 namespace dit {
 hipError_t launch_attn_d128_qb1(const AttnArgs&, int, int, bool, hipStream_t);
@@ -1412,6 +1413,245 @@ dit_status dit_linear_quant_forward(const int8_t* x, const float* x_scale, const
 void dit_attn_set_timing_events(void* before, void* after) {
     g_ev_before = static_cast<hipEvent_t>(before);
     g_ev_after = static_cast<hipEvent_t>(after);
+}
+
+// ---- chunk-wise generation over a paged cache ----
+
+namespace {
+
+bool dtype16_or_32(int32_t t) { return t == DIT_BF16 || t == DIT_F32 || t == DIT_F16; }
+
+// A split and base that rotate rows of D channels.
+bool rotation_ok(int32_t D, int32_t d_t, int32_t d_h, int32_t d_w, float base) {
+    if (d_t < 0 || d_h < 0 || d_w < 0 || (d_t | d_h | d_w) & 1) return false;
+    return (int64_t)d_t + d_h + d_w == D && base > 0.f && isfinite(base);
+}
+
+// Turns per position of every pair: base^(-2i / d) / 2 pi, as a power of two whose exponent is held in two parts (see
+// rope_entry; powl took 10 us for the pairs of a head).
+void set_turns(dit::RowsArgs* a, int32_t d_t, int32_t d_h, int32_t d_w, float base) {
+    const int32_t d[3] = {d_t, d_h, d_w};
+    const long double l = log2l((long double)base);
+    const double hi = (double)l, lo = (double)(l - (long double)hi);
+    int pair = 0;
+    for (int ax = 0; ax < 3; ++ax) {
+        a->hd[ax] = d[ax] / 2;
+        for (int i = 0; i < a->hd[ax]; ++i) {
+            const double x = -(double)i / a->hd[ax], t = x * hi, rest = fma(x, hi, -t) + x * lo, y = exp2(t);
+            a->turn[pair++] = fma(y, rest * 0.6931471805599453, y) * 0.15915494309189535;
+        }
+    }
+}
+
+dit_status cache_ok(const dit_kv_cache& c) {
+    if (c.n_pages < 1 || c.page_size < 1 || c.Hk < 1 || c.n_requests < 1 || c.max_pages < 1) return DIT_ERR_INVALID_ARG;
+    if (c.dtype != DIT_BF16 && c.dtype != DIT_F16) return DIT_ERR_INVALID_ARG;
+    if (c.D != 64 && c.D != 128) return DIT_ERR_UNSUPPORTED;
+    // the dimensions that have more than one entry, by stride: each clears the rows of those below it
+    struct Dim {
+        int64_t n, stride;
+    } d[3] = {{c.n_pages, c.page}, {c.page_size, c.token}, {c.Hk, c.head}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (d[j].stride < d[i].stride) {
+                const Dim t = d[i];
+                d[i] = d[j];
+                d[j] = t;
+            }
+    const int64_t most = (int64_t)1 << 35;  // elements of 64 GiB
+    int64_t extent = c.D;
+    for (const Dim& x : d) {
+        if (x.n == 1) continue;
+        if (x.stride < extent) return DIT_ERR_INVALID_ARG;
+        if (x.stride > most / (x.n - 1)) return DIT_ERR_UNSUPPORTED;
+        extent += (x.n - 1) * x.stride;
+        if (extent > most) return DIT_ERR_UNSUPPORTED;
+    }
+    return DIT_OK;
+}
+bool cache_aligned(const dit_kv_cache& c, const void* k, const void* v) {
+    if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u) return false;
+    return (c.n_pages == 1 || c.page % 8 == 0) && (c.page_size == 1 || c.token % 8 == 0) && (c.Hk == 1 || c.head % 8 == 0);
+}
+bool aligned4(const void* a, const void* b, const void* c) {
+    return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & 3u) == 0;
+}
+
+dit::PageArgs page_args(const dit_kv_cache& c, const int32_t* table, const int32_t* q_start, const int32_t* kv_len) {
+    dit::PageArgs p{};
+    p.table = table;
+    p.q_start = q_start;
+    p.kv_len = kv_len;
+    p.n_requests = c.n_requests;
+    p.max_pages = c.max_pages;
+    p.n_pages = c.n_pages;
+    // (a stride that is never taken need not fit)
+    p.page16 = c.n_pages > 1 ? (uint32_t)(c.page / 8) : 0;
+    p.token16 = c.page_size > 1 ? (uint32_t)(c.token / 8) : 0;
+    p.head16 = c.Hk > 1 ? (uint32_t)(c.head / 8) : 0;
+    p.page = dit::fast_div((uint32_t)c.page_size);
+    return p;
+}
+
+// Rows of N tokens: as the other calls have it, but that a single token's or head's stride is never taken.
+bool rows_ok(const dit_strides& s, int32_t H, int32_t D, int32_t N) {
+    if ((N > 1 && s.token < D) || (H > 1 && s.head < D)) return false;
+    if (N > 1 && H > 1) return s.token >= (int64_t)H * s.head || s.head >= (int64_t)N * s.token;
+    return true;
+}
+bool rows_aligned(const void* p, const dit_strides& s, int32_t H, int32_t N, int32_t dtype) {
+    const int64_t per16 = dtype == DIT_F32 ? 4 : 8;
+    if (reinterpret_cast<uintptr_t>(p) & 15u) return false;
+    return (N == 1 || s.token % per16 == 0) && (H == 1 || s.head % per16 == 0);
+}
+dit::RowTensor row_tensor(const void* x, void* y, const float* gamma, int32_t H, const dit_strides& sx, const dit_strides& sy) {
+    return {x, y, gamma, x ? H : 0, sx.token, sx.head, sy.token, sy.head};
+}
+
+}  // namespace
+
+dit_status dit_qk_rope_forward(const void* q, const void* k, const int32_t* pos, void* q_out, void* k_out,
+                               const dit_qk_rope_params* p, void* stream) {
+    if (!p || p->N < 0 || p->flags != 0 || bad_dtype(p->in_dtype) || !dtype16_or_32(p->out_dtype)) return DIT_ERR_INVALID_ARG;
+    if (p->D != 64 && p->D != 128) return DIT_ERR_UNSUPPORTED;
+    if (p->N == 0) return DIT_OK;
+    if ((!q && !k) || !q != !q_out || !k != !k_out) return DIT_ERR_INVALID_ARG;
+    if ((q && p->H < 1) || (!q && p->H != 0) || (k && p->Hk < 1) || (!k && p->Hk != 0)) return DIT_ERR_INVALID_ARG;
+    if (pos && !rotation_ok(p->D, p->d_t, p->d_h, p->d_w, p->rope_base)) return DIT_ERR_INVALID_ARG;
+    dit_status st = norm_ok(p->norm);
+    if (st != DIT_OK) return st;
+    if (q && !(rows_ok(p->sq, p->H, p->D, p->N) && rows_ok(p->sq_out, p->H, p->D, p->N))) return DIT_ERR_INVALID_ARG;
+    if (k && !(rows_ok(p->sk, p->Hk, p->D, p->N) && rows_ok(p->sk_out, p->Hk, p->D, p->N))) return DIT_ERR_INVALID_ARG;
+    if (p->norm.mode == DIT_NORM_TOKEN && !dit::rows_fit(p->H, p->Hk, 0, p->D)) return DIT_ERR_UNSUPPORTED;
+    if (!aligned4(pos, nullptr, nullptr)) return DIT_ERR_ALIGNMENT;
+    if (q && !(rows_aligned(q, p->sq, p->H, p->N, p->in_dtype) && rows_aligned(q_out, p->sq_out, p->H, p->N, p->out_dtype)))
+        return DIT_ERR_ALIGNMENT;
+    if (k && !(rows_aligned(k, p->sk, p->Hk, p->N, p->in_dtype) && rows_aligned(k_out, p->sk_out, p->Hk, p->N, p->out_dtype)))
+        return DIT_ERR_ALIGNMENT;
+    dit::RowsArgs a{};
+    a.q = row_tensor(q, q_out, p->norm.q_gamma, p->H, p->sq, p->sq_out);
+    a.k = row_tensor(k, k_out, p->norm.k_gamma, p->Hk, p->sk, p->sk_out);
+    a.pos = pos;
+    a.N = p->N;
+    a.x_f32 = p->in_dtype == DIT_F32;
+    a.y_type = p->out_dtype;
+    a.norm = p->norm.mode;
+    a.eps = p->norm.eps;
+    if (pos) set_turns(&a, p->d_t, p->d_h, p->d_w, p->rope_base);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("rows_kernel", s, [&] { return dit::launch_rows(a, p->D, s); });
+}
+
+dit_status dit_kv_append_forward(const void* q, const void* k, const void* v, const int32_t* pos, const int32_t* page_table,
+                                 const int32_t* q_start, const int32_t* kv_len, void* q_out, void* k_cache, void* v_cache,
+                                 const dit_kv_append_params* p, void* stream) {
+    if (!p || p->N < 0 || p->flags != 0 || bad_dtype(p->in_dtype) || !dtype16_or_32(p->out_dtype)) return DIT_ERR_INVALID_ARG;
+    dit_status st = cache_ok(p->cache);
+    if (st != DIT_OK) return st;
+    if (p->N == 0) return DIT_OK;
+    if (!k || !v || !k_cache || !v_cache || !page_table || !q_start || !kv_len || !q != !q_out) return DIT_ERR_INVALID_ARG;
+    if ((q && p->H < 1) || (!q && p->H != 0)) return DIT_ERR_INVALID_ARG;
+    const int32_t D = p->cache.D, Hk = p->cache.Hk;
+    if (pos && !rotation_ok(D, p->d_t, p->d_h, p->d_w, p->rope_base)) return DIT_ERR_INVALID_ARG;
+    st = norm_ok(p->norm);
+    if (st != DIT_OK) return st;
+    if (q && !(rows_ok(p->sq, p->H, D, p->N) && rows_ok(p->sq_out, p->H, D, p->N))) return DIT_ERR_INVALID_ARG;
+    if (!rows_ok(p->sk, Hk, D, p->N) || !rows_ok(p->sv, Hk, D, p->N)) return DIT_ERR_INVALID_ARG;
+    if (p->norm.mode == DIT_NORM_TOKEN && !dit::rows_fit(p->H, Hk, Hk, D)) return DIT_ERR_UNSUPPORTED;
+    if (!aligned4(pos, page_table, q_start) || !aligned4(kv_len, nullptr, nullptr) || !cache_aligned(p->cache, k_cache, v_cache))
+        return DIT_ERR_ALIGNMENT;
+    if (!rows_aligned(k, p->sk, Hk, p->N, p->in_dtype) || !rows_aligned(v, p->sv, Hk, p->N, p->in_dtype)) return DIT_ERR_ALIGNMENT;
+    if (q && !(rows_aligned(q, p->sq, p->H, p->N, p->in_dtype) && rows_aligned(q_out, p->sq_out, p->H, p->N, p->out_dtype)))
+        return DIT_ERR_ALIGNMENT;
+    dit::RowsArgs a{};
+    a.q = row_tensor(q, q_out, p->norm.q_gamma, p->H, p->sq, p->sq_out);
+    a.k = row_tensor(k, nullptr, p->norm.k_gamma, Hk, p->sk, p->sk);
+    a.v = row_tensor(v, nullptr, nullptr, Hk, p->sv, p->sv);
+    a.pos = pos;
+    a.N = p->N;
+    a.x_f32 = p->in_dtype == DIT_F32;
+    a.y_type = p->out_dtype;
+    a.norm = p->norm.mode;
+    a.eps = p->norm.eps;
+    a.cached = 1;
+    a.cache_f16 = p->cache.dtype == DIT_F16;
+    a.pages = page_args(p->cache, page_table, q_start, kv_len);
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    if (pos) set_turns(&a, p->d_t, p->d_h, p->d_w, p->rope_base);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("rows_kernel", s, [&] { return dit::launch_rows(a, D, s); });
+}
+
+namespace {
+
+dit_status check_paged(const dit_paged_attn_params* p, dit::PagedPlan* plan) {
+    if (!p || p->N < 0 || p->H < 1 || p->flags != 0 || p->frame < 0 || p->window < 0 || p->max_q < 0 || p->max_kv < 0)
+        return DIT_ERR_INVALID_ARG;
+    if (bad_dtype(p->out_dtype) || !dtype16_or_32(p->q_dtype) || (p->window && !p->frame)) return DIT_ERR_INVALID_ARG;
+    const dit_status st = cache_ok(p->cache);
+    if (st != DIT_OK) return st;
+    if (p->H % p->cache.Hk) return DIT_ERR_INVALID_ARG;
+    if (!rows_ok(p->sq, p->H, p->cache.D, p->N) || !rows_ok(p->so, p->H, p->cache.D, p->N)) return DIT_ERR_INVALID_ARG;
+    if ((int64_t)p->N * (p->H / p->cache.Hk) > 0x7fffffff) return DIT_ERR_UNSUPPORTED;
+    int64_t keys = (int64_t)p->cache.max_pages * p->cache.page_size;
+    if (p->max_kv && p->max_kv < keys) keys = p->max_kv;
+    if (keys > 0x7fffffff) keys = 0x7fffffff;
+    *plan = p->N ? dit::plan_paged(p->N, p->cache.n_requests, p->H, p->cache.Hk, p->cache.D, keys, p->max_q) : dit::PagedPlan{};
+    return DIT_OK;
+}
+
+}  // namespace
+
+size_t dit_attn_paged_workspace_bytes(const dit_paged_attn_params* p) {
+    dit::PagedPlan plan;
+    if (check_paged(p, &plan) != DIT_OK) return 0;
+    const size_t n = plan.few_bytes + plan.big_bytes;
+    return n < kAlign ? kAlign : n;
+}
+
+dit_status dit_attn_paged_forward(const void* q, const void* k_cache, const void* v_cache, const int32_t* page_table,
+                                  const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
+                                  const dit_paged_attn_params* p, void* workspace, size_t workspace_bytes, void* stream) {
+    dit::PagedPlan plan;
+    const dit_status st = check_paged(p, &plan);
+    if (st != DIT_OK) return st;
+    if (p->N == 0) return DIT_OK;
+    if (!q || !k_cache || !v_cache || !page_table || !q_start || !kv_len || !out) return DIT_ERR_INVALID_ARG;
+    if (!aligned4(page_table, q_start, kv_len) || !aligned4(lse, nullptr, nullptr) || !cache_aligned(p->cache, k_cache, v_cache))
+        return DIT_ERR_ALIGNMENT;
+    if (!rows_aligned(q, p->sq, p->H, p->N, p->q_dtype) || !rows_aligned(out, p->so, p->H, p->N, p->out_dtype))
+        return DIT_ERR_ALIGNMENT;
+    const size_t need = plan.few_bytes + plan.big_bytes;
+    if (need && (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < need)) return DIT_ERR_WORKSPACE;
+    dit::PagedAttnArgs a{};
+    a.q = q;
+    a.k_cache = static_cast<const uint8_t*>(k_cache);
+    a.v_cache = static_cast<const uint8_t*>(v_cache);
+    a.out = out;
+    a.lse = lse;
+    a.pages = page_args(p->cache, page_table, q_start, kv_len);
+    a.N = p->N;
+    a.H = p->H;
+    a.Hk = p->cache.Hk;
+    a.G = p->H / p->cache.Hk;
+    a.group = dit::fast_div((uint32_t)a.G);
+    a.sq_t = p->sq.token;
+    a.sq_h = p->sq.head;
+    a.so_t = p->so.token;
+    a.so_h = p->so.head;
+    a.q_type = p->q_dtype;
+    a.out_type = p->out_dtype;
+    a.frame = p->frame;
+    a.window = p->window;
+    a.frame_div = dit::fast_div((uint32_t)(p->frame ? p->frame : 1));
+    a.scale = p->scale > 0.f ? p->scale : 1.0f / sqrtf((float)p->cache.D);
+    a.scale_log2 = a.scale * dit::kLog2e;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return timed_launch("attn_paged_kernel", s, [&] {
+        return dit::launch_attn_paged(a, plan, p->cache.D, p->cache.dtype == DIT_F16 ? dit::OP_F16 : dit::OP_BF16,
+                                      static_cast<uint8_t*>(workspace), s);
+    });
 }
 
 const char* dit_strerror(dit_status s) {

@@ -1,0 +1,831 @@
+// Attention of chunks of new tokens over a paged key/value cache (gfx950).
+//
+// For query token i of a request's `new` ones, at place p = kv_len - new + i:
+//     out = softmax(scale q K^T over the keys first(p) .. past(p) - 1 whose pages are there) V.
+// Rows: the query heads that share a key head are rows of one tile (row = token * G + head in the group), so that each tile
+// of keys is read once for all of them.
+//
+// Scores: S^T(key, row) = K Q^T on v_mfma_f32_16x16x32, 16 keys x 16 rows a block: a lane (i = lane % 16, g = lane / 16) holds
+// row i's scores of keys 4g .. 4g+3 of each block.  The rounded probabilities of blocks 2m and 2m + 1 are, as they lie, the
+// lane's B operand of O^T += V^T P^T over 32 keys; the matching A operand, eight keys of one channel, comes out of LDS rows of
+// V by two transposing reads (ds_read_b64_tr_b16: four rows x 16 channels a group of 16 lanes).  So K and V go from the
+// pages to LDS as the rows they are (global_load_lds, 16 bytes a lane), and P never moves between lanes.
+#include "dit_paged.h"
+
+#include "../../include/dit_attn.h"
+#include "dit_attn_fwd_pipe16.h"
+
+namespace dit {
+
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* ltr_t;
+
+constexpr float kNoScore = -1e30f;  // running maximum of a row that has none (finite: differences stay numbers)
+
+// ---- rows of K and V in LDS ----
+// A row's 16-byte pieces lie in an order of the row's own, so that a fragment's read takes each bank once: K fragments read one
+// piece of 16 rows, V fragments two neighbouring pieces of 8 rows (twice).  global_load_lds fills LDS in lane order: the order
+// is in which piece a lane fetches.
+template <int D>
+__device__ __forceinline__ int k_slot(int row, int piece) {
+    return D == 128 ? piece ^ (row & 15) : piece ^ ((row >> 1) & 7);
+}
+template <int D>
+__device__ __forceinline__ int v_slot(int row, int piece) {
+    return D == 128 ? piece ^ ((row & 7) << 1) : piece ^ (((row >> 1) & 3) << 1);
+}
+
+// Operand of 16 keys (rows key0 .. +15), channels 32 ks .. +31: the lane's key i, channels 8g .. +7.
+template <int D>
+__device__ __forceinline__ u32x4 k_fragment(const uint8_t* k, int key0, int ks, int i, int g) {
+    const int row = key0 + i;
+    return *reinterpret_cast<const u32x4*>(k + row * (2 * D) + 16 * k_slot<D>(row, 4 * ks + g));
+}
+// Operand of 16 channels (16 cb .. +15) and 32 keys (rows key0 .. +31): the lane's channel i, keys 4g .. +3 and 16 + 4g .. +3.
+template <int D>
+__device__ __forceinline__ u32x4 v_fragment(uint8_t* v, int key0, int cb, int i, int g) {
+    uint2 h[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        const int row = key0 + 16 * b + 4 * g + (i >> 2);
+        uint8_t* const p = v + row * (2 * D) + 16 * v_slot<D>(row, 2 * cb + ((i & 3) >> 1)) + 8 * (i & 1);
+        h[b] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr_t)p));
+    }
+    return mk4(h[0].x, h[0].y, h[1].x, h[1].y);
+}
+
+// ---- which work ----
+struct Unit {
+    int r;             // request
+    int q0, new_;      // its first new token, their number
+    int keys;          // its keys
+    int tile;          // of query rows
+    int piece, pieces; // of its keys
+    int slot;          // of the piece, among the key head's
+};
+
+// A request as the wavefronts see it.
+struct Load {
+    int tiles, key_tiles;
+};
+template <int BQ>
+__device__ __forceinline__ Load load_of(const PagedAttnArgs& a, int r, bool live, int& q0, int& n, int& keys) {
+    q0 = n = keys = 0;
+    if (live) {
+        const int s0 = a.pages.q_start[r], s1 = a.pages.q_start[r + 1];
+        q0 = s0 < 0 ? 0 : s0 < a.N ? s0 : a.N;
+        n = s1 < q0 ? 0 : (s1 < a.N ? s1 : a.N) - q0;
+        keys = keys_of(a.pages, r);
+    }
+    const int64_t rows = (int64_t)n * a.G;
+    Load l;
+    l.tiles = rows < a.rows_lo || rows > a.rows_hi ? 0 : (int)((rows + BQ - 1) / BQ);
+    int64_t most = keys;
+    if (a.window) {  // tokens of one tile see no more than this
+        const int64_t w = (int64_t)a.window * a.frame + BQ + a.frame;
+        most = w < most ? w : most;
+    }
+    l.key_tiles = (int)((most + kBK - 1) / kBK);
+    return l;
+}
+
+__device__ __forceinline__ int scan_add(int x, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
+// Key tiles of a piece: as many as make `pieces` units of all tiles' keys, `least` at least.
+template <int BQ>
+__device__ __forceinline__ int piece_tiles(const PagedAttnArgs& a, int lane) {
+    if (!a.pieces) return 0x7fffffff;
+    float all = 0.f;
+    for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
+        int q0, n, keys;
+        const Load l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
+        all += (float)l.tiles * (float)l.key_tiles;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) all += __shfl_xor(all, d);
+    const float c = ceilf(all / (float)a.pieces);
+    return c < (float)a.least ? a.least : c < 1e9f ? (int)c : 1000000000;
+}
+
+__device__ __forceinline__ int pieces_of(int key_tiles, int c) { return key_tiles <= c ? 1 : (key_tiles + c - 1) / c; }
+
+// Unit u of a key head's (WHOLE: tile u of its tiles, whatever their pieces): false if there are not so many.  total: of them.
+template <int BQ, bool WHOLE>
+__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int c, int u, int lane, Unit* out) {
+    int units_before = 0, slots_before = 0;
+    for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
+        int q0, n, keys;
+        const Load l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
+        const int pieces = pieces_of(l.key_tiles, c);
+        const int slots = l.tiles * pieces, units = WHOLE ? l.tiles : slots;
+        const int upto = scan_add(units, lane), slots_upto = WHOLE ? scan_add(slots, lane) : upto;
+        const uint64_t b = __ballot(u - units_before < upto);
+        if (b) {
+            const int at = __builtin_ctzll(b);
+            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+            out->r = r0 + at;
+            out->q0 = of(q0);
+            out->new_ = of(n);
+            out->keys = of(keys);
+            out->pieces = of(pieces);
+            const int in = u - units_before - (of(upto) - of(units)), tiles = of(l.tiles);
+            // pieces of the same keys next to each other
+            out->piece = WHOLE ? 0 : in / tiles;
+            out->tile = WHOLE ? in : in - out->piece * tiles;
+            out->slot = slots_before + of(slots_upto) - of(slots) + (WHOLE ? in : in);
+            return true;
+        }
+        units_before += __builtin_amdgcn_readlane(upto, 63);
+        slots_before += __builtin_amdgcn_readlane(slots_upto, 63);
+    }
+    return false;
+}
+template <int BQ, bool WHOLE>
+__device__ __forceinline__ int count_units(const PagedAttnArgs& a, int c, int lane) {
+    int all = 0;
+    for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
+        int q0, n, keys;
+        const Load l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
+        all += l.tiles * (WHOLE ? 1 : pieces_of(l.key_tiles, c));
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) all += __shfl_xor(all, d);
+    return __builtin_amdgcn_readfirstlane(all);
+}
+
+// The n-th of a workgroup's units: workgroups go round the eight XCDs, each of which gets a run of neighbouring units, that
+// is of the same head's keys.  -1: none left.
+__device__ __forceinline__ int64_t nth_unit(int64_t total, int n) {
+    const int64_t run = (total + 7) / 8, at = (int64_t)(blockIdx.x >> 3) + (int64_t)n * (gridDim.x >> 3);
+    if (at >= run) return -1;
+    const int64_t u = (blockIdx.x & 7) * run + at;
+    return u < total ? u : -1;
+}
+
+// Keys [first, past) that the token at place p sees of `keys`.
+__device__ __forceinline__ void seen_by(const PagedAttnArgs& a, int64_t p, int keys, int& first, int& past) {
+    first = 0;
+    past = keys;
+    if (a.frame) {
+        const int64_t f = p >= 0 ? (int64_t)div_by((uint32_t)p, a.frame_div) : -1;
+        const int64_t end = (f + 1) * a.frame;
+        past = end < keys ? (int)end : keys;
+        if (a.window) {
+            const int64_t begin = (f - a.window + 1) * a.frame;
+            first = begin < 0 ? 0 : begin < keys ? (int)begin : keys;
+        }
+    }
+}
+
+// ---- keys' rows ----
+// Lane l's key of a tile: its row's place in the cache in units of 16 bytes, and whether there is one.
+struct KeyRow {
+    uint32_t off16;
+    bool there;
+};
+__device__ __forceinline__ int entry_of(const PageArgs& p, const int32_t* table, int key, int keys) {
+    const int n = key < keys ? key : keys - 1;
+    return table[div_by((uint32_t)n, p.page)];
+}
+__device__ __forceinline__ KeyRow row_of(const PageArgs& p, int entry, int key, int keys) {
+    const int n = key < keys ? key : keys - 1;
+    const uint32_t in = (uint32_t)n - div_by((uint32_t)n, p.page) * p.page.d;
+    KeyRow k;
+    k.there = key < keys && entry >= 0 && entry < p.n_pages;
+    k.off16 = (uint32_t)entry * p.page16 + in * p.token16;
+    return k;
+}
+
+// ---- query rows ----
+__device__ __forceinline__ u32x4 load_q(const void* q, int64_t off, int type, int op) {
+    if (type == (op == OP_F16 ? DIT_F16 : DIT_BF16)) return *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(q) + off);
+    float x[8];
+    if (type == DIT_F16) {
+        const f16x8 h = *reinterpret_cast<const f16x8*>(static_cast<const uint16_t*>(q) + off);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
+    } else {
+        load8(q, off, type == DIT_F32, x);
+    }
+    return op == OP_F16 ? pack8<OP_F16>(x) : pack8<OP_BF16>(x);
+}
+
+__device__ __forceinline__ void store4(void* out, int64_t off, int type, f32x4 v) {
+    if (type == DIT_F32) *reinterpret_cast<f32x4*>(static_cast<float*>(out) + off) = v;
+    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + off) = make_uint2(pack2<OP_BF16>(v[0], v[1]), pack2<OP_BF16>(v[2], v[3]));
+}
+
+// The probabilities of a tile in which some keys are masked for some rows, times rows of V of which some hold an infinity or a
+// NaN: 0 times those is no 0, so the masked ones are left out one by one, on the vector ALU.  (Rare: such values in such a
+// tile only.)  keep: bit b of the lane's mask = its row sees key 16 (b / 4) + 4 g + b % 4 of the KEYS keys.
+template <int D, int OP, int KEYS>
+__device__ __forceinline__ void pv_one_by_one(const uint8_t* v, const uint32_t (&P)[KEYS / 8], uint32_t keep,
+                                                        f32x4 (&O)[D / 16], int i, int g) {
+#pragma unroll 1
+    for (int key = 0; key < KEYS; ++key) {
+        // the lane that holds row i's probability of this key, and where
+        const int b = 4 * (key >> 4) + (key & 3), from = ((key & 15) >> 2) * 16 + i;
+        uint32_t pair = 0;
+#pragma unroll
+        for (int w = 0; w < KEYS / 8; ++w) pair = w == (b >> 1) ? P[w] : pair;
+        pair = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)pair);
+        const uint32_t k = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)keep);
+        const uint32_t bits = (b & 1) ? pair >> 16 : pair & 0xffffu;
+        const float p = OP == OP_F16 ? (float)__builtin_bit_cast(f16x2, bits)[0] : __uint_as_float(bits << 16);
+        if (!((k >> b) & 1)) continue;
+#pragma unroll
+        for (int cb = 0; cb < D / 16; ++cb) {
+            const uint2 raw = *reinterpret_cast<const uint2*>(v + key * (2 * D) + 16 * v_slot<D>(key, 2 * cb + (g >> 1)) + 8 * (g & 1));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t u = r < 2 ? raw.x : raw.y;
+                const float x = OP == OP_F16 ? (float)__builtin_bit_cast(f16x2, u)[r & 1] : (r & 1) ? bf16_hi(u) : bf16_lo(u);
+                O[cb][r] = fmaf(p, x, O[cb][r]);
+            }
+        }
+    }
+}
+// Whether a pair of 16-bit numbers holds an infinity or a NaN.
+template <int OP>
+__device__ __forceinline__ bool pair_not_finite(uint32_t u) {
+    constexpr uint32_t e = OP == OP_F16 ? 0x7c00u : 0x7f80u;
+    return (u & e) == e || ((u >> 16) & e) == e;
+}
+
+// One wavefront's rows: 16 QB of them, and what it has of their softmax.
+template <int D, int QB>
+struct RowState {
+    f32x4 O[QB][D / 16];
+    float m[QB], l[QB];  // of the lane's row i; l: the lane's own keys
+    int first[QB], past[QB];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            m[q] = kNoScore;
+            l[q] = 0.f;
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb) O[q][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+
+// One tile of KEYS keys (64 or 32) in LDS: scores, softmax, O += P V.  `there`: bit = key's page is there; masked: some key is
+// masked for some row of the wavefront.
+template <int D, int OP, int QB, int KEYS>
+__device__ __forceinline__ void tile_step(RowState<D, QB>& st, const u32x4 (&Q)[QB][D / 32], const uint8_t* kt, uint8_t* vt,
+                                          int key0, uint64_t there, bool masked, float scale_log2, int i, int g) {
+    constexpr int NB = KEYS / 16, NKS = D / 32, NCB = D / 16;
+    f32x4 S[QB][NB];
+#pragma unroll
+    for (int q = 0; q < QB; ++q)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) S[q][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const u32x4 k = k_fragment<D>(kt, 16 * b, ks, i, g);
+#pragma unroll
+            for (int q = 0; q < QB; ++q) S[q][b] = mfma16<OP>(k, Q[q][ks], S[q][b]);
+        }
+    uint32_t keep[QB];
+    if (masked) {
+        const uint64_t mine = there >> (4 * g);
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            keep[q] = 0;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int key = key0 + 16 * b + 4 * g + r;
+                    const bool ok = ((mine >> (16 * b + r)) & 1) && key >= st.first[q] && key < st.past[q];
+                    keep[q] |= (ok ? 1u : 0u) << (4 * b + r);
+                    S[q][b][r] = ok ? S[q][b][r] : -INFINITY;
+                }
+        }
+    }
+    uint32_t P[QB][2 * NB];
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+        float mx = S[q][0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, S[q][b][r]);
+        mx = fmaxf(max_across_rows16(mx), st.m[q]);
+        const float alpha = __builtin_amdgcn_exp2f((st.m[q] - mx) * scale_log2);
+        if (__any(mx > st.m[q])) {
+            st.l[q] *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) st.O[q][cb][r] *= alpha;
+            st.m[q] = mx;
+        }
+        // (s - m) c as one fma(s, c, -m c).  -m c is rounded: by 2^-13 at most below 2^12; beyond, where it would be by more
+        // than an exponent holds, the difference is taken first.
+        float off = -mx * scale_log2;
+        if (__any(__builtin_fabsf(off) > 4096.0f)) {
+            off = 0.f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) S[q][b][r] -= mx;
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float e[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                e[r] = __builtin_amdgcn_exp2f(fmaf(S[q][b][r], scale_log2, off));
+                sum += e[r];
+            }
+            P[q][2 * b] = pack2<OP>(e[0], e[1]);
+            P[q][2 * b + 1] = pack2<OP>(e[2], e[3]);
+        }
+        st.l[q] += sum;
+    }
+    if (masked) {
+        bool bad = false;
+#pragma unroll
+        for (int m = 0; m < NB / 2; ++m)
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb) {
+                const u32x4 v = v_fragment<D>(vt, 32 * m, cb, i, g);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) bad = bad || pair_not_finite<OP>(v[w]);
+            }
+        if (__any(bad)) {
+#pragma unroll
+            for (int q = 0; q < QB; ++q) pv_one_by_one<D, OP, KEYS>(vt, P[q], keep[q], st.O[q], i, g);
+            return;
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < NB / 2; ++m)
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb) {
+            const u32x4 v = v_fragment<D>(vt, 32 * m, cb, i, g);
+#pragma unroll
+            for (int q = 0; q < QB; ++q)
+                st.O[q][cb] = mfma16<OP>(v, mk4(P[q][4 * m], P[q][4 * m + 1], P[q][4 * m + 2], P[q][4 * m + 3]), st.O[q][cb]);
+        }
+}
+
+// Query rows of a wavefront: 16 QB from `row0` of the unit's; rows past the end are the last one again, and not stored.
+struct RowPlace {
+    int token, head;  // token counted from the request's first new one
+    bool live;
+};
+__device__ __forceinline__ RowPlace place_of(const PagedAttnArgs& a, const Unit& u, int hk, int64_t row) {
+    const int64_t rows = (int64_t)u.new_ * a.G;
+    RowPlace p;
+    p.live = row < rows;
+    const uint32_t n = (uint32_t)(p.live ? row : rows - 1);
+    const uint32_t t = div_by(n, a.group);
+    p.token = (int)t;
+    p.head = hk * a.G + (int)(n - t * a.G);
+    return p;
+}
+
+template <int D, int OP, int QB>
+__device__ __forceinline__ void load_rows(const PagedAttnArgs& a, const Unit& u, int hk, int64_t row0, int i, int g,
+                                          u32x4 (&Q)[QB][D / 32], RowState<D, QB>& st) {
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+        const RowPlace p = place_of(a, u, hk, row0 + 16 * q + i);
+        const int64_t off = (int64_t)(u.q0 + p.token) * a.sq_t + (int64_t)p.head * a.sq_h + 8 * g;
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) Q[q][ks] = load_q(a.q, off + 32 * ks, a.q_type, OP);
+        seen_by(a, (int64_t)u.keys - u.new_ + p.token, u.keys, st.first[q], st.past[q]);
+    }
+}
+
+// Rows out: normalised, or (a tile in pieces) as they are with their maxima and sums.  l: summed over the row's lanes.
+template <int D, int QB>
+__device__ __forceinline__ void store_rows_of(const PagedAttnArgs& a, const Unit& u, int hk, int rows_of_tile, int row_in_tile,
+                                              int64_t row0, int i, int g, const RowState<D, QB>& st, const float (&l)[QB]) {
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+        const RowPlace p = place_of(a, u, hk, row0 + 16 * q + i);
+        if (u.pieces > 1) {
+            if (u.slot >= a.part_cap) continue;
+            const int64_t at = ((int64_t)hk * a.part_cap + u.slot) * rows_of_tile + row_in_tile + 16 * q + i;
+            float* const o = a.part_o + at * D + 4 * g;
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb) *reinterpret_cast<f32x4*>(o + 16 * cb) = st.O[q][cb];
+            if (g == 0) a.part_ml[at] = make_float2(st.m[q] * a.scale_log2, l[q]);
+            continue;
+        }
+        if (!p.live) continue;
+        const float inv = l[q] > 0.f || l[q] != l[q] ? 1.0f / l[q] : 0.f;
+        const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + 4 * g;
+#pragma unroll
+        for (int cb = 0; cb < D / 16; ++cb) {
+            f32x4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = st.O[q][cb][r] * inv;
+            store4(a.out, off + 16 * cb, a.out_type, v);
+        }
+        if (a.lse && g == 0)
+            a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (st.m[q] * a.scale_log2 + __builtin_amdgcn_logf(l[q])) * 0.6931471805599453f;
+    }
+}
+
+// Key tiles of the unit: from the first key that its first token sees to the last that its last token sees, and of those its
+// piece.
+template <int BQ>
+__device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit& u, int& begin, int& end) {
+    const int64_t rows = (int64_t)u.new_ * a.G, row0 = (int64_t)u.tile * BQ;
+    const int64_t row1 = row0 + BQ < rows ? row0 + BQ - 1 : rows - 1;
+    const int64_t place = (int64_t)u.keys - u.new_;
+    int lo, hi, none;
+    seen_by(a, place + div_by((uint32_t)row0, a.group), u.keys, lo, none);
+    seen_by(a, place + div_by((uint32_t)row1, a.group), u.keys, none, hi);
+    const int b = lo / kBK, e = hi > lo ? (hi + kBK - 1) / kBK : b;
+    begin = b + (int)((int64_t)(e - b) * u.piece / u.pieces);
+    end = b + (int)((int64_t)(e - b) * (u.piece + 1) / u.pieces);
+}
+
+// ---- few rows: each wavefront of a workgroup has keys of its own ----
+// 16 QB rows; the unit's keys go to the four wavefronts 32 at a time, each of which has LDS of its own for 32 rows of K and V.
+// Its fragments are read into registers at once, and the next keys are on their way while they are multiplied.  The four
+// results are joined in LDS at the end.
+constexpr int kFewWaves = 4;
+template <int D, int QB>
+constexpr int few_lds() { return kFewWaves * 2 * 32 * 2 * D; }
+
+template <int D, int OP, int QB>
+__global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const PagedAttnArgs a) {
+    constexpr int BQ = 16 * QB, KEYS = 32, RB = 2 * D;
+    constexpr int RPI = 64 * 16 / RB;  // rows that one load of the wavefront brings
+    __shared__ __attribute__((aligned(16))) uint8_t smem[few_lds<D, QB>()];
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint8_t* const kt = smem + wave * (2 * KEYS * RB);
+    uint8_t* const vt = kt + KEYS * RB;
+    const int c = piece_tiles<BQ>(a, lane);
+    const int per_head = count_units<BQ, false>(a, c, lane);
+    const int64_t total = (int64_t)per_head * a.Hk;
+    for (int n = 0;; ++n) {
+        const int64_t id = nth_unit(total, n);
+        if (id < 0) return;
+        const int hk = (int)(id / per_head);
+        Unit u;
+        if (!find_unit<BQ, false>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        RowState<D, QB> st;
+        u32x4 Q[QB][D / 32];
+        const int64_t row0 = (int64_t)u.tile * BQ;
+        load_rows<D, OP, QB>(a, u, hk, row0, i, g, Q, st);
+        st.clear();
+        int begin, end;
+        key_tiles_of<BQ>(a, u, begin, end);
+        const int32_t* const table = a.pages.table + (int64_t)u.r * a.pages.max_pages;
+        const uint8_t* const kc = a.k_cache + (int64_t)hk * a.pages.head16 * 16;
+        const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
+        // the wavefront's blocks of 32 keys: from b on, every kFewWaves-th
+        int b = 2 * begin + wave;
+        const int blocks = 2 * end;
+        int entry = 0;
+        uint64_t there = 0;
+        auto fetch = [&](int block) {  // its entries are there
+            const int key = KEYS * block + (lane & 31);
+            const KeyRow kr = row_of(a.pages, entry, key, u.keys);
+            there = __ballot(kr.there) & 0xffffffffull;
+#pragma unroll
+            for (int p = 0; p < KEYS / RPI; ++p) {
+                const int row = p * RPI + lane / (RB / 16), slot = lane % (RB / 16);
+                const uint32_t off = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)kr.off16);
+                if ((there >> row) & 1) {
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kc + (uint64_t)(off + k_slot<D>(row, slot)) * 16),
+                                                     (lptr_t)(kt + p * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(vc + (uint64_t)(off + v_slot<D>(row, slot)) * 16),
+                                                     (lptr_t)(vt + p * 1024), 16, 0, 0);
+                } else {
+                    *reinterpret_cast<u32x4*>(kt + p * 1024 + 16 * lane) = mk4(0, 0, 0, 0);
+                    *reinterpret_cast<u32x4*>(vt + p * 1024 + 16 * lane) = mk4(0, 0, 0, 0);
+                }
+            }
+        };
+        if (b < blocks) {
+            entry = entry_of(a.pages, table, KEYS * b + (lane & 31), u.keys);
+            fetch(b);
+            entry = entry_of(a.pages, table, KEYS * (b + kFewWaves) + (lane & 31), u.keys);
+        }
+        for (; b < blocks; b += kFewWaves) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // (its own rows: no other wavefront waits for them)
+            const int key0 = KEYS * b;
+            bool masked = there != 0xffffffffull;
+#pragma unroll
+            for (int q = 0; q < QB; ++q) masked = masked || st.first[q] > key0 || st.past[q] < key0 + KEYS;
+            tile_step<D, OP, QB, KEYS>(st, Q, kt, vt, key0, there, __any(masked), a.scale_log2, i, g);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (b + kFewWaves < blocks) {
+                fetch(b + kFewWaves);
+                entry = entry_of(a.pages, table, KEYS * (b + 2 * kFewWaves) + (lane & 31), u.keys);
+            }
+        }
+        // the four wavefronts' rows: maxima, then sums and O relative to the largest
+        float l[QB];
+        __syncthreads();
+        float2* const ml = reinterpret_cast<float2*>(smem);  // [wave][row]
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            l[q] = sum_across_rows16(st.l[q]);
+            if (g == 0) ml[wave * BQ + 16 * q + i] = make_float2(st.m[q], l[q]);
+        }
+        __syncthreads();
+        float f[QB];
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            float2 x[kFewWaves];
+            float top = kNoScore;
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) {
+                x[w] = ml[w * BQ + 16 * q + i];
+                top = fmaxf(top, x[w].x);
+            }
+            l[q] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) l[q] += x[w].y * __builtin_amdgcn_exp2f((x[w].x - top) * a.scale_log2);
+            f[q] = __builtin_amdgcn_exp2f((st.m[q] - top) * a.scale_log2);
+            st.m[q] = top;
+        }
+        // O: wavefront w > 0 leaves its own, wavefront 0 adds them up in order
+        float* const area = reinterpret_cast<float*>(smem + 1024);  // [wave - 1][lane][4]
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            // (a block of 16 rows at a time: three wavefronts' D / 16 pieces of 1 KiB)
+            if (q > 0) __syncthreads();
+#pragma unroll
+            for (int cb = 0; cb < D / 16; ++cb) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) st.O[q][cb][r] *= f[q];
+                if (wave > 0) *reinterpret_cast<f32x4*>(area + (((wave - 1) * (D / 16) + cb) * 64 + lane) * 4) = st.O[q][cb];
+            }
+            __syncthreads();
+            if (wave == 0) {
+#pragma unroll
+                for (int cb = 0; cb < D / 16; ++cb)
+#pragma unroll
+                    for (int w = 0; w < kFewWaves - 1; ++w) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(area + ((w * (D / 16) + cb) * 64 + lane) * 4);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) st.O[q][cb][r] += x[r];
+                    }
+            }
+        }
+        if (wave == 0) store_rows_of<D, QB>(a, u, hk, BQ, 0, row0, i, g, st, l);
+        __syncthreads();
+    }
+}
+
+// ---- many rows: the wavefronts of a workgroup share the keys ----
+constexpr int kBigWaves = 4, kBigQB = 2;
+static_assert(kPagedBigRows == 16 * kBigQB * kBigWaves, "rows of a workgroup");
+template <int D>
+constexpr int big_lds() { return 2 * 2 * kBK * 2 * D; }
+
+template <int D, int OP>
+__global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const PagedAttnArgs a) {
+    constexpr int NW = kBigWaves, QB = kBigQB, BQ = kPagedBigRows, RB = 2 * D, PART = kBK * RB;
+    constexpr int RPI = 64 * 16 / RB, NL = kBK / NW / RPI;  // rows a load, loads of a wavefront's 16 rows
+    extern __shared__ __attribute__((aligned(16))) uint8_t dyn[];
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = piece_tiles<BQ>(a, lane);
+    const int per_head = count_units<BQ, false>(a, c, lane);
+    const int64_t total = (int64_t)per_head * a.Hk;
+    for (int n = 0;; ++n) {
+        const int64_t id = nth_unit(total, n);
+        if (id < 0) return;
+        const int hk = (int)(id / per_head);
+        Unit u;
+        if (!find_unit<BQ, false>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        RowState<D, QB> st;
+        u32x4 Q[QB][D / 32];
+        const int64_t row0 = (int64_t)u.tile * BQ + wave * 16 * QB;
+        load_rows<D, OP, QB>(a, u, hk, row0, i, g, Q, st);
+        st.clear();
+        int begin, end;
+        key_tiles_of<BQ>(a, u, begin, end);
+        const int32_t* const table = a.pages.table + (int64_t)u.r * a.pages.max_pages;
+        const uint8_t* const kc = a.k_cache + (int64_t)hk * a.pages.head16 * 16;
+        const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
+        int entry = 0;
+        uint64_t there = 0, there_next = 0;
+        auto fetch = [&](int tile, int buf) {  // its entries are there
+            const KeyRow kr = row_of(a.pages, entry, kBK * tile + lane, u.keys);
+            there_next = __ballot(kr.there);
+            uint8_t* const kt = dyn + buf * 2 * PART;
+            uint8_t* const vt = kt + PART;
+#pragma unroll
+            for (int p = 0; p < NL; ++p) {
+                const int first = wave * (kBK / NW) + p * RPI;
+                const int row = first + lane / (RB / 16), slot = lane % (RB / 16);
+                const uint32_t off = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)kr.off16);
+                if ((there_next >> row) & 1) {
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kc + (uint64_t)(off + k_slot<D>(row, slot)) * 16),
+                                                     (lptr_t)(kt + first * RB), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(vc + (uint64_t)(off + v_slot<D>(row, slot)) * 16),
+                                                     (lptr_t)(vt + first * RB), 16, 0, 0);
+                } else {
+                    *reinterpret_cast<u32x4*>(kt + first * RB + 16 * lane) = mk4(0, 0, 0, 0);
+                    *reinterpret_cast<u32x4*>(vt + first * RB + 16 * lane) = mk4(0, 0, 0, 0);
+                }
+            }
+        };
+        int lo = 0, hi = 0x7fffffff;  // keys that every row of the wavefront sees
+        int any_lo = 0x7fffffff, any_hi = 0;
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            lo = lo > st.first[q] ? lo : st.first[q];
+            hi = hi < st.past[q] ? hi : st.past[q];
+            any_lo = any_lo < st.first[q] ? any_lo : st.first[q];
+            any_hi = any_hi > st.past[q] ? any_hi : st.past[q];
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) {
+            lo = max(lo, __shfl_xor(lo, d));
+            hi = min(hi, __shfl_xor(hi, d));
+            any_lo = min(any_lo, __shfl_xor(any_lo, d));
+            any_hi = max(any_hi, __shfl_xor(any_hi, d));
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+        any_hi = row0 < (int64_t)u.new_ * a.G ? __builtin_amdgcn_readfirstlane(any_hi) : 0;
+        if (begin < end) {
+            entry = entry_of(a.pages, table, kBK * begin + lane, u.keys);
+            fetch(begin, 0);
+            entry = entry_of(a.pages, table, kBK * (begin + 1) + lane, u.keys);
+        }
+        for (int j = begin; j < end; ++j) {
+            const int buf = (j - begin) & 1;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            there = there_next;
+            if (j + 1 < end) {
+                fetch(j + 1, buf ^ 1);
+                entry = entry_of(a.pages, table, kBK * (j + 2) + lane, u.keys);
+            }
+            const int key0 = kBK * j;
+            if (there == 0 || key0 >= any_hi || key0 + kBK <= any_lo) continue;
+            const bool masked = there != ~0ull || key0 < lo || key0 + kBK > hi;
+            tile_step<D, OP, QB, kBK>(st, Q, dyn + buf * 2 * PART, dyn + buf * 2 * PART + PART, key0, there, masked,
+                                      a.scale_log2, i, g);
+        }
+        float l[QB];
+#pragma unroll
+        for (int q = 0; q < QB; ++q) l[q] = sum_across_rows16(st.l[q]);
+        store_rows_of<D, QB>(a, u, hk, BQ, wave * 16 * QB, row0, i, g, st, l);
+        __syncthreads();
+    }
+}
+
+// ---- tiles in pieces put together ----
+// A workgroup a tile; 16 rows at a time, 16 lanes a row.
+template <int D, int BQ>
+__global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a) {
+    constexpr int CL = D / 16;  // channels a lane
+    const int lane = threadIdx.x & 63;
+    const int c = piece_tiles<BQ>(a, lane);
+    const int per_head = count_units<BQ, true>(a, c, lane);
+    const int64_t total = (int64_t)per_head * a.Hk;
+    for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
+        const int hk = (int)(id / per_head);
+        Unit u;
+        if (!find_unit<BQ, true>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        if (u.pieces < 2) continue;
+        // piece s of the tile is tiles-of-the-request slots behind piece s - 1; u.slot counts from the request's first
+        const int64_t rows = (int64_t)u.new_ * a.G;
+        const int tiles = (int)((rows + BQ - 1) / BQ);
+        for (int row = threadIdx.x >> 4; row < BQ; row += 16) {
+            const RowPlace p = place_of(a, u, hk, (int64_t)u.tile * BQ + row);
+            if (!p.live) continue;
+            const int ch = (threadIdx.x & 15) * CL;
+            float top = -INFINITY, sum = 0.f, o[CL];
+            auto at = [&](int s) { return ((int64_t)hk * a.part_cap + u.slot + (int64_t)s * tiles) * BQ + row; };
+            const int pieces = u.slot + (u.pieces - 1) * tiles < a.part_cap ? u.pieces : 0;
+            for (int s = 0; s < pieces; ++s) top = fmaxf(top, a.part_ml[at(s)].x);
+#pragma unroll
+            for (int k = 0; k < CL; ++k) o[k] = 0.f;
+            for (int s = 0; s < pieces; ++s) {
+                const float2 ml = a.part_ml[at(s)];
+                const float w = __builtin_amdgcn_exp2f(ml.x - top);
+                sum = fmaf(ml.y, w, sum);
+                const f32x4* const src = reinterpret_cast<const f32x4*>(a.part_o + at(s) * D + ch);
+#pragma unroll
+                for (int k = 0; k < CL; k += 4) {
+                    const f32x4 x = src[k / 4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[k + r] = fmaf(x[r], w, o[k + r]);
+                }
+            }
+            const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+            const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + ch;
+#pragma unroll
+            for (int k = 0; k < CL; k += 4)
+                store4(a.out, off + k, a.out_type, f32x4{o[k] * inv, o[k + 1] * inv, o[k + 2] * inv, o[k + 3] * inv});
+            if (a.lse && (threadIdx.x & 15) == 0)
+                a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+        }
+    }
+}
+
+template <int D, int OP, int QB>
+hipError_t launch_few(const PagedAttnArgs& a, int units, hipStream_t s) {
+    hipLaunchKernelGGL((attn_paged_few_kernel<D, OP, QB>), dim3((units + 7) / 8 * 8), dim3(64 * kFewWaves), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.pieces) return e;
+    hipLaunchKernelGGL((attn_paged_join_kernel<D, 16 * QB>), dim3(units), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+template <int D, int OP>
+hipError_t launch_big(const PagedAttnArgs& a, int units, hipStream_t s) {
+    static std::atomic<uint64_t> done{0};
+    const auto kern = attn_paged_big_kernel<D, OP>;
+    hipError_t e = allow_dynamic_lds(kern, big_lds<D>(), done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kBigWaves), big_lds<D>(), s, a);
+    e = hipGetLastError();
+    if (e != hipSuccess || !a.pieces) return e;
+    hipLaunchKernelGGL((attn_paged_join_kernel<D, kPagedBigRows>), dim3(units), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int D, int OP>
+hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_t* ws, hipStream_t s) {
+    PagedAttnArgs a = args;
+    auto parts = [&](int pieces, int cap, int rows) {
+        a.pieces = pieces;
+        a.part_cap = cap;
+        a.part_o = reinterpret_cast<float*>(ws);
+        a.part_ml = reinterpret_cast<float2*>(ws + (size_t)a.Hk * cap * rows * D * sizeof(float));
+    };
+    hipError_t e = hipSuccess;
+    if (plan.few) {
+        a.rows_lo = 1;
+        a.rows_hi = plan.big ? 16 * plan.few_qb : 0x7fffffff;
+        a.least = 2;
+        parts(plan.few_pieces, plan.few_cap, 16 * plan.few_qb);
+        e = plan.few_qb == 1 ? launch_few<D, OP, 1>(a, plan.few_units, s) : launch_few<D, OP, 2>(a, plan.few_units, s);
+    }
+    if (e == hipSuccess && plan.big) {
+        a.rows_lo = plan.few ? 16 * plan.few_qb + 1 : 1;
+        a.rows_hi = 0x7fffffff;
+        a.least = 4;
+        ws += plan.few_bytes;
+        parts(plan.big_pieces, plan.big_cap, kPagedBigRows);
+        e = launch_big<D, OP>(a, plan.big_units, s);
+    }
+    return e;
+}
+
+}  // namespace
+
+PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int max_q) {
+    PagedPlan p{};
+    const int64_t G = H / Hk, rows = (int64_t)N * G, least = N < R ? N : R;
+    const int64_t most_q = max_q > 0 && max_q < N ? max_q : N;  // new tokens of a request
+    p.few_qb = most_q * G > 16 ? 2 : 1;
+    const bool uniform = most_q * least <= 2 * (int64_t)N;  // few requests have far fewer new tokens than that
+    p.few = most_q * G <= 32 || !uniform;
+    p.big = most_q * G > 32;
+    const int64_t key_tiles = (max_keys + kBK - 1) / kBK;
+    // tiles of a key head, at most: whatever q_start says, and what is left over of each request
+    auto layout = [&](int BQ, int wanted, int slack, int& units, int& pieces, int& cap, size_t& bytes) {
+        const int64_t tiles = (rows + least * (BQ - 1)) / BQ;
+        const int64_t per_head = (wanted + Hk - 1) / Hk;
+        if (tiles * Hk < slack && key_tiles > 4) {
+            pieces = (int)per_head;
+            cap = (int)(per_head + tiles);
+            bytes = (size_t)Hk * cap * BQ * (D * sizeof(float) + sizeof(float2));
+            bytes = (bytes + 255) / 256 * 256;
+            units = Hk * cap;
+        } else {
+            units = (int)(tiles * Hk < 65536 ? tiles * Hk : 65536);
+        }
+    };
+    if (p.few) layout(16 * p.few_qb, 4 * kCUs, 2 * kCUs, p.few_units, p.few_pieces, p.few_cap, p.few_bytes);
+    if (p.big) layout(kPagedBigRows, 2 * kCUs, 2 * kCUs, p.big_units, p.big_pieces, p.big_cap, p.big_bytes);
+    return p;
+}
+
+hipError_t launch_attn_paged(const PagedAttnArgs& a, const PagedPlan& plan, int D, int op, uint8_t* workspace, hipStream_t s) {
+    if (D == 128) return op == OP_F16 ? launch_paged<128, OP_F16>(a, plan, workspace, s) : launch_paged<128, OP_BF16>(a, plan, workspace, s);
+    return op == OP_F16 ? launch_paged<64, OP_F16>(a, plan, workspace, s) : launch_paged<64, OP_BF16>(a, plan, workspace, s);
+}
+
+}  // namespace dit
