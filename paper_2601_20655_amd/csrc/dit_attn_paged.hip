@@ -25,32 +25,40 @@ typedef __attribute__((address_space(3))) s16x4* ltr_t;
 constexpr float kNoScore = -1e30f;  // running maximum of a row that has none (finite: differences stay numbers)
 
 // ---- rows of K and V in LDS ----
-// A row's 16-byte pieces lie in an order of the row's own, so that a fragment's read takes each bank once: K fragments read one
-// piece of 16 rows, V fragments two neighbouring pieces of 8 rows (twice).  global_load_lds fills LDS in lane order: the order
-// is in which piece a lane fetches.
+// A wavefront-wide load brings 1 KiB: 4 rows of 128 channels or 8 of 64, in lane order.  So that a fragment's read takes each
+// bank once, a row's 16-byte pieces lie in an order of the row's own (the order is in which piece a lane fetches), and each
+// KiB a little past the one before it: K fragments read one piece of 16 rows, V fragments two neighbouring pieces of 8
+// rows (twice).  Orders that exchange pieces among four neighbours (K) or pairs among four (V) leave the rest of a fragment's place to the
+// instruction's own offset: one address register for all of K's fragments, four for V's.
 template <int D>
-__device__ __forceinline__ int k_slot(int row, int piece) {
-    return D == 128 ? piece ^ (row & 15) : piece ^ ((row >> 1) & 7);
-}
-template <int D>
-__device__ __forceinline__ int v_slot(int row, int piece) {
-    return D == 128 ? piece ^ ((row & 7) << 1) : piece ^ (((row >> 1) & 3) << 1);
-}
+struct Rows {
+    static constexpr int RB = 2 * D;            // bytes of a row
+    static constexpr int PPR = RB / 16;         // pieces of a row
+    static constexpr int RPL = 1024 / RB;       // rows of a load
+    static constexpr int KG = 1024 + 64, VG = D == 128 ? 1024 + 128 : 1024;  // from a load's rows to the next one's
+    static constexpr int k_bytes(int rows) { return rows / RPL * KG; }
+    static constexpr int v_bytes(int rows) { return rows / RPL * VG; }
+    // which piece the lane with place `slot` of row `row` (of a load's) fetches
+    static __device__ __forceinline__ int k_piece(int row, int slot) { return slot ^ (D == 128 ? row & 3 : (row >> 1) & 3); }
+    static __device__ __forceinline__ int v_piece(int row, int slot) { return slot ^ (D == 128 ? (row & 3) << 1 : ((row >> 1) & 3) << 1); }
+    // where piece `piece` of row `row` lies
+    static __device__ __forceinline__ int k_at(int row, int piece) { return row / RPL * KG + row % RPL * RB + 16 * k_piece(row % RPL, piece); }
+    static __device__ __forceinline__ int v_at(int row, int piece) { return row / RPL * VG + row % RPL * RB + 16 * v_piece(row % RPL, piece); }
+};
 
 // Operand of 16 keys (rows key0 .. +15), channels 32 ks .. +31: the lane's key i, channels 8g .. +7.
 template <int D>
 __device__ __forceinline__ u32x4 k_fragment(const uint8_t* k, int key0, int ks, int i, int g) {
-    const int row = key0 + i;
-    return *reinterpret_cast<const u32x4*>(k + row * (2 * D) + 16 * k_slot<D>(row, 4 * ks + g));
+    return *reinterpret_cast<const u32x4*>(k + Rows<D>::k_at(i, g) + key0 / Rows<D>::RPL * Rows<D>::KG + 64 * ks);
 }
 // Operand of 16 channels (16 cb .. +15) and 32 keys (rows key0 .. +31): the lane's channel i, keys 4g .. +3 and 16 + 4g .. +3.
 template <int D>
 __device__ __forceinline__ u32x4 v_fragment(uint8_t* v, int key0, int cb, int i, int g) {
     uint2 h[2];
+    const int at = Rows<D>::v_at(4 * g + (i >> 2), 2 * (cb & 3) + ((i & 3) >> 1)) + 8 * (i & 1);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        const int row = key0 + 16 * b + 4 * g + (i >> 2);
-        uint8_t* const p = v + row * (2 * D) + 16 * v_slot<D>(row, 2 * cb + ((i & 3) >> 1)) + 8 * (i & 1);
+        uint8_t* const p = v + at + (key0 + 16 * b) / Rows<D>::RPL * Rows<D>::VG + (cb >> 2) * 128;
         h[b] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr_t)p));
     }
     return mk4(h[0].x, h[0].y, h[1].x, h[1].y);
@@ -226,30 +234,29 @@ __device__ __forceinline__ void store4(void* out, int64_t off, int type, f32x4 v
 
 // The probabilities of a tile in which some keys are masked for some rows, times rows of V of which some hold an infinity or a
 // NaN: 0 times those is no 0, so the masked ones are left out one by one, on the vector ALU.  (Rare: such values in such a
-// tile only.)  keep: bit b of the lane's mask = its row sees key 16 (b / 4) + 4 g + b % 4 of the KEYS keys.
-template <int D, int OP, int KEYS>
-__device__ __forceinline__ void pv_one_by_one(const uint8_t* v, const uint32_t (&P)[KEYS / 8], uint32_t keep,
-                                                        f32x4 (&O)[D / 16], int i, int g) {
+// tile only.)  keep: bit b of the lane's mask = its row sees key 16 (b / 4) + 4 g + b % 4 of the 32.
+template <int D, int OP, class Acc>
+__device__ __forceinline__ void pv_one_by_one(const uint8_t* v, const uint32_t (&P)[4], uint32_t keep, Acc&& O, int i, int g) {
 #pragma unroll 1
-    for (int key = 0; key < KEYS; ++key) {
+    for (int key = 0; key < 32; ++key) {
         // the lane that holds row i's probability of this key, and where
         const int b = 4 * (key >> 4) + (key & 3), from = ((key & 15) >> 2) * 16 + i;
-        uint32_t pair = 0;
+        uint32_t pair = P[0];
 #pragma unroll
-        for (int w = 0; w < KEYS / 8; ++w) pair = w == (b >> 1) ? P[w] : pair;
+        for (int w = 1; w < 4; ++w) pair = w == (b >> 1) ? P[w] : pair;
         pair = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)pair);
         const uint32_t k = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)keep);
         const uint32_t bits = (b & 1) ? pair >> 16 : pair & 0xffffu;
         const float p = OP == OP_F16 ? (float)__builtin_bit_cast(f16x2, bits)[0] : __uint_as_float(bits << 16);
-        if (!((k >> b) & 1)) continue;
+        const bool ok = (k >> b) & 1;
 #pragma unroll
         for (int cb = 0; cb < D / 16; ++cb) {
-            const uint2 raw = *reinterpret_cast<const uint2*>(v + key * (2 * D) + 16 * v_slot<D>(key, 2 * cb + (g >> 1)) + 8 * (g & 1));
+            const uint2 raw = *reinterpret_cast<const uint2*>(v + Rows<D>::v_at(key, 2 * cb + (g >> 1)) + 8 * (g & 1));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const uint32_t u = r < 2 ? raw.x : raw.y;
                 const float x = OP == OP_F16 ? (float)__builtin_bit_cast(f16x2, u)[r & 1] : (r & 1) ? bf16_hi(u) : bf16_lo(u);
-                O[cb][r] = fmaf(p, x, O[cb][r]);
+                O(cb, r, [&](float o) { return ok ? fmaf(p, x, o) : o; });
             }
         }
     }
@@ -314,6 +321,7 @@ __device__ __forceinline__ void tile_step(RowState<D, QB>& st, const u32x4 (&Q)[
                 }
         }
     }
+    static_assert(KEYS == 32, "the words of 32 keys");
     uint32_t P[QB][2 * NB];
 #pragma unroll
     for (int q = 0; q < QB; ++q) {
@@ -368,7 +376,9 @@ __device__ __forceinline__ void tile_step(RowState<D, QB>& st, const u32x4 (&Q)[
             }
         if (__any(bad)) {
 #pragma unroll
-            for (int q = 0; q < QB; ++q) pv_one_by_one<D, OP, KEYS>(vt, P[q], keep[q], st.O[q], i, g);
+            for (int q = 0; q < QB; ++q)
+                pv_one_by_one<D, OP>(vt, P[q], keep[q], [&](int cb, int r, auto&& add) { st.O[q][cb][r] = add(st.O[q][cb][r]); },
+                                           i, g);
             return;
         }
     }
@@ -464,17 +474,17 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
 // results are joined in LDS at the end.
 constexpr int kFewWaves = 4;
 template <int D, int QB>
-constexpr int few_lds() { return kFewWaves * 2 * 32 * 2 * D; }
+constexpr int few_lds() { return kFewWaves * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
 
 template <int D, int OP, int QB>
 __global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const PagedAttnArgs a) {
-    constexpr int BQ = 16 * QB, KEYS = 32, RB = 2 * D;
-    constexpr int RPI = 64 * 16 / RB;  // rows that one load of the wavefront brings
-    __shared__ __attribute__((aligned(16))) uint8_t smem[few_lds<D, QB>()];
+    using R = Rows<D>;
+    constexpr int BQ = 16 * QB, KEYS = 32, RPI = R::RPL;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint8_t* const kt = smem + wave * (2 * KEYS * RB);
-    uint8_t* const vt = kt + KEYS * RB;
+    uint8_t* const kt = smem + wave * (Rows<D>::k_bytes(KEYS) + Rows<D>::v_bytes(KEYS));
+    uint8_t* const vt = kt + Rows<D>::k_bytes(KEYS);
     const int c = piece_tiles<BQ>(a, lane);
     const int per_head = count_units<BQ, false>(a, c, lane);
     const int64_t total = (int64_t)per_head * a.Hk;
@@ -505,16 +515,16 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const Pa
             there = __ballot(kr.there) & 0xffffffffull;
 #pragma unroll
             for (int p = 0; p < KEYS / RPI; ++p) {
-                const int row = p * RPI + lane / (RB / 16), slot = lane % (RB / 16);
+                const int in = lane / R::PPR, slot = lane % R::PPR, row = p * RPI + in;
                 const uint32_t off = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)kr.off16);
                 if ((there >> row) & 1) {
-                    __builtin_amdgcn_global_load_lds((gptr_t)(kc + (uint64_t)(off + k_slot<D>(row, slot)) * 16),
-                                                     (lptr_t)(kt + p * 1024), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)(vc + (uint64_t)(off + v_slot<D>(row, slot)) * 16),
-                                                     (lptr_t)(vt + p * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(kc + (uint64_t)(off + R::k_piece(in, slot)) * 16),
+                                                     (lptr_t)(kt + p * R::KG), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((gptr_t)(vc + (uint64_t)(off + R::v_piece(in, slot)) * 16),
+                                                     (lptr_t)(vt + p * R::VG), 16, 0, 0);
                 } else {
-                    *reinterpret_cast<u32x4*>(kt + p * 1024 + 16 * lane) = mk4(0, 0, 0, 0);
-                    *reinterpret_cast<u32x4*>(vt + p * 1024 + 16 * lane) = mk4(0, 0, 0, 0);
+                    *reinterpret_cast<u32x4*>(kt + p * R::KG + 16 * lane) = mk4(0, 0, 0, 0);
+                    *reinterpret_cast<u32x4*>(vt + p * R::VG + 16 * lane) = mk4(0, 0, 0, 0);
                 }
             }
         };
@@ -592,104 +602,366 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const Pa
 }
 
 // ---- many rows: the wavefronts of a workgroup share the keys ----
+// 32 rows a wavefront, 128 a workgroup, two workgroups a compute unit.  Software-pipelined in halves of a tile, 32 keys: while the
+// matrix cores work on a half's scores the vector ALU takes the exponentials of the half before it, and while they multiply
+// those with V it takes the maxima of the new scores.  So a half's scores are needed one half ahead of its V, and a turn of the
+// loop, which multiplies V of tile j, takes K rows 32 keys on: K(j) in LDS is rows 64 j + 32 .. 64 j + 95.  K(j + 1) and V(j + 1) are
+// on their way meanwhile.  A row's maximum is raised only where a score tops it by more than 2^8 (exponents stay far from their
+// ends, and what divides the row takes it out again).
 constexpr int kBigWaves = 4, kBigQB = 2;
 static_assert(kPagedBigRows == 16 * kBigQB * kBigWaves, "rows of a workgroup");
 template <int D>
-constexpr int big_lds() { return 2 * 2 * kBK * 2 * D; }
+constexpr int big_lds() { return 2 * (Rows<D>::k_bytes(kBK) + Rows<D>::v_bytes(kBK)); }
 
 template <int D, int OP>
 __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const PagedAttnArgs a) {
-    constexpr int NW = kBigWaves, QB = kBigQB, BQ = kPagedBigRows, RB = 2 * D, PART = kBK * RB;
-    constexpr int RPI = 64 * 16 / RB, NL = kBK / NW / RPI;  // rows a load, loads of a wavefront's 16 rows
+    using R = Rows<D>;
+    constexpr int NW = kBigWaves, QB = kBigQB, BQ = kPagedBigRows;
+    constexpr int RPI = R::RPL, NL = kBK / NW / RPI;  // rows a load, loads of a wavefront's 16 rows
+    constexpr int NKS = D / 32, NCB = D / 16, NOG = NCB / 4, NKF = 2 * NKS;
+    constexpr int LA = 4;        // fragments are read from LDS so many ahead of their products
+    constexpr int NCH = 4 * QB;  // slices of two scores
+    constexpr int PRE = 2;       // exponentials run so many slices ahead of their rounding
+    static_assert(LA <= NKF && LA <= NCB && PRE >= NCH / NKF, "look-ahead within a half");
     extern __shared__ __attribute__((aligned(16))) uint8_t dyn[];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = piece_tiles<BQ>(a, lane);
     const int per_head = count_units<BQ, false>(a, c, lane);
     const int64_t total = (int64_t)per_head * a.Hk;
+    const float scale = a.scale_log2, thr = kRescaleThr / scale;
+    // K buffers 0 and 1, then V's
+    auto kbuf = [&](int b) { return dyn + b * R::k_bytes(kBK); };
+    auto vbuf = [&](int b) { return dyn + 2 * R::k_bytes(kBK) + b * R::v_bytes(kBK); };
+    // (In what runs for masked tiles only, all that hangs on the lane's number is worked out from one that the compiler cannot
+    // see through: left to itself it works it out ahead of the loop, and then has no registers for the loop.)
+    auto opaque_lane = [&]() {
+        int x = lane;
+        asm volatile("" : "+v"(x));
+        return x;
+    };
     for (int n = 0;; ++n) {
         const int64_t id = nth_unit(total, n);
         if (id < 0) return;
         const int hk = (int)(id / per_head);
         Unit u;
         if (!find_unit<BQ, false>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
-        RowState<D, QB> st;
-        u32x4 Q[QB][D / 32];
-        const int64_t row0 = (int64_t)u.tile * BQ + wave * 16 * QB;
-        load_rows<D, OP, QB>(a, u, hk, row0, i, g, Q, st);
-        st.clear();
-        int begin, end;
-        key_tiles_of<BQ>(a, u, begin, end);
-        const int32_t* const table = a.pages.table + (int64_t)u.r * a.pages.max_pages;
-        const uint8_t* const kc = a.k_cache + (int64_t)hk * a.pages.head16 * 16;
-        const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
-        int entry = 0;
-        uint64_t there = 0, there_next = 0;
-        auto fetch = [&](int tile, int buf) {  // its entries are there
-            const KeyRow kr = row_of(a.pages, entry, kBK * tile + lane, u.keys);
-            there_next = __ballot(kr.there);
-            uint8_t* const kt = dyn + buf * 2 * PART;
-            uint8_t* const vt = kt + PART;
-#pragma unroll
-            for (int p = 0; p < NL; ++p) {
-                const int first = wave * (kBK / NW) + p * RPI;
-                const int row = first + lane / (RB / 16), slot = lane % (RB / 16);
-                const uint32_t off = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)kr.off16);
-                if ((there_next >> row) & 1) {
-                    __builtin_amdgcn_global_load_lds((gptr_t)(kc + (uint64_t)(off + k_slot<D>(row, slot)) * 16),
-                                                     (lptr_t)(kt + first * RB), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)(vc + (uint64_t)(off + v_slot<D>(row, slot)) * 16),
-                                                     (lptr_t)(vt + first * RB), 16, 0, 0);
-                } else {
-                    *reinterpret_cast<u32x4*>(kt + first * RB + 16 * lane) = mk4(0, 0, 0, 0);
-                    *reinterpret_cast<u32x4*>(vt + first * RB + 16 * lane) = mk4(0, 0, 0, 0);
-                }
-            }
-        };
+        u32x4 Q[QB][NKS];
+        f32x16 O[NOG][QB], S0, S1;  // scores: quarter 2 q + kb = row block q, keys 16 kb .. of the half
+        float m[QB], l[QB], off[QB];
         int lo = 0, hi = 0x7fffffff;  // keys that every row of the wavefront sees
-        int any_lo = 0x7fffffff, any_hi = 0;
+        const int64_t row0 = (int64_t)u.tile * BQ + wave * 16 * QB;
+        {
+            RowState<D, QB> st;
+            load_rows<D, OP, QB>(a, u, hk, row0, i, g, Q, st);
 #pragma unroll
-        for (int q = 0; q < QB; ++q) {
-            lo = lo > st.first[q] ? lo : st.first[q];
-            hi = hi < st.past[q] ? hi : st.past[q];
-            any_lo = any_lo < st.first[q] ? any_lo : st.first[q];
-            any_hi = any_hi > st.past[q] ? any_hi : st.past[q];
+            for (int q = 0; q < QB; ++q) {
+                lo = max(lo, st.first[q]);
+                hi = min(hi, st.past[q]);
+                m[q] = kNoScore;
+                off[q] = -kNoScore * scale;
+                l[q] = 0.f;
+#pragma unroll
+                for (int og = 0; og < NOG; ++og)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) O[og][q][r] = 0.f;
+            }
         }
 #pragma unroll
         for (int d = 8; d > 0; d >>= 1) {
             lo = max(lo, __shfl_xor(lo, d));
             hi = min(hi, __shfl_xor(hi, d));
-            any_lo = min(any_lo, __shfl_xor(any_lo, d));
-            any_hi = max(any_hi, __shfl_xor(any_hi, d));
         }
         lo = __builtin_amdgcn_readfirstlane(lo);
         hi = __builtin_amdgcn_readfirstlane(hi);
-        any_lo = __builtin_amdgcn_readfirstlane(any_lo);
-        any_hi = row0 < (int64_t)u.new_ * a.G ? __builtin_amdgcn_readfirstlane(any_hi) : 0;
-        if (begin < end) {
-            entry = entry_of(a.pages, table, kBK * begin + lane, u.keys);
-            fetch(begin, 0);
-            entry = entry_of(a.pages, table, kBK * (begin + 1) + lane, u.keys);
-        }
-        for (int j = begin; j < end; ++j) {
-            const int buf = (j - begin) & 1;
+        int begin, end;
+        key_tiles_of<BQ>(a, u, begin, end);
+        const int32_t* const table = a.pages.table + (int64_t)u.r * a.pages.max_pages;
+        const uint8_t* const kc = a.k_cache + (int64_t)hk * a.pages.head16 * 16;
+        const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
+
+        // ---- tiles: rows' places are worked out ahead by lane l for row l, for all wavefronts alike ----
+        // of two tiles that were located ahead of their fetch: which of their keys are there, and where row `lane` lies
+        uint64_t there_a = 0, there_b = 0;
+        uint32_t off_a = 0, off_b = 0;
+        int entry = 0;  // of row `lane` of the tile behind them
+        // the tile behind the two (its entries are there); the entries of the one behind it are asked for
+        auto locate = [&](int tile) {
+            there_a = there_b;
+            off_a = off_b;
+            const KeyRow kr = row_of(a.pages, entry, kBK * tile + lane, u.keys);
+            there_b = __ballot(kr.there);
+            off_b = kr.off16;
+            entry = entry_of(a.pages, table, kBK * (tile + 1) + lane, u.keys);
+        };
+        // this wavefront's 16 rows of a part; row r of it is where lane (r + turn) % 64 says
+        auto fetch_part = [&](const uint8_t* cache, uint8_t* buf, uint64_t there, uint32_t off16, int turn, bool v, auto whole) {
+            const int row_l = lane / R::PPR, slot_l = lane % R::PPR;
+            const uint8_t* const src = cache + 16 * (v ? R::v_piece(row_l, slot_l) : R::k_piece(row_l, slot_l));
+            uint8_t* const dst = buf + wave * NL * (v ? R::VG : R::KG);
+#pragma unroll
+            for (int p = 0; p < NL; ++p) {
+                const int from = (16 * wave + p * RPI + row_l + turn) & 63;
+                const uint32_t at = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)off16);
+                uint8_t* const to = dst + p * (v ? R::VG : R::KG);
+                if (whole || ((there >> from) & 1))
+                    __builtin_amdgcn_global_load_lds((gptr_t)(src + (uint64_t)at * 16), (lptr_t)to, 16, 0, 0);
+                else
+                    *reinterpret_cast<u32x4*>(to + 16 * lane) = mk4(0, 0, 0, 0);
+            }
+        };
+        // K and V of the first located tile's turn: V's rows are the tile's, K's its second half and the first of the next one
+        constexpr uint64_t kLow = 0xffffffffull;
+        auto fetch = [&](int b, auto whole) {
+            fetch_part(kc, kbuf(b), (there_a & ~kLow) | (there_b & kLow), lane < 32 ? off_b : off_a, 32, false, whole);
+            fetch_part(vc, vbuf(b), there_a, off_a, 0, true, whole);
+        };
+        auto landed = [&]() {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
-            there = there_next;
-            if (j + 1 < end) {
-                fetch(j + 1, buf ^ 1);
-                entry = entry_of(a.pages, table, kBK * (j + 2) + lane, u.keys);
-            }
-            const int key0 = kBK * j;
-            if (there == 0 || key0 >= any_hi || key0 + kBK <= any_lo) continue;
-            const bool masked = there != ~0ull || key0 < lo || key0 + kBK > hi;
-            tile_step<D, OP, QB, kBK>(st, Q, dyn + buf * 2 * PART, dyn + buf * 2 * PART + PART, key0, there, masked,
-                                      a.scale_log2, i, g);
-        }
-        float l[QB];
+        };
+
+        auto is_masked = [&](int tile, uint64_t there) { return there != ~0ull || kBK * tile < lo || kBK * tile + kBK > hi; };
+        // bit 4 kb + r: the lane's row q sees key key0 + 16 kb + 4 g + r; there: bits of the half's keys
+        auto keep_of = [&](int q, int key0, uint32_t there) {
+            const int ln = opaque_lane(), g = ln >> 4;
+            int first, past;
+            seen_by(a, (int64_t)u.keys - u.new_ + place_of(a, u, hk, row0 + 16 * q + (ln & 15)).token, u.keys, first, past);
+            const uint32_t mine = there >> (4 * g);
+            uint32_t k = 0;
 #pragma unroll
-        for (int q = 0; q < QB; ++q) l[q] = sum_across_rows16(st.l[q]);
-        store_rows_of<D, QB>(a, u, hk, BQ, wave * 16 * QB, row0, i, g, st, l);
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int key = key0 + 16 * kb + 4 * g + r;
+                    k |= (((mine >> (16 * kb + r)) & 1) && key >= first && key < past ? 1u : 0u) << (4 * kb + r);
+                }
+            return k;
+        };
+        bool far = false;  // a row's maximum is too large for (s - m) c in one fma (tile_step)
+        auto raise = [&](const f32x16& S) {
+            far = false;
+#pragma unroll
+            for (int q = 0; q < QB; ++q) {
+                float mx = S[8 * q];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, S[8 * q + e]);
+                mx = max_across_rows16(mx);
+                const float to = mx > m[q] + thr ? mx : m[q];
+                const float alpha = __builtin_amdgcn_exp2f((m[q] - to) * scale);
+                m[q] = to;
+                off[q] = -to * scale;
+                l[q] *= alpha;
+                far = far || (to != kNoScore && __builtin_fabsf(off[q]) > 4096.0f);
+#pragma unroll
+                for (int og = 0; og < NOG; ++og)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) O[og][q][r] *= alpha;
+            }
+            far = __any(far);
+        };
+        // slice x = (q, w): word w of the operand of the half's keys for row block q
+        auto exp_slice = [&](f32x16& S, int x) {
+            const int q = x / 4, e = 2 * x;
+            S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], scale, off[q]));
+            S[e + 1] = __builtin_amdgcn_exp2f(fmaf(S[e + 1], scale, off[q]));
+        };
+        auto pack_slice = [&](f32x16& S, uint32_t (&P)[QB][4], float (&sum)[QB][2], int x) {
+            const int q = x / 4, e = 2 * x;
+            P[q][x % 4] = pack2<OP>(S[e], S[e + 1]);
+            sum[q][0] += S[e];
+            sum[q][1] += S[e + 1];
+        };
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        auto score = [&](u32x4 k, int f, int q, f32x16& S) {
+            const int ks = f >> 1, kb = f & 1;
+            S = ks == 0 ? mfma16_q_init<OP>(k, Q[q][ks], zero, S, 2 * q + kb) : mfma16_q<OP>(k, Q[q][ks], S, 2 * q + kb);
+        };
+        auto product = [&](u32x4 v, const uint32_t (&P)[QB][4], int cb, int q) {
+            O[cb / 4][q] = mfma16_q<OP>(v, mk4(P[q][0], P[q][1], P[q][2], P[q][3]), O[cb / 4][q], cb % 4);
+        };
+
+        // One half (its scores in Sc) and the next one's scores (into Sn), no key of either masked for any row.  kn: the next one's
+        // rows of K, vb: this one's of V
+        auto plain_half = [&](f32x16& Sc, f32x16& Sn, const uint8_t* kn, uint8_t* vb) __attribute__((always_inline)) {
+            u32x4 kf[NKF], vf[NCB];
+            auto k_frag = [&](int f) { return k_fragment<D>(kn, 16 * (f & 1), f >> 1, i, g); };
+            auto v_frag = [&](int v) { return v_fragment<D>(vb, 0, v, i, g); };
+#pragma unroll
+            for (int f = 0; f < LA; ++f) kf[f] = k_frag(f);
+            uint32_t P[QB][4];
+            float sum[QB][2];
+#pragma unroll
+            for (int q = 0; q < QB; ++q) sum[q][0] = sum[q][1] = 0.f;
+#pragma unroll
+            for (int x = 0; x < PRE; ++x) exp_slice(Sc, x);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int f = 0; f < NKF; ++f) {
+                if (f + LA < NKF) kf[f + LA] = k_frag(f + LA);
+                if (f >= NKF - LA) vf[f - (NKF - LA)] = v_frag(f - (NKF - LA));
+                score(kf[f], f, 0, Sn);
+#pragma unroll
+                for (int x = f * NCH / NKF; x < (f + 1) * NCH / NKF; ++x)
+                    if (x + PRE < NCH) exp_slice(Sc, x + PRE);
+                __builtin_amdgcn_sched_barrier(0);
+                score(kf[f], f, 1, Sn);
+#pragma unroll
+                for (int x = f * NCH / NKF; x < (f + 1) * NCH / NKF; ++x) pack_slice(Sc, P, sum, x);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int q = 0; q < QB; ++q) l[q] += sum[q][0] + sum[q][1];
+            float mx[QB] = {-INFINITY, -INFINITY};
+            auto max_slice = [&](int x) { mx[x & 1] = max3(mx[x & 1], Sn[8 * (x & 1) + 2 * (x >> 1)], Sn[8 * (x & 1) + 2 * (x >> 1) + 1]); };
+#pragma unroll
+            for (int v = 0; v < NCB; ++v) {
+                if (v + LA < NCB) vf[v + LA] = v_frag(v + LA);
+                product(vf[v], P, v, 0);
+                if (v >= 1) {
+#pragma unroll
+                    for (int x = (v - 1) * NCH / NCB; x < v * NCH / NCB; ++x) max_slice(x);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                product(vf[v], P, v, 1);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int x = (NCB - 1) * NCH / NCB; x < NCH; ++x) max_slice(x);
+            if (__any(mx[0] > m[0] + thr || mx[1] > m[1] + thr)) raise(Sn);
+        };
+
+        // One half, whatever is masked of it, and the next one's scores (if there is one) into the same registers.
+        auto any_half = [&](f32x16& S, bool masked, int key0, uint32_t there, uint8_t* vb, bool more, bool masked_next, uint32_t there_next,
+                            const uint8_t* kn) __attribute__((always_inline)) {
+            const int ln = opaque_lane(), i = ln & 15, g = ln >> 4;
+            if (far) {
+#pragma unroll
+                for (int q = 0; q < QB; ++q) {
+                    const bool some = m[q] != kNoScore;
+                    off[q] = some ? 0.f : off[q];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) S[8 * q + e] -= some ? m[q] : 0.f;
+                }
+            }
+            uint32_t P[QB][4];
+            float sum[QB][2];
+#pragma unroll
+            for (int q = 0; q < QB; ++q) sum[q][0] = sum[q][1] = 0.f;
+#pragma unroll
+            for (int x = 0; x < NCH; ++x) exp_slice(S, x);
+#pragma unroll
+            for (int x = 0; x < NCH; ++x) pack_slice(S, P, sum, x);
+#pragma unroll
+            for (int q = 0; q < QB; ++q) l[q] += sum[q][0] + sum[q][1];
+            bool bad = false;
+            if (masked) {
+#pragma unroll
+                for (int v = 0; v < NCB; ++v) {
+                    const u32x4 x = v_fragment<D>(vb, 0, v, i, g);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) bad = bad || pair_not_finite<OP>(x[w]);
+                }
+            }
+            if (__any(bad)) {
+#pragma unroll
+                for (int q = 0; q < QB; ++q)
+                    pv_one_by_one<D, OP>(vb, P[q], keep_of(q, key0, there), [&](int cb, int r, auto&& add) {
+                        O[cb / 4][q][4 * (cb % 4) + r] = add(O[cb / 4][q][4 * (cb % 4) + r]);
+                    }, i, g);
+            } else {
+#pragma unroll
+                for (int v = 0; v < NCB; ++v) {
+                    const u32x4 x = v_fragment<D>(vb, 0, v, i, g);
+#pragma unroll
+                    for (int q = 0; q < QB; ++q) product(x, P, v, q);
+                }
+            }
+            if (!more) return;
+#pragma unroll
+            for (int f = 0; f < NKF; ++f) {
+                const u32x4 k = k_fragment<D>(kn, 16 * (f & 1), f >> 1, i, g);
+#pragma unroll
+                for (int q = 0; q < QB; ++q) score(k, f, q, S);
+            }
+            if (masked_next) {
+#pragma unroll
+                for (int q = 0; q < QB; ++q) {
+                    const uint32_t k = keep_of(q, key0 + 32, there_next);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) S[8 * q + e] = (k >> e) & 1 ? S[8 * q + e] : -INFINITY;
+                }
+            }
+            raise(S);
+        };
+
+        if (begin < end) {
+            constexpr std::integral_constant<bool, true> whole{};
+            constexpr std::integral_constant<bool, false> some{};
+            constexpr int KH = R::k_bytes(32), VH = R::v_bytes(32);  // a half's bytes
+            entry = entry_of(a.pages, table, kBK * begin + lane, u.keys);
+            locate(begin);
+            locate(begin + 1);  // (past the end: no key is there)
+            // the first half's rows of K, in the other buffer's second half, and the first turn's
+            if (wave < 2) fetch_part(kc, kbuf(1) + KH, there_a, off_a, 0, false, some);
+            fetch(0, some);
+            uint64_t there_c = there_a, there_n = there_b;  // of tiles j and j + 1
+            locate(begin + 2);  // there_a, there_b: of tiles j + 1 and j + 2
+            landed();
+#pragma unroll
+            for (int f = 0; f < NKF; ++f) {
+                const u32x4 k = k_fragment<D>(kbuf(1) + KH, 16 * (f & 1), f >> 1, i, g);
+#pragma unroll
+                for (int q = 0; q < QB; ++q) score(k, f, q, S0);
+            }
+            if (is_masked(begin, there_c)) {
+#pragma unroll
+                for (int q = 0; q < QB; ++q) {
+                    const uint32_t k = keep_of(q, kBK * begin, (uint32_t)there_c);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) S0[8 * q + e] = (k >> e) & 1 ? S0[8 * q + e] : -INFINITY;
+                }
+            }
+            raise(S0);
+            __syncthreads();  // (all have read the first half, whose place K(begin + 1) takes)
+            int j = begin, b = 0;  // b: buffers of tile j
+            auto next = [&]() {
+                there_c = there_n;
+                there_n = there_b;
+                locate(j + 3);
+                ++j;
+                b ^= 1;
+                landed();
+            };
+            while (true) {
+                // turns in which neither the two tiles that are used nor what is fetched meanwhile holds a masked key
+                while (j + 2 < end && !far && !is_masked(j, there_c) && !is_masked(j + 1, there_n) && there_b == ~0ull) {
+                    fetch(b ^ 1, whole);
+                    plain_half(S0, S1, kbuf(b), vbuf(b));
+                    plain_half(S1, S0, kbuf(b) + KH, vbuf(b) + VH);
+                    next();
+                }
+                const bool more = j + 1 < end;
+                if (more) fetch(b ^ 1, some);
+                const bool m0 = is_masked(j, there_c), m1 = is_masked(j + 1, there_n);
+                any_half(S0, m0, kBK * j, (uint32_t)there_c, vbuf(b), true, m0, (uint32_t)(there_c >> 32), kbuf(b));
+                any_half(S0, m0, kBK * j + 32, (uint32_t)(there_c >> 32), vbuf(b) + VH, more, m1, (uint32_t)there_n, kbuf(b) + KH);
+                if (!more) break;
+                next();
+            }
+        }
+        RowState<D, QB> st;
+        float sums[QB];
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            st.m[q] = m[q];
+            sums[q] = sum_across_rows16(l[q]);
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) st.O[q][cb][r] = O[cb / 4][q][4 * (cb % 4) + r];
+        }
+        store_rows_of<D, QB>(a, u, hk, BQ, wave * 16 * QB, row0, i, g, st, sums);
         __syncthreads();
     }
 }
@@ -746,8 +1018,12 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArg
 
 template <int D, int OP, int QB>
 hipError_t launch_few(const PagedAttnArgs& a, int units, hipStream_t s) {
-    hipLaunchKernelGGL((attn_paged_few_kernel<D, OP, QB>), dim3((units + 7) / 8 * 8), dim3(64 * kFewWaves), 0, s, a);
-    hipError_t e = hipGetLastError();
+    static std::atomic<uint64_t> done{0};
+    const auto kern = attn_paged_few_kernel<D, OP, QB>;
+    hipError_t e = allow_dynamic_lds(kern, few_lds<D, QB>(), done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kFewWaves), (few_lds<D, QB>()), s, a);
+    e = hipGetLastError();
     if (e != hipSuccess || !a.pieces) return e;
     hipLaunchKernelGGL((attn_paged_join_kernel<D, 16 * QB>), dim3(units), dim3(256), 0, s, a);
     return hipGetLastError();
