@@ -1490,6 +1490,7 @@ dit::PageArgs page_args(const dit_kv_cache& c, const int32_t* table, const int32
     p.token16 = c.page_size > 1 ? (uint32_t)(c.token / 8) : 0;
     p.head16 = c.Hk > 1 ? (uint32_t)(c.head / 8) : 0;
     p.page = dit::fast_div((uint32_t)c.page_size);
+    p.runs = c.page_size % 16 == 0 && c.token <= ((int64_t)1 << 31) / 2 / 16;
     return p;
 }
 

@@ -22,6 +22,7 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* ltr_t;
 
+constexpr int kWaitLoads = 0x0f70;  // s_waitcnt vmcnt(0), the other counters at their most
 constexpr float kNoScore = -1e30f;  // running maximum of a row that has none (finite: differences stay numbers)
 
 // ---- rows of K and V in LDS ----
@@ -46,23 +47,57 @@ struct Rows {
     static __device__ __forceinline__ int v_at(int row, int piece) { return row / RPL * VG + row % RPL * RB + 16 * v_piece(row % RPL, piece); }
 };
 
-// Operand of 16 keys (rows key0 .. +15), channels 32 ks .. +31: the lane's key i, channels 8g .. +7.
+// Operand of 16 keys (rows key0 .. +15), channels 32 ks .. +31: the lane's key i, channels 8g .. +7.  k_lane: where the lane
+// reads row 0's, ks = 0.
+template <int D>
+__device__ __forceinline__ int k_lane(int i, int g) { return Rows<D>::k_at(i, g); }
+template <int D>
+__device__ __forceinline__ u32x4 k_fragment_at(const uint8_t* k, int key0, int ks) {
+    return *reinterpret_cast<const u32x4*>(k + key0 / Rows<D>::RPL * Rows<D>::KG + 64 * ks);
+}
 template <int D>
 __device__ __forceinline__ u32x4 k_fragment(const uint8_t* k, int key0, int ks, int i, int g) {
-    return *reinterpret_cast<const u32x4*>(k + Rows<D>::k_at(i, g) + key0 / Rows<D>::RPL * Rows<D>::KG + 64 * ks);
+    return k_fragment_at<D>(k + k_lane<D>(i, g), key0, ks);
 }
 // Operand of 16 channels (16 cb .. +15) and 32 keys (rows key0 .. +31): the lane's channel i, keys 4g .. +3 and 16 + 4g .. +3.
+// v_lane: where the lane reads row 0's, of the blocks cb % 4 = c.
 template <int D>
-__device__ __forceinline__ u32x4 v_fragment(uint8_t* v, int key0, int cb, int i, int g) {
+__device__ __forceinline__ int v_lane(int c, int i, int g) {
+    return Rows<D>::v_at(4 * g + (i >> 2), 2 * c + ((i & 3) >> 1)) + 8 * (i & 1);
+}
+template <int D>
+__device__ __forceinline__ u32x4 v_fragment_at(uint8_t* v, int key0, int cb) {
     uint2 h[2];
-    const int at = Rows<D>::v_at(4 * g + (i >> 2), 2 * (cb & 3) + ((i & 3) >> 1)) + 8 * (i & 1);
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        uint8_t* const p = v + at + (key0 + 16 * b) / Rows<D>::RPL * Rows<D>::VG + (cb >> 2) * 128;
+        uint8_t* const p = v + (key0 + 16 * b) / Rows<D>::RPL * Rows<D>::VG + (cb >> 2) * 128;
         h[b] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr_t)p));
     }
     return mk4(h[0].x, h[0].y, h[1].x, h[1].y);
 }
+template <int D>
+__device__ __forceinline__ u32x4 v_fragment(uint8_t* v, int key0, int cb, int i, int g) {
+    return v_fragment_at<D>(v + v_lane<D>(cb & 3, i, g), key0, cb);
+}
+
+// 16 bytes a lane from base + off (bytes, of the lane) to LDS, lane l's 16 l behind `to`.  (As the instruction and not by the
+// compiler's built-in function: for a transposing read behind that one the compiler waits until every such load has landed, as it
+// cannot tell whether the read is of what the load writes.  Whoever reads waits for kWaitLoads first.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is never kept, which is what the warning is about
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t off, uint8_t* to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :
+                 : "s"((uint32_t)(uintptr_t)(lptr_t)to), "v"(off), "s"(base)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void load_to_lds(const uint8_t* from, uint8_t* to) {  // the lane's own address
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :
+                 : "s"((uint32_t)(uintptr_t)(lptr_t)to), "v"(from)
+                 : "memory", "m0");
+}
+#pragma clang diagnostic pop
 
 // ---- which work ----
 struct Unit {
@@ -108,66 +143,93 @@ __device__ __forceinline__ int scan_add(int x, int lane) {
     return x;
 }
 
-// Key tiles of a piece: as many as make `pieces` units of all tiles' keys, `least` at least.
-template <int BQ>
-__device__ __forceinline__ int piece_tiles(const PagedAttnArgs& a, int lane) {
-    if (!a.pieces) return 0x7fffffff;
-    float all = 0.f;
-    for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
-        int q0, n, keys;
-        const Load l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
-        all += (float)l.tiles * (float)l.key_tiles;
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) all += __shfl_xor(all, d);
-    const float c = ceilf(all / (float)a.pieces);
-    return c < (float)a.least ? a.least : c < 1e9f ? (int)c : 1000000000;
-}
-
 __device__ __forceinline__ int pieces_of(int key_tiles, int c) { return key_tiles <= c ? 1 : (key_tiles + c - 1) / c; }
 
-// Unit u of a key head's (WHOLE: tile u of its tiles, whatever their pieces): false if there are not so many.  total: of them.
+// What the wavefront's lanes know of 64 requests.
+template <int BQ>
+struct Requests {
+    int q0, n, keys;
+    Load l;
+    __device__ __forceinline__ void read(const PagedAttnArgs& a, int r0, int lane) {
+        l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
+    }
+};
+__device__ __forceinline__ int sum_of_lanes(int x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// The key head's units: `c` key tiles of a piece, at most, units in all, tiles in all.  c is such that all tiles' keys make no
+// more than a.pieces units, where there are not more tiles than that already.
+struct Units {
+    int c, units, tiles;
+};
+template <int BQ>
+__device__ __forceinline__ Units count_units(const PagedAttnArgs& a, const Requests<BQ>& first, int lane) {
+    auto total = [&](auto&& of) {
+        int all = of(first);
+        for (int r0 = 64; r0 < a.pages.n_requests; r0 += 64) {
+            Requests<BQ> r;
+            r.read(a, r0, lane);
+            all += of(r);
+        }
+        return sum_of_lanes(all);
+    };
+    Units u;
+    u.tiles = u.units = total([](const Requests<BQ>& r) { return r.l.tiles; });
+    u.c = 0x7fffffff;
+    if (!a.pieces || u.tiles >= a.pieces) return u;
+    float keys = (float)first.l.tiles * (float)first.l.key_tiles;
+    for (int r0 = 64; r0 < a.pages.n_requests; r0 += 64) {
+        Requests<BQ> r;
+        r.read(a, r0, lane);
+        keys += (float)r.l.tiles * (float)r.l.key_tiles;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) keys += __shfl_xor(keys, d);
+    float c = ceilf(keys / (float)a.pieces);
+    c = c < (float)a.least ? (float)a.least : c;
+    for (int k = 0; k < 4; ++k) {
+        u.c = c < 1e9f ? (int)c : 1000000000;
+        u.units = total([&](const Requests<BQ>& r) { return r.l.tiles * pieces_of(r.l.key_tiles, u.c); });
+        if (u.units <= a.pieces) break;
+        c = ceilf(c * ((float)u.units / (float)a.pieces));
+    }
+    u.c = __builtin_amdgcn_readfirstlane(u.c);
+    return u;
+}
+
+// Unit u of a key head's (WHOLE: tile u of its tiles, whatever their pieces): false if there are not so many.
 template <int BQ, bool WHOLE>
-__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int c, int u, int lane, Unit* out) {
+__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, const Requests<BQ>& first, int c, int u, int lane, Unit* out) {
     int units_before = 0, slots_before = 0;
     for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
-        int q0, n, keys;
-        const Load l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
-        const int pieces = pieces_of(l.key_tiles, c);
-        const int slots = l.tiles * pieces, units = WHOLE ? l.tiles : slots;
+        Requests<BQ> r = first;
+        if (r0) r.read(a, r0, lane);
+        const int pieces = pieces_of(r.l.key_tiles, c);
+        const int slots = r.l.tiles * pieces, units = WHOLE ? r.l.tiles : slots;
         const int upto = scan_add(units, lane), slots_upto = WHOLE ? scan_add(slots, lane) : upto;
         const uint64_t b = __ballot(u - units_before < upto);
         if (b) {
             const int at = __builtin_ctzll(b);
             auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
             out->r = r0 + at;
-            out->q0 = of(q0);
-            out->new_ = of(n);
-            out->keys = of(keys);
+            out->q0 = of(r.q0);
+            out->new_ = of(r.n);
+            out->keys = of(r.keys);
             out->pieces = of(pieces);
-            const int in = u - units_before - (of(upto) - of(units)), tiles = of(l.tiles);
+            const int in = u - units_before - (of(upto) - of(units)), tiles = of(r.l.tiles);
             // pieces of the same keys next to each other
             out->piece = WHOLE ? 0 : in / tiles;
             out->tile = WHOLE ? in : in - out->piece * tiles;
-            out->slot = slots_before + of(slots_upto) - of(slots) + (WHOLE ? in : in);
+            out->slot = slots_before + of(slots_upto) - of(slots) + in;
             return true;
         }
         units_before += __builtin_amdgcn_readlane(upto, 63);
         slots_before += __builtin_amdgcn_readlane(slots_upto, 63);
     }
     return false;
-}
-template <int BQ, bool WHOLE>
-__device__ __forceinline__ int count_units(const PagedAttnArgs& a, int c, int lane) {
-    int all = 0;
-    for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
-        int q0, n, keys;
-        const Load l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
-        all += l.tiles * (WHOLE ? 1 : pieces_of(l.key_tiles, c));
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) all += __shfl_xor(all, d);
-    return __builtin_amdgcn_readfirstlane(all);
 }
 
 // The n-th of a workgroup's units: workgroups go round the eight XCDs, each of which gets a run of neighbouring units, that
@@ -200,15 +262,15 @@ struct KeyRow {
     uint32_t off16;
     bool there;
 };
-__device__ __forceinline__ int entry_of(const PageArgs& p, const int32_t* table, int key, int keys) {
-    const int n = key < keys ? key : keys - 1;
+__device__ __forceinline__ int entry_of(const PageArgs& p, const int32_t* table, int key, int keys) {  // keys > 0
+    const int n = key < 0 ? 0 : key < keys ? key : keys - 1;
     return table[div_by((uint32_t)n, p.page)];
 }
 __device__ __forceinline__ KeyRow row_of(const PageArgs& p, int entry, int key, int keys) {
-    const int n = key < keys ? key : keys - 1;
+    const int n = key < 0 ? 0 : key < keys ? key : keys - 1;
     const uint32_t in = (uint32_t)n - div_by((uint32_t)n, p.page) * p.page.d;
     KeyRow k;
-    k.there = key < keys && entry >= 0 && entry < p.n_pages;
+    k.there = (uint32_t)key < (uint32_t)keys && entry >= 0 && entry < p.n_pages;
     k.off16 = (uint32_t)entry * p.page16 + in * p.token16;
     return k;
 }
@@ -485,15 +547,17 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const Pa
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint8_t* const kt = smem + wave * (Rows<D>::k_bytes(KEYS) + Rows<D>::v_bytes(KEYS));
     uint8_t* const vt = kt + Rows<D>::k_bytes(KEYS);
-    const int c = piece_tiles<BQ>(a, lane);
-    const int per_head = count_units<BQ, false>(a, c, lane);
+    Requests<BQ> requests;
+    requests.read(a, 0, lane);
+    const Units all = count_units<BQ>(a, requests, lane);
+    const int per_head = all.units;
     const int64_t total = (int64_t)per_head * a.Hk;
     for (int n = 0;; ++n) {
         const int64_t id = nth_unit(total, n);
         if (id < 0) return;
         const int hk = (int)(id / per_head);
         Unit u;
-        if (!find_unit<BQ, false>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        if (!find_unit<BQ, false>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
         RowState<D, QB> st;
         u32x4 Q[QB][D / 32];
         const int64_t row0 = (int64_t)u.tile * BQ;
@@ -613,7 +677,8 @@ static_assert(kPagedBigRows == 16 * kBigQB * kBigWaves, "rows of a workgroup");
 template <int D>
 constexpr int big_lds() { return 2 * (Rows<D>::k_bytes(kBK) + Rows<D>::v_bytes(kBK)); }
 
-template <int D, int OP>
+// RUNS: 16 tokens from a multiple of 16 on lie in one page, so that a wavefront's rows of a part start at one place.
+template <int D, int OP, bool RUNS>
 __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const PagedAttnArgs a) {
     using R = Rows<D>;
     constexpr int NW = kBigWaves, QB = kBigQB, BQ = kPagedBigRows;
@@ -626,8 +691,10 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
     extern __shared__ __attribute__((aligned(16))) uint8_t dyn[];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = piece_tiles<BQ>(a, lane);
-    const int per_head = count_units<BQ, false>(a, c, lane);
+    Requests<BQ> requests;
+    requests.read(a, 0, lane);
+    const Units all = count_units<BQ>(a, requests, lane);
+    const int per_head = all.units;
     const int64_t total = (int64_t)per_head * a.Hk;
     const float scale = a.scale_log2, thr = kRescaleThr / scale;
     // K buffers 0 and 1, then V's
@@ -645,10 +712,11 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
         if (id < 0) return;
         const int hk = (int)(id / per_head);
         Unit u;
-        if (!find_unit<BQ, false>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        if (!find_unit<BQ, false>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
         u32x4 Q[QB][NKS];
         f32x16 O[NOG][QB], S0, S1;  // scores: quarter 2 q + kb = row block q, keys 16 kb .. of the half
-        float m[QB], l[QB], off[QB];
+        float m[QB], top[QB], off[QB];  // maximum, what a score has to top to raise it, what its exponent is short of
+        float l[QB][2];                 // sums, of every other key of the lane's
         int lo = 0, hi = 0x7fffffff;  // keys that every row of the wavefront sees
         const int64_t row0 = (int64_t)u.tile * BQ + wave * 16 * QB;
         {
@@ -659,8 +727,9 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 lo = max(lo, st.first[q]);
                 hi = min(hi, st.past[q]);
                 m[q] = kNoScore;
+                top[q] = kNoScore + thr;
                 off[q] = -kNoScore * scale;
-                l[q] = 0.f;
+                l[q][0] = l[q][1] = 0.f;
 #pragma unroll
                 for (int og = 0; og < NOG; ++og)
 #pragma unroll
@@ -680,44 +749,107 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
         const uint8_t* const kc = a.k_cache + (int64_t)hk * a.pages.head16 * 16;
         const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
 
-        // ---- tiles: rows' places are worked out ahead by lane l for row l, for all wavefronts alike ----
-        // of two tiles that were located ahead of their fetch: which of their keys are there, and where row `lane` lies
-        uint64_t there_a = 0, there_b = 0;
+        // ---- where rows of K and V are ----
+        // RUNS: lane x has run x % 4 (16 keys) of tile first_tile + x / 4: the place of its first row, and in `ok` whether its page
+        // is there; the pages of the sixteen tiles behind the next turn but thirteen are asked for meanwhile.  Else lane l has row l of the tiles
+        // j + 1 and j + 2, j the one whose turn it is: off_a, off_b, there_a, there_b (there_c: of j), and asks for the page of j + 3.
+        constexpr int kTurns = 14;  // a turn needs its tile and the two behind it
+        int first_tile = 0, entry = 0;
         uint32_t off_a = 0, off_b = 0;
-        int entry = 0;  // of row `lane` of the tile behind them
-        // the tile behind the two (its entries are there); the entries of the one behind it are asked for
-        auto locate = [&](int tile) {
-            there_a = there_b;
-            off_a = off_b;
-            const KeyRow kr = row_of(a.pages, entry, kBK * tile + lane, u.keys);
-            there_b = __ballot(kr.there);
-            off_b = kr.off16;
-            entry = entry_of(a.pages, table, kBK * (tile + 1) + lane, u.keys);
-        };
-        // this wavefront's 16 rows of a part; row r of it is where lane (r + turn) % 64 says
-        auto fetch_part = [&](const uint8_t* cache, uint8_t* buf, uint64_t there, uint32_t off16, int turn, bool v, auto whole) {
-            const int row_l = lane / R::PPR, slot_l = lane % R::PPR;
-            const uint8_t* const src = cache + 16 * (v ? R::v_piece(row_l, slot_l) : R::k_piece(row_l, slot_l));
-            uint8_t* const dst = buf + wave * NL * (v ? R::VG : R::KG);
-#pragma unroll
-            for (int p = 0; p < NL; ++p) {
-                const int from = (16 * wave + p * RPI + row_l + turn) & 63;
-                const uint32_t at = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)off16);
-                uint8_t* const to = dst + p * (v ? R::VG : R::KG);
-                if (whole || ((there >> from) & 1))
-                    __builtin_amdgcn_global_load_lds((gptr_t)(src + (uint64_t)at * 16), (lptr_t)to, 16, 0, 0);
-                else
-                    *reinterpret_cast<u32x4*>(to + 16 * lane) = mk4(0, 0, 0, 0);
+        uint64_t ok = 0, there_a = 0, there_b = 0, there_c = 0;
+        auto ask = [&](int tile) { return entry_of(a.pages, table, RUNS ? kBK * tile + 16 * lane : kBK * tile + lane, u.keys); };
+        auto start_at = [&](int tile) {
+            if constexpr (RUNS) {
+                const KeyRow kr = row_of(a.pages, ask(tile), kBK * tile + 16 * lane, u.keys);
+                ok = __ballot(kr.there);
+                off_a = kr.off16;
+                first_tile = tile;
+                entry = ask(tile + kTurns);
+            } else {
+                const KeyRow r1 = row_of(a.pages, ask(tile + 1), kBK * (tile + 1) + lane, u.keys);
+                const KeyRow r2 = row_of(a.pages, ask(tile + 2), kBK * (tile + 2) + lane, u.keys);
+                there_a = __ballot(r1.there);
+                there_b = __ballot(r2.there);
+                off_a = r1.off16;
+                off_b = r2.off16;
+                entry = ask(tile + 3);
             }
         };
-        // K and V of the first located tile's turn: V's rows are the tile's, K's its second half and the first of the next one
-        constexpr uint64_t kLow = 0xffffffffull;
-        auto fetch = [&](int b, auto whole) {
-            fetch_part(kc, kbuf(b), (there_a & ~kLow) | (there_b & kLow), lane < 32 ? off_b : off_a, 32, false, whole);
-            fetch_part(vc, vbuf(b), there_a, off_a, 0, true, whole);
+        auto step_to = [&](int tile) {  // tile: the next turn's
+            if constexpr (RUNS) {
+                if (tile - first_tile < kTurns) return;
+                const KeyRow kr = row_of(a.pages, entry, kBK * tile + 16 * lane, u.keys);
+                ok = __ballot(kr.there);
+                off_a = kr.off16;
+                first_tile = tile;
+                entry = ask(tile + kTurns);
+            } else {
+                there_c = there_a;
+                off_a = off_b;
+                there_a = there_b;
+                const KeyRow kr = row_of(a.pages, entry, kBK * (tile + 2) + lane, u.keys);
+                there_b = __ballot(kr.there);
+                off_b = kr.off16;
+                entry = ask(tile + 3);
+            }
+        };
+        // bit r: key r of the tile j + n is there (n = 0, 1, 2)
+        auto there_of = [&](int j, int n) -> uint64_t {
+            if constexpr (RUNS) {
+                const uint32_t runs = (uint32_t)(ok >> (4 * (j + n - first_tile))) & 15u;
+                uint64_t x = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x |= (runs >> k) & 1u ? 0xffffull << (16 * k) : 0ull;
+                const int left = u.keys - kBK * (j + n);
+                return left >= kBK ? x : left <= 0 ? 0ull : x & ((1ull << left) - 1);
+            } else {
+                return n == 0 ? there_c : n == 1 ? there_a : there_b;
+            }
+        };
+        auto pages_there = [&](int j) -> bool {  // of tiles j .. j + 2, whole ones
+            if constexpr (RUNS) return ((uint32_t)(ok >> (4 * (j - first_tile))) & 0xfffu) == 0xfffu;
+            else return (there_c & there_a & there_b) == ~0ull;
+        };
+        // This wavefront's 16 rows of a part of tile j + 1's turn, from row `from` of the tile on (0, or for K 32: past its end the next
+        // tile's follow).  whole: all of them are there.
+        auto fetch_part = [&](int lane, const uint8_t* cache, uint8_t* buf, int j, int from, bool v, auto whole)
+            __attribute__((always_inline)) {
+            const int row_l = lane / R::PPR, slot_l = lane % R::PPR, first = 16 * wave + from;
+            const uint32_t piece = 16 * (v ? R::v_piece(row_l, slot_l) : R::k_piece(row_l, slot_l));
+            uint8_t* const dst = buf + wave * NL * (v ? R::VG : R::KG);
+            const uint64_t there = whole ? ~0ull : first < kBK ? there_of(j, 1) >> first : there_of(j, 2) >> (first - kBK);
+            if constexpr (RUNS) {
+                const uint8_t* src = cache + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(
+                                                 (int)off_a, 4 * (j + 1 - first_tile) + wave + from / 16) * 16;
+                const uint32_t row = 16 * a.pages.token16, in = row_l * row + piece;
+#pragma unroll
+                for (int p = 0; p < NL; ++p) {
+                    uint8_t* const to = dst + p * (v ? R::VG : R::KG);
+                    if (whole || ((there >> (p * RPI + row_l)) & 1)) load_to_lds(src + p * RPI * row, in, to);
+                    else *reinterpret_cast<u32x4*>(to + 16 * lane) = mk4(0, 0, 0, 0);
+                }
+            } else {
+                const uint32_t off16 = first < kBK ? off_a : off_b;
+                uint32_t at[NL];
+#pragma unroll
+                for (int p = 0; p < NL; ++p)
+                    at[p] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((first + p * RPI + row_l) & 63), (int)off16);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int p = 0; p < NL; ++p) {
+                    uint8_t* const to = dst + p * (v ? R::VG : R::KG);
+                    if (whole || ((there >> (p * RPI + row_l)) & 1)) load_to_lds(cache + piece + (uint64_t)at[p] * 16, to);
+                    else *reinterpret_cast<u32x4*>(to + 16 * lane) = mk4(0, 0, 0, 0);
+                }
+            }
+        };
+        // K and V of tile j + 1's turn: V's rows are the tile's, K's its second half and the first of the next one
+        auto fetch = [&](int lane, int j, int b, auto whole) __attribute__((always_inline)) {
+            fetch_part(lane, kc, kbuf(b), j, 32, false, whole);
+            fetch_part(lane, vc, vbuf(b), j, 0, true, whole);
         };
         auto landed = [&]() {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(kWaitLoads);
             __syncthreads();
         };
 
@@ -747,11 +879,13 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
 #pragma unroll
                 for (int e = 1; e < 8; ++e) mx = fmaxf(mx, S[8 * q + e]);
                 mx = max_across_rows16(mx);
-                const float to = mx > m[q] + thr ? mx : m[q];
+                const float to = mx > top[q] ? mx : m[q];
                 const float alpha = __builtin_amdgcn_exp2f((m[q] - to) * scale);
                 m[q] = to;
+                top[q] = to + thr;
                 off[q] = -to * scale;
-                l[q] *= alpha;
+                l[q][0] *= alpha;
+                l[q][1] *= alpha;
                 far = far || (to != kNoScore && __builtin_fabsf(off[q]) > 4096.0f);
 #pragma unroll
                 for (int og = 0; og < NOG; ++og)
@@ -766,11 +900,11 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], scale, off[q]));
             S[e + 1] = __builtin_amdgcn_exp2f(fmaf(S[e + 1], scale, off[q]));
         };
-        auto pack_slice = [&](f32x16& S, uint32_t (&P)[QB][4], float (&sum)[QB][2], int x) {
+        auto pack_slice = [&](f32x16& S, uint32_t (&P)[QB][4], int x) {
             const int q = x / 4, e = 2 * x;
             P[q][x % 4] = pack2<OP>(S[e], S[e + 1]);
-            sum[q][0] += S[e];
-            sum[q][1] += S[e + 1];
+            l[q][0] += S[e];
+            l[q][1] += S[e + 1];
         };
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
         auto score = [&](u32x4 k, int f, int q, f32x16& S) {
@@ -783,16 +917,15 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
 
         // One half (its scores in Sc) and the next one's scores (into Sn), no key of either masked for any row.  kn: the next one's
         // rows of K, vb: this one's of V
-        auto plain_half = [&](f32x16& Sc, f32x16& Sn, const uint8_t* kn, uint8_t* vb) __attribute__((always_inline)) {
+        // (the lane's own addresses in them).
+        auto plain_half = [&](f32x16& Sc, f32x16& Sn, const uint8_t* kn, uint8_t* const (&vb)[4], auto half) __attribute__((always_inline)) {
+            constexpr int H = decltype(half)::value;
             u32x4 kf[NKF], vf[NCB];
-            auto k_frag = [&](int f) { return k_fragment<D>(kn, 16 * (f & 1), f >> 1, i, g); };
-            auto v_frag = [&](int v) { return v_fragment<D>(vb, 0, v, i, g); };
+            auto k_frag = [&](int f) { return k_fragment_at<D>(kn, 32 * H + 16 * (f & 1), f >> 1); };
+            auto v_frag = [&](int v) { return v_fragment_at<D>(vb[v & 3], 32 * H, v); };
 #pragma unroll
             for (int f = 0; f < LA; ++f) kf[f] = k_frag(f);
             uint32_t P[QB][4];
-            float sum[QB][2];
-#pragma unroll
-            for (int q = 0; q < QB; ++q) sum[q][0] = sum[q][1] = 0.f;
 #pragma unroll
             for (int x = 0; x < PRE; ++x) exp_slice(Sc, x);
             __builtin_amdgcn_sched_barrier(0);
@@ -807,11 +940,9 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 __builtin_amdgcn_sched_barrier(0);
                 score(kf[f], f, 1, Sn);
 #pragma unroll
-                for (int x = f * NCH / NKF; x < (f + 1) * NCH / NKF; ++x) pack_slice(Sc, P, sum, x);
+                for (int x = f * NCH / NKF; x < (f + 1) * NCH / NKF; ++x) pack_slice(Sc, P, x);
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int q = 0; q < QB; ++q) l[q] += sum[q][0] + sum[q][1];
             float mx[QB] = {-INFINITY, -INFINITY};
             auto max_slice = [&](int x) { mx[x & 1] = max3(mx[x & 1], Sn[8 * (x & 1) + 2 * (x >> 1)], Sn[8 * (x & 1) + 2 * (x >> 1) + 1]); };
 #pragma unroll
@@ -828,7 +959,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             }
 #pragma unroll
             for (int x = (NCB - 1) * NCH / NCB; x < NCH; ++x) max_slice(x);
-            if (__any(mx[0] > m[0] + thr || mx[1] > m[1] + thr)) raise(Sn);
+            if (__any(mx[0] > top[0] || mx[1] > top[1])) raise(Sn);
         };
 
         // One half, whatever is masked of it, and the next one's scores (if there is one) into the same registers.
@@ -845,15 +976,10 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 }
             }
             uint32_t P[QB][4];
-            float sum[QB][2];
-#pragma unroll
-            for (int q = 0; q < QB; ++q) sum[q][0] = sum[q][1] = 0.f;
 #pragma unroll
             for (int x = 0; x < NCH; ++x) exp_slice(S, x);
 #pragma unroll
-            for (int x = 0; x < NCH; ++x) pack_slice(S, P, sum, x);
-#pragma unroll
-            for (int q = 0; q < QB; ++q) l[q] += sum[q][0] + sum[q][1];
+            for (int x = 0; x < NCH; ++x) pack_slice(S, P, x);
             bool bad = false;
             if (masked) {
 #pragma unroll
@@ -899,55 +1025,65 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             constexpr std::integral_constant<bool, true> whole{};
             constexpr std::integral_constant<bool, false> some{};
             constexpr int KH = R::k_bytes(32), VH = R::v_bytes(32);  // a half's bytes
-            entry = entry_of(a.pages, table, kBK * begin + lane, u.keys);
-            locate(begin);
-            locate(begin + 1);  // (past the end: no key is there)
-            // the first half's rows of K, in the other buffer's second half, and the first turn's
-            if (wave < 2) fetch_part(kc, kbuf(1) + KH, there_a, off_a, 0, false, some);
-            fetch(0, some);
-            uint64_t there_c = there_a, there_n = there_b;  // of tiles j and j + 1
-            locate(begin + 2);  // there_a, there_b: of tiles j + 1 and j + 2
+            // as if tile begin - 1's turn were over: the first half's rows of K, in the other buffer's second half, and the first turn's
+            int j = begin - 1;
+            start_at(j);
+            if (wave < 2) fetch_part(lane, kc, kbuf(1) + KH, j, 0, false, some);
+            fetch(lane, j, 0, some);
+            j = begin;
+            step_to(j);
             landed();
+            // keys [key0, key0 + 32) of which the lane's rows see some, those of the half whose scores S are
+            auto mask = [&](f32x16& S, int key0, uint32_t there) {
+#pragma unroll
+                for (int q = 0; q < QB; ++q) {
+                    const uint32_t k = keep_of(q, key0, there);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) S[8 * q + e] = (k >> e) & 1 ? S[8 * q + e] : -INFINITY;
+                }
+            };
+            const uint64_t there_0 = there_of(j, 0);
 #pragma unroll
             for (int f = 0; f < NKF; ++f) {
                 const u32x4 k = k_fragment<D>(kbuf(1) + KH, 16 * (f & 1), f >> 1, i, g);
 #pragma unroll
                 for (int q = 0; q < QB; ++q) score(k, f, q, S0);
             }
-            if (is_masked(begin, there_c)) {
-#pragma unroll
-                for (int q = 0; q < QB; ++q) {
-                    const uint32_t k = keep_of(q, kBK * begin, (uint32_t)there_c);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) S0[8 * q + e] = (k >> e) & 1 ? S0[8 * q + e] : -INFINITY;
-                }
-            }
+            if (is_masked(begin, there_0)) mask(S0, kBK * begin, (uint32_t)there_0);
             raise(S0);
             __syncthreads();  // (all have read the first half, whose place K(begin + 1) takes)
-            int j = begin, b = 0;  // b: buffers of tile j
-            auto next = [&]() {
-                there_c = there_n;
-                there_n = there_b;
-                locate(j + 3);
-                ++j;
-                b ^= 1;
-                landed();
-            };
+            int b = 0;  // buffers of tile j
             while (true) {
-                // turns in which neither the two tiles that are used nor what is fetched meanwhile holds a masked key
-                while (j + 2 < end && !far && !is_masked(j, there_c) && !is_masked(j + 1, there_n) && there_b == ~0ull) {
-                    fetch(b ^ 1, whole);
-                    plain_half(S0, S1, kbuf(b), vbuf(b));
-                    plain_half(S1, S0, kbuf(b) + KH, vbuf(b) + VH);
-                    next();
+                const int ln = opaque_lane();  // (what the loop reads is worked out here, not spilled and read back)
+                const int k_l = k_lane<D>(ln & 15, ln >> 4);
+                int v_l[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v_l[x] = v_lane<D>(x, ln & 15, ln >> 4);
+                // Turns in which neither the tiles that are used nor what is fetched meanwhile holds a masked key.
+                while (j + 2 < end && !far && kBK * j >= lo && kBK * j + 2 * kBK <= hi && pages_there(j)) {
+                    fetch(ln, j, b ^ 1, whole);
+                    const uint8_t* const kl = kbuf(b) + k_l;
+                    uint8_t* vl[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) vl[x] = vbuf(b) + v_l[x];
+                    plain_half(S0, S1, kl, vl, std::integral_constant<int, 0>{});
+                    plain_half(S1, S0, kl, vl, std::integral_constant<int, 1>{});
+                    ++j;
+                    b ^= 1;
+                    step_to(j);
+                    landed();
                 }
                 const bool more = j + 1 < end;
-                if (more) fetch(b ^ 1, some);
-                const bool m0 = is_masked(j, there_c), m1 = is_masked(j + 1, there_n);
-                any_half(S0, m0, kBK * j, (uint32_t)there_c, vbuf(b), true, m0, (uint32_t)(there_c >> 32), kbuf(b));
-                any_half(S0, m0, kBK * j + 32, (uint32_t)(there_c >> 32), vbuf(b) + VH, more, m1, (uint32_t)there_n, kbuf(b) + KH);
+                if (more) fetch(opaque_lane(), j, b ^ 1, some);
+                const uint64_t t0 = there_of(j, 0), t1 = there_of(j, 1);
+                const bool m0 = is_masked(j, t0), m1 = is_masked(j + 1, t1);
+                any_half(S0, m0, kBK * j, (uint32_t)t0, vbuf(b), true, m0, (uint32_t)(t0 >> 32), kbuf(b));
+                any_half(S0, m0, kBK * j + 32, (uint32_t)(t0 >> 32), vbuf(b) + VH, more, m1, (uint32_t)t1, kbuf(b) + KH);
                 if (!more) break;
-                next();
+                ++j;
+                b ^= 1;
+                step_to(j);
+                landed();
             }
         }
         RowState<D, QB> st;
@@ -955,7 +1091,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
             st.m[q] = m[q];
-            sums[q] = sum_across_rows16(l[q]);
+            sums[q] = sum_across_rows16(l[q][0] + l[q][1]);
 #pragma unroll
             for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
@@ -972,13 +1108,15 @@ template <int D, int BQ>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a) {
     constexpr int CL = D / 16;  // channels a lane
     const int lane = threadIdx.x & 63;
-    const int c = piece_tiles<BQ>(a, lane);
-    const int per_head = count_units<BQ, true>(a, c, lane);
+    Requests<BQ> requests;
+    requests.read(a, 0, lane);
+    const Units all = count_units<BQ>(a, requests, lane);
+    const int per_head = all.tiles;
     const int64_t total = (int64_t)per_head * a.Hk;
     for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
         const int hk = (int)(id / per_head);
         Unit u;
-        if (!find_unit<BQ, true>(a, c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        if (!find_unit<BQ, true>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
         if (u.pieces < 2) continue;
         // piece s of the tile is tiles-of-the-request slots behind piece s - 1; u.slot counts from the request's first
         const int64_t rows = (int64_t)u.new_ * a.G;
@@ -1030,8 +1168,9 @@ hipError_t launch_few(const PagedAttnArgs& a, int units, hipStream_t s) {
 }
 template <int D, int OP>
 hipError_t launch_big(const PagedAttnArgs& a, int units, hipStream_t s) {
-    static std::atomic<uint64_t> done{0};
-    const auto kern = attn_paged_big_kernel<D, OP>;
+    static std::atomic<uint64_t> done_runs{0}, done_rows{0};
+    const auto kern = a.pages.runs ? attn_paged_big_kernel<D, OP, true> : attn_paged_big_kernel<D, OP, false>;
+    std::atomic<uint64_t>& done = a.pages.runs ? done_runs : done_rows;
     hipError_t e = allow_dynamic_lds(kern, big_lds<D>(), done);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kBigWaves), big_lds<D>(), s, a);
@@ -1073,29 +1212,39 @@ hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_
 
 PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int max_q) {
     PagedPlan p{};
-    const int64_t G = H / Hk, rows = (int64_t)N * G, least = N < R ? N : R;
-    const int64_t most_q = max_q > 0 && max_q < N ? max_q : N;  // new tokens of a request
+    const int64_t G = H / Hk, rows = (int64_t)N * G, some = N < R ? N : R;  // requests with a new token
+    const int64_t most_q = max_q > 0 && max_q < N ? max_q : N;              // new tokens of a request
     p.few_qb = most_q * G > 16 ? 2 : 1;
-    const bool uniform = most_q * least <= 2 * (int64_t)N;  // few requests have far fewer new tokens than that
+    const bool uniform = most_q * some <= 2 * (int64_t)N;  // few requests have far fewer new tokens than that
     p.few = most_q * G <= 32 || !uniform;
     p.big = most_q * G > 32;
-    const int64_t key_tiles = (max_keys + kBK - 1) / kBK;
-    // tiles of a key head, at most: whatever q_start says, and what is left over of each request
-    auto layout = [&](int BQ, int wanted, int slack, int& units, int& pieces, int& cap, size_t& bytes) {
-        const int64_t tiles = (rows + least * (BQ - 1)) / BQ;
-        const int64_t per_head = (wanted + Hk - 1) / Hk;
-        if (tiles * Hk < slack && key_tiles > 4) {
-            pieces = (int)per_head;
-            cap = (int)(per_head + tiles);
-            bytes = (size_t)Hk * cap * BQ * (D * sizeof(float) + sizeof(float2));
-            bytes = (bytes + 255) / 256 * 256;
-            units = Hk * cap;
-        } else {
-            units = (int)(tiles * Hk < 65536 ? tiles * Hk : 65536);
+    const int64_t key_tiles = max_keys > 0 ? (max_keys + kBK - 1) / kBK : 1;
+    // Two workgroups a compute unit.  Time in key tiles of a workgroup: rounds of workgroups, each as long as its keys and its two
+    // ends; tiles in pieces need the launch that joins them.
+    auto layout = [&](int BQ, int least, double ends, double join, int& units, int& pieces, int& cap, size_t& bytes) {
+        constexpr int64_t slots = 2 * kCUs;
+        // tiles of a key head: at most (whatever q_start says, with what is left over of each request), and as far as is known
+        const int64_t most = (rows + some * (BQ - 1)) / BQ;
+        const int64_t each = (most_q * G + BQ - 1) / BQ, tiles = some * each < most ? some * each : most;
+        auto time = [&](int n) {
+            const int64_t rounds = (tiles * Hk * n + slots - 1) / slots;
+            return (double)rounds * ((double)((key_tiles + n - 1) / n) + ends) + (n > 1 ? join : 0.0);
+        };
+        int best = 1;
+        for (int n = 2; n <= 64 && n * (int64_t)least <= key_tiles; ++n) {
+            if ((tiles * n + most) * Hk * BQ > (int64_t)1 << 19) break;  // rows of pieces: 272 MB at head_dim 128
+            if (time(n) < 0.97 * time(best)) best = n;
         }
+        if (best > 1) {
+            pieces = (int)(tiles * best);
+            cap = (int)(tiles * best + most);
+            bytes = ((size_t)Hk * cap * BQ * (D * sizeof(float) + sizeof(float2)) + 255) / 256 * 256;
+        }
+        const int64_t n = tiles * Hk * best;
+        units = (int)(n < 65536 ? n : 65536);
     };
-    if (p.few) layout(16 * p.few_qb, 4 * kCUs, 2 * kCUs, p.few_units, p.few_pieces, p.few_cap, p.few_bytes);
-    if (p.big) layout(kPagedBigRows, 2 * kCUs, 2 * kCUs, p.big_units, p.big_pieces, p.big_cap, p.big_bytes);
+    if (p.few) layout(16 * p.few_qb, 2, 6.0, 4.0, p.few_units, p.few_pieces, p.few_cap, p.few_bytes);
+    if (p.big) layout(kPagedBigRows, 4, 6.0, 6.0, p.big_units, p.big_pieces, p.big_cap, p.big_bytes);
     return p;
 }
 

@@ -27,6 +27,7 @@ struct PageArgs {
     int n_requests, max_pages, n_pages;
     uint32_t page16, token16, head16;
     FastDiv page;  // page_size
+    int runs;      // 16 tokens from a multiple of 16 on lie in one page, their rows within 2^31 bytes
 };
 
 // Tokens that the table of a request has room for, and those of them that are there.
