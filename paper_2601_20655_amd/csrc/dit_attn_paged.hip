@@ -347,33 +347,30 @@ struct RowState {
     }
 };
 
-// One tile of KEYS keys (64 or 32) in LDS: scores, softmax, O += P V.  `there`: bit = key's page is there; masked: some key is
-// masked for some row of the wavefront.
-template <int D, int OP, int QB, int KEYS>
-__device__ __forceinline__ void tile_step(RowState<D, QB>& st, const u32x4 (&Q)[QB][D / 32], const uint8_t* kt, uint8_t* vt,
-                                          int key0, uint64_t there, bool masked, float scale_log2, int i, int g) {
-    constexpr int NB = KEYS / 16, NKS = D / 32, NCB = D / 16;
-    f32x4 S[QB][NB];
-#pragma unroll
-    for (int q = 0; q < QB; ++q)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) S[q][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const u32x4 k = k_fragment<D>(kt, 16 * b, ks, i, g);
-#pragma unroll
-            for (int q = 0; q < QB; ++q) S[q][b] = mfma16<OP>(k, Q[q][ks], S[q][b]);
-        }
+// 32 keys: scores, softmax, O += P V.  kf(f), vf(cb): their fragments.  MASKED: `there` (bit = the key's page is there) and the
+// rows' ranges leave some out, and vt is where V's rows lie in LDS.
+template <int D, int OP, int QB, bool MASKED, class KF, class VF>
+__device__ __forceinline__ void block_step(RowState<D, QB>& st, const u32x4 (&Q)[QB][D / 32], KF&& kf, VF&& vf, const uint8_t* vt,
+                                           int key0, uint32_t there, float scale_log2, int i, int g) {
+    constexpr int NKS = D / 32, NCB = D / 16;
+    f32x4 S[QB][2];
     uint32_t keep[QB];
-    if (masked) {
-        const uint64_t mine = there >> (4 * g);
+#pragma unroll
+    for (int f = 0; f < 2 * NKS; ++f) {
+        const u32x4 k = kf(f);
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
-            keep[q] = 0;
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            S[q][f & 1] = mfma16<OP>(k, Q[q][f >> 1], f < 2 ? zero : S[q][f & 1]);
+        }
+    }
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+    for (int q = 0; q < QB; ++q) {
+        if constexpr (MASKED) {
+            keep[q] = 0;
+            const uint32_t mine = there >> (4 * g);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int key = key0 + 16 * b + 4 * g + r;
@@ -383,18 +380,17 @@ __device__ __forceinline__ void tile_step(RowState<D, QB>& st, const u32x4 (&Q)[
                 }
         }
     }
-    static_assert(KEYS == 32, "the words of 32 keys");
-    uint32_t P[QB][2 * NB];
+    uint32_t P[QB][4];
 #pragma unroll
     for (int q = 0; q < QB; ++q) {
         float mx = S[q][0][0];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int r = 0; r < 4; ++r) mx = fmaxf(mx, S[q][b][r]);
         mx = fmaxf(max_across_rows16(mx), st.m[q]);
-        const float alpha = __builtin_amdgcn_exp2f((st.m[q] - mx) * scale_log2);
         if (__any(mx > st.m[q])) {
+            const float alpha = __builtin_amdgcn_exp2f((st.m[q] - mx) * scale_log2);
             st.l[q] *= alpha;
 #pragma unroll
             for (int cb = 0; cb < NCB; ++cb)
@@ -408,51 +404,43 @@ __device__ __forceinline__ void tile_step(RowState<D, QB>& st, const u32x4 (&Q)[
         if (__any(__builtin_fabsf(off) > 4096.0f)) {
             off = 0.f;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) S[q][b][r] -= mx;
         }
-        float sum = 0.f;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
+        for (int b = 0; b < 2; ++b) {
             float e[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 e[r] = __builtin_amdgcn_exp2f(fmaf(S[q][b][r], scale_log2, off));
-                sum += e[r];
+                st.l[q] += e[r];
             }
             P[q][2 * b] = pack2<OP>(e[0], e[1]);
             P[q][2 * b + 1] = pack2<OP>(e[2], e[3]);
         }
-        st.l[q] += sum;
     }
-    if (masked) {
+    if constexpr (MASKED) {
         bool bad = false;
 #pragma unroll
-        for (int m = 0; m < NB / 2; ++m)
+        for (int cb = 0; cb < NCB; ++cb) {
+            const u32x4 v = vf(cb);
 #pragma unroll
-            for (int cb = 0; cb < NCB; ++cb) {
-                const u32x4 v = v_fragment<D>(vt, 32 * m, cb, i, g);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) bad = bad || pair_not_finite<OP>(v[w]);
-            }
+            for (int w = 0; w < 4; ++w) bad = bad || pair_not_finite<OP>(v[w]);
+        }
         if (__any(bad)) {
 #pragma unroll
             for (int q = 0; q < QB; ++q)
-                pv_one_by_one<D, OP>(vt, P[q], keep[q], [&](int cb, int r, auto&& add) { st.O[q][cb][r] = add(st.O[q][cb][r]); },
-                                           i, g);
+                pv_one_by_one<D, OP>(vt, P[q], keep[q], [&](int cb, int r, auto&& add) { st.O[q][cb][r] = add(st.O[q][cb][r]); }, i, g);
             return;
         }
     }
 #pragma unroll
-    for (int m = 0; m < NB / 2; ++m)
+    for (int cb = 0; cb < NCB; ++cb) {
+        const u32x4 v = vf(cb);
 #pragma unroll
-        for (int cb = 0; cb < NCB; ++cb) {
-            const u32x4 v = v_fragment<D>(vt, 32 * m, cb, i, g);
-#pragma unroll
-            for (int q = 0; q < QB; ++q)
-                st.O[q][cb] = mfma16<OP>(v, mk4(P[q][4 * m], P[q][4 * m + 1], P[q][4 * m + 2], P[q][4 * m + 3]), st.O[q][cb]);
-        }
+        for (int q = 0; q < QB; ++q) st.O[q][cb] = mfma16<OP>(v, mk4(P[q][0], P[q][1], P[q][2], P[q][3]), st.O[q][cb]);
+    }
 }
 
 // Query rows of a wavefront: 16 QB from `row0` of the unit's; rows past the end are the last one again, and not stored.
@@ -492,7 +480,7 @@ __device__ __forceinline__ void store_rows_of(const PagedAttnArgs& a, const Unit
     for (int q = 0; q < QB; ++q) {
         const RowPlace p = place_of(a, u, hk, row0 + 16 * q + i);
         if (u.pieces > 1) {
-            if (u.slot >= a.part_cap) continue;
+            if (u.slot >= a.part_cap || !p.live) continue;
             const int64_t at = ((int64_t)hk * a.part_cap + u.slot) * rows_of_tile + row_in_tile + 16 * q + i;
             float* const o = a.part_o + at * D + 4 * g;
 #pragma unroll
@@ -532,21 +520,21 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
 
 // ---- few rows: each wavefront of a workgroup has keys of its own ----
 // 16 QB rows; the unit's keys go to the four wavefronts 32 at a time, each of which has LDS of its own for 32 rows of K and V.
-// Its fragments are read into registers at once, and the next keys are on their way while they are multiplied.  The four
-// results are joined in LDS at the end.
+// Memory bounds it: a wavefront reads its fragments into registers as soon as the rows have landed, and asks for the next ones
+// before it multiplies.  Two workgroups a compute unit then keep up to 128 KiB on their way.  The four results are joined in LDS.
 constexpr int kFewWaves = 4;
-template <int D, int QB>
+template <int D>
 constexpr int few_lds() { return kFewWaves * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
 
-template <int D, int OP, int QB>
-__global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const PagedAttnArgs a) {
+template <int D, int OP, int QB, bool RUNS>
+__global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const PagedAttnArgs a) {
     using R = Rows<D>;
-    constexpr int BQ = 16 * QB, KEYS = 32, RPI = R::RPL;
+    constexpr int BQ = 16 * QB, KEYS = 32, RPI = R::RPL, NL = KEYS / RPI, NKF = D / 16, NCB = D / 16;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    uint8_t* const kt = smem + wave * (Rows<D>::k_bytes(KEYS) + Rows<D>::v_bytes(KEYS));
-    uint8_t* const vt = kt + Rows<D>::k_bytes(KEYS);
+    uint8_t* const kt = smem + wave * (R::k_bytes(KEYS) + R::v_bytes(KEYS));
+    uint8_t* const vt = kt + R::k_bytes(KEYS);
     Requests<BQ> requests;
     requests.read(a, 0, lane);
     const Units all = count_units<BQ>(a, requests, lane);
@@ -558,11 +546,6 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const Pa
         const int hk = (int)(id / per_head);
         Unit u;
         if (!find_unit<BQ, false>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
-        RowState<D, QB> st;
-        u32x4 Q[QB][D / 32];
-        const int64_t row0 = (int64_t)u.tile * BQ;
-        load_rows<D, OP, QB>(a, u, hk, row0, i, g, Q, st);
-        st.clear();
         int begin, end;
         key_tiles_of<BQ>(a, u, begin, end);
         const int32_t* const table = a.pages.table + (int64_t)u.r * a.pages.max_pages;
@@ -571,44 +554,114 @@ __global__ void __launch_bounds__(64 * kFewWaves) attn_paged_few_kernel(const Pa
         // the wavefront's blocks of 32 keys: from b on, every kFewWaves-th
         int b = 2 * begin + wave;
         const int blocks = 2 * end;
-        int entry = 0;
-        uint64_t there = 0;
-        auto fetch = [&](int block) {  // its entries are there
-            const int key = KEYS * block + (lane & 31);
+        // RUNS: lane x knows where run x % 2 (16 keys) of the wavefront's block x / 2 from `first` on begins; else lane x knows row x
+        // of block `first`, and asks for the page of the next one.
+        int first = b, entry = 0;
+        uint32_t off16 = 0, there = 0;  // there: of the block fetched last
+        uint64_t ok = 0;
+        auto locate = [&](int block) {
+            first = block;
+            const int key = RUNS ? KEYS * (block + kFewWaves * (lane >> 1)) + 16 * (lane & 1) : KEYS * block + (lane & 31);
+            if (RUNS) entry = entry_of(a.pages, table, key, u.keys);
             const KeyRow kr = row_of(a.pages, entry, key, u.keys);
-            there = __ballot(kr.there) & 0xffffffffull;
+            ok = __ballot(kr.there);
+            off16 = kr.off16;
+            if (!RUNS) entry = entry_of(a.pages, table, key + KEYS * kFewWaves, u.keys);
+        };
+        auto fetch = [&](int block) {
+            if (!RUNS || block - first >= 32 * kFewWaves) locate(block);
+            const int at = RUNS ? (block - first) / kFewWaves * 2 : 0;
+            const int left = u.keys - KEYS * block;
+            there = RUNS ? ((uint32_t)(ok >> at) & 1 ? 0xffffu : 0u) | ((uint32_t)(ok >> at) & 2 ? 0xffff0000u : 0u) : (uint32_t)ok;
+            there = left >= KEYS ? there : left <= 0 ? 0u : there & ((1u << left) - 1);
+            const int in = lane / R::PPR, slot = lane % R::PPR;
+            const uint32_t kp = 16 * R::k_piece(in, slot), vp = 16 * R::v_piece(in, slot);
+            const bool whole = there == 0xffffffffu;
+            if constexpr (RUNS) {
+                const uint32_t row = 16 * a.pages.token16;
 #pragma unroll
-            for (int p = 0; p < KEYS / RPI; ++p) {
-                const int in = lane / R::PPR, slot = lane % R::PPR, row = p * RPI + in;
-                const uint32_t off = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * row, (int)kr.off16);
-                if ((there >> row) & 1) {
-                    __builtin_amdgcn_global_load_lds((gptr_t)(kc + (uint64_t)(off + R::k_piece(in, slot)) * 16),
-                                                     (lptr_t)(kt + p * R::KG), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((gptr_t)(vc + (uint64_t)(off + R::v_piece(in, slot)) * 16),
-                                                     (lptr_t)(vt + p * R::VG), 16, 0, 0);
-                } else {
-                    *reinterpret_cast<u32x4*>(kt + p * R::KG + 16 * lane) = mk4(0, 0, 0, 0);
-                    *reinterpret_cast<u32x4*>(vt + p * R::VG + 16 * lane) = mk4(0, 0, 0, 0);
+                for (int run = 0; run < 2; ++run) {
+                    const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)off16, at + run) * 16;
+#pragma unroll
+                    for (int x = 0; x < NL / 2; ++x) {
+                        const int p = run * (NL / 2) + x;
+                        if (whole || ((there >> (p * RPI + in)) & 1)) {
+                            load_to_lds(kc + from + x * RPI * row, in * row + kp, kt + p * R::KG);
+                            load_to_lds(vc + from + x * RPI * row, in * row + vp, vt + p * R::VG);
+                        } else {
+                            *reinterpret_cast<u32x4*>(kt + p * R::KG + 16 * lane) = mk4(0, 0, 0, 0);
+                            *reinterpret_cast<u32x4*>(vt + p * R::VG + 16 * lane) = mk4(0, 0, 0, 0);
+                        }
+                    }
+                }
+            } else {
+                uint32_t at_row[NL];
+#pragma unroll
+                for (int p = 0; p < NL; ++p) at_row[p] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (p * RPI + in), (int)off16);
+#pragma unroll
+                for (int p = 0; p < NL; ++p) {
+                    if (whole || ((there >> (p * RPI + in)) & 1)) {
+                        load_to_lds(kc + kp + (uint64_t)at_row[p] * 16, kt + p * R::KG);
+                        load_to_lds(vc + vp + (uint64_t)at_row[p] * 16, vt + p * R::VG);
+                    } else {
+                        *reinterpret_cast<u32x4*>(kt + p * R::KG + 16 * lane) = mk4(0, 0, 0, 0);
+                        *reinterpret_cast<u32x4*>(vt + p * R::VG + 16 * lane) = mk4(0, 0, 0, 0);
+                    }
                 }
             }
         };
         if (b < blocks) {
-            entry = entry_of(a.pages, table, KEYS * b + (lane & 31), u.keys);
+            if (!RUNS) entry = entry_of(a.pages, table, KEYS * b + (lane & 31), u.keys);
+            if (RUNS) locate(b);
             fetch(b);
-            entry = entry_of(a.pages, table, KEYS * (b + kFewWaves) + (lane & 31), u.keys);
         }
-        for (; b < blocks; b += kFewWaves) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // (its own rows: no other wavefront waits for them)
-            const int key0 = KEYS * b;
-            bool masked = there != 0xffffffffull;
+        RowState<D, QB> st;
+        u32x4 Q[QB][D / 32];
+        const int64_t row0 = (int64_t)u.tile * BQ;
+        load_rows<D, OP, QB>(a, u, hk, row0, i, g, Q, st);
+        st.clear();
+        int lo = 0, hi = 0x7fffffff;  // keys that every row sees
 #pragma unroll
-            for (int q = 0; q < QB; ++q) masked = masked || st.first[q] > key0 || st.past[q] < key0 + KEYS;
-            tile_step<D, OP, QB, KEYS>(st, Q, kt, vt, key0, there, __any(masked), a.scale_log2, i, g);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (b + kFewWaves < blocks) {
-                fetch(b + kFewWaves);
-                entry = entry_of(a.pages, table, KEYS * (b + 2 * kFewWaves) + (lane & 31), u.keys);
+        for (int q = 0; q < QB; ++q) {
+            lo = max(lo, st.first[q]);
+            hi = min(hi, st.past[q]);
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) {
+            lo = max(lo, __shfl_xor(lo, d));
+            hi = min(hi, __shfl_xor(hi, d));
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        for (; b < blocks; b += kFewWaves) {
+            __builtin_amdgcn_s_waitcnt(0);  // (its own rows: no other wavefront waits for them)
+            const int key0 = KEYS * b;
+            const uint32_t t = there;
+            const bool more = b + kFewWaves < blocks;
+            if (t != 0xffffffffu || key0 < lo || key0 + KEYS > hi) {
+                if (t) {
+                    int ln = lane;
+                    asm volatile("" : "+v"(ln));  // (see opaque_lane in the other kernel)
+                    const int i = ln & 15, g = ln >> 4;
+                    block_step<D, OP, QB, true>(
+                        st, Q, [&](int f) { return k_fragment<D>(kt, 16 * (f & 1), f >> 1, i, g); },
+                        [&](int cb) { return v_fragment<D>(vt, 0, cb, i, g); }, vt, key0, t, a.scale_log2, i, g);
+                }
+                __builtin_amdgcn_s_waitcnt(0);
+                if (more) fetch(b + kFewWaves);
+                continue;
             }
+            u32x4 kf[NKF], vf[NCB];
+#pragma unroll
+            for (int f = 0; f < NKF; ++f) kf[f] = k_fragment<D>(kt, 16 * (f & 1), f >> 1, i, g);
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb) vf[cb] = v_fragment<D>(vt, 0, cb, i, g);
+            __builtin_amdgcn_s_waitcnt(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) fetch(b + kFewWaves);
+            __builtin_amdgcn_sched_barrier(0);
+            block_step<D, OP, QB, false>(st, Q, [&](int f) { return kf[f]; }, [&](int cb) { return vf[cb]; }, vt, key0, t,
+                                         a.scale_log2, i, g);
         }
         // the four wavefronts' rows: maxima, then sums and O relative to the largest
         float l[QB];
@@ -1156,11 +1209,11 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArg
 
 template <int D, int OP, int QB>
 hipError_t launch_few(const PagedAttnArgs& a, int units, hipStream_t s) {
-    static std::atomic<uint64_t> done{0};
-    const auto kern = attn_paged_few_kernel<D, OP, QB>;
-    hipError_t e = allow_dynamic_lds(kern, few_lds<D, QB>(), done);
+    static std::atomic<uint64_t> done_runs{0}, done_rows{0};
+    const auto kern = a.pages.runs ? attn_paged_few_kernel<D, OP, QB, true> : attn_paged_few_kernel<D, OP, QB, false>;
+    hipError_t e = allow_dynamic_lds(kern, few_lds<D>(), a.pages.runs ? done_runs : done_rows);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kFewWaves), (few_lds<D, QB>()), s, a);
+    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kFewWaves), few_lds<D>(), s, a);
     e = hipGetLastError();
     if (e != hipSuccess || !a.pieces) return e;
     hipLaunchKernelGGL((attn_paged_join_kernel<D, 16 * QB>), dim3(units), dim3(256), 0, s, a);
