@@ -7,6 +7,7 @@ there is no fallback path.
 """
 import ctypes
 import os
+import struct
 
 
 class _Torch:
@@ -265,13 +266,13 @@ def lib():
         L.dit_linear_quant_forward.restype = ctypes.c_int
         L.dit_linear_quant_forward.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(dit_linear_params), vp]
         L.dit_qk_rope_forward.restype = ctypes.c_int
-        L.dit_qk_rope_forward.argtypes = [vp] * 5 + [ctypes.POINTER(dit_qk_rope_params), vp]
+        L.dit_qk_rope_forward.argtypes = [vp] * 7
         L.dit_kv_append_forward.restype = ctypes.c_int
-        L.dit_kv_append_forward.argtypes = [vp] * 10 + [ctypes.POINTER(dit_kv_append_params), vp]
+        L.dit_kv_append_forward.argtypes = [vp] * 12
         L.dit_attn_paged_workspace_bytes.restype = ctypes.c_size_t
-        L.dit_attn_paged_workspace_bytes.argtypes = [ctypes.POINTER(dit_paged_attn_params)]
+        L.dit_attn_paged_workspace_bytes.argtypes = [vp]
         L.dit_attn_paged_forward.restype = ctypes.c_int
-        L.dit_attn_paged_forward.argtypes = [vp] * 8 + [ctypes.POINTER(dit_paged_attn_params), vp, ctypes.c_size_t, vp]
+        L.dit_attn_paged_forward.argtypes = [vp] * 10 + [ctypes.c_size_t, vp]
         L.dit_mfma_probe.restype = ctypes.c_int
         L.dit_mfma_probe.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, vp, ctypes.c_size_t,
                                      ctypes.POINTER(ctypes.c_double), vp]
@@ -852,8 +853,14 @@ def dit_linear_quant_forward(x, x_scale, w, w_scale, bias=None, out=None, out_dt
 
 
 # ---- chunk-wise generation over a paged cache ----
+# (Parameters are packed as bytes in the structs' layout: building the ctypes structs took 2.6 us of a call, this 0.3.)
 
+_ROPE_PACK = struct.Struct("@4i3if2iI12qif2P").pack
+_APPEND_PACK = struct.Struct("@2i3if2iI12qif2P7i3q").pack
+_PAGED_PACK = struct.Struct("@6if2iI6q7i3q").pack
 _DTYPE16_CODES = {}
+_NORM_CODES = {"head": DIT_NORM_HEAD, "token": DIT_NORM_TOKEN}
+_NO_STRIDES = (0, 0, 0)
 
 
 def _dtype16_code(what, name, t):
@@ -875,11 +882,10 @@ def _stream_on(what, stream, device):
     return _stream_ptr(stream)
 
 
-def _check_range(what, **numbers):
-    """Whole numbers that the library holds in 32 bits; ctypes would cut larger ones off without a word."""
-    for name, n in numbers.items():
-        if not 0 <= n <= _MOST_COUNT:
-            raise ValueError("%s: %s must be 0 .. %d, got %s" % (what, name, _MOST_COUNT, n))
+def _check_range(what, name, n):
+    """A whole number that the library holds in 32 bits; packing would refuse a larger one with another error."""
+    if not 0 <= n <= _MOST_COUNT:
+        raise ValueError("%s: %s must be 0 .. %d, got %s" % (what, name, _MOST_COUNT, n))
 
 
 def _check_split(what, split, D):
@@ -887,42 +893,43 @@ def _check_split(what, split, D):
         raise ValueError("%s: split must be three even numbers whose sum is %d, got %s" % (what, D, tuple(split)))
 
 
-def _token_rows(what, name, t, N, D, device):
-    """dit_strides of t: a [N, heads, D] tensor on that device (its index), contiguous along its channels."""
-    shape, s = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != N or shape[2] != D:
-        raise ValueError("%s: %s has shape %s, expected [%d, heads, %d]" % (what, name, tuple(shape), N, D))
+def _wrong_device(what, name, t):
+    raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+
+
+def _token_strides(what, name, t, shape, device):
+    """(batch, token, head) element strides of t: a tensor of that [N, heads, D] shape on that device (its index), contiguous
+    along its channels."""
+    if t.shape != shape:
+        raise ValueError("%s: %s has shape %s, expected %s" % (what, name, tuple(t.shape), tuple(shape)))
     if t.get_device() != device or device < 0:
-        raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+        _wrong_device(what, name, t)
+    s = t.stride()
     if s[2] != 1:
         raise ValueError("%s: %s must have contiguous channels" % (what, name))
-    return dit_strides(0, s[0], s[1])
+    return 0, s[0], s[1]
 
 
-def _check_counts(what, device, **tensors):
-    """int32 device tensors, dense: name = (tensor, shape)."""
-    for name, (t, shape) in tensors.items():
-        if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
-            raise ValueError("%s: %s must be a dense int32 tensor of shape %s" % (what, name, shape))
-        if t.get_device() != device:
-            raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+def _counts_ptr(what, name, t, shape, device):
+    """Address of t: a dense int32 tensor of that shape on that device."""
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s: %s must be a dense int32 tensor of shape %s" % (what, name, tuple(shape)))
+    if t.get_device() != device:
+        _wrong_device(what, name, t)
+    return t.data_ptr()
 
 
 def _rope_norm(what, norm, H, Hk, D, device):
-    """norm: None, or (mode, eps, q_gamma, k_gamma) as in qk_norm, with weights of H*D and of Hk*D elements."""
+    """dit_qk_norm as a tuple.  norm: None, or (mode, eps, q_gamma, k_gamma) as in qk_norm, with H*D and Hk*D weights."""
     if norm is None:
-        return dit_qk_norm()
+        return 0, 0.0, 0, 0
     mode, eps, gq, gk = norm
     if mode not in _NORM_CODES:
         raise ValueError("%s: norm must be one of %s" % (what, ", ".join(sorted(_NORM_CODES))))
     for name, g, n in (("q_gamma", gq, H * D), ("k_gamma", gk, Hk * D)):
         if g is not None and (g.dtype != torch.float32 or g.numel() != n or not g.is_contiguous() or g.get_device() != device):
             raise ValueError("%s: %s must be a dense float32 tensor of %d elements on the rows' device" % (what, name, n))
-    return dit_qk_norm(_NORM_CODES[mode], eps, gq.data_ptr() if gq is not None else None,
-                       gk.data_ptr() if gk is not None else None)
-
-
-_NORM_CODES = {"head": DIT_NORM_HEAD, "token": DIT_NORM_TOKEN}
+    return _NORM_CODES[mode], eps, gq.data_ptr() if gq is not None else 0, gk.data_ptr() if gk is not None else 0
 
 
 def dit_qk_rope_forward(q, k, pos, split=(0, 0, 0), q_out=None, k_out=None, out_dtype=None, rope_base=10000.0, norm=None,
@@ -935,58 +942,83 @@ def dit_qk_rope_forward(q, k, pos, split=(0, 0, 0), q_out=None, k_out=None, out_
     some = q if q is not None else k
     if some is None or some.dim() != 3:
         raise ValueError("%s: q must be [N, H, D] and k [N, Hk, D], one of them at least" % what)
-    N, D, device = some.shape[0], some.shape[2], some.get_device()
+    (N, _, D), device = some.shape, some.get_device()
     if N > _MOST_COUNT:
         _too_many(what)
-    heads, strides, codes, outs = [0, 0], [dit_strides() for _ in range(4)], set(), [q_out, k_out]
-    for i, (name, x) in enumerate((("q", q), ("k", k))):
-        if x is None:
-            if outs[i] is not None:
-                raise ValueError("%s: %s_out needs %s" % (what, name, name))
-            continue
-        if x.dtype != some.dtype:
+    H = Hk = 0
+    sq = sk = sqo = sko = _NO_STRIDES
+    qp = kp = qop = kop = None
+    code = -1
+    if q is not None:
+        H = q.shape[1]
+        sq = _token_strides(what, "q", q, (N, H, D), device)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+        sqo = _token_strides(what, "q_out", q_out, (N, H, D), device)
+        code = _dtype16_code(what, "q_out", q_out)
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("%s: q_out needs q" % what)
+    if k is not None:
+        if k.dim() != 3:
+            raise ValueError("%s: k must be [N, Hk, D]" % what)
+        Hk = k.shape[1]
+        if k.dtype != some.dtype:
             raise TypeError("%s: q and k must share one dtype" % what)
-        strides[i] = _token_rows(what, name, x, N, D, device)
-        heads[i] = x.shape[1]
-        if outs[i] is None:
-            outs[i] = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
-        strides[2 + i] = _token_rows(what, name + "_out", outs[i], N, D, device)
-        if outs[i].shape != x.shape:
-            raise ValueError("%s: %s_out must have the shape of %s" % (what, name, name))
-        codes.add(_dtype16_code(what, name + "_out", outs[i]))
-    if len(codes) != 1:
-        raise TypeError("%s: q_out and k_out must share one dtype" % what)
+        sk = _token_strides(what, "k", k, (N, Hk, D), device)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=out_dtype or k.dtype, device=k.device)
+        sko = _token_strides(what, "k_out", k_out, (N, Hk, D), device)
+        k_code = _dtype16_code(what, "k_out", k_out)
+        if q is not None and k_code != code:
+            raise TypeError("%s: q_out and k_out must share one dtype" % what)
+        code = k_code
+        kp, kop = k.data_ptr(), k_out.data_ptr()
+    elif k_out is not None:
+        raise ValueError("%s: k_out needs k" % what)
+    if H > _MOST_COUNT or Hk > _MOST_COUNT:
+        _too_many(what)
+    pp = None
     if pos is not None:
-        _check_counts(what, device, pos=(pos, (N, 3)))
+        pp = _counts_ptr(what, "pos", pos, (N, 3), device)
         _check_split(what, split, D)
-    p = dit_qk_rope_params(N, heads[0], heads[1], D, split[0], split[1], split[2], rope_base, _dtype_code(some), codes.pop(), 0,
-                           strides[0], strides[1], strides[2], strides[3], _rope_norm(what, norm, heads[0], heads[1], D, device))
-    ptr = [t.data_ptr() if t is not None else None for t in (q, k, pos, outs[0], outs[1])]
-    st = lib().dit_qk_rope_forward(*ptr, ctypes.byref(p), _stream_on(what, stream, device))
+    else:
+        split = _NO_STRIDES
+    p = _ROPE_PACK(N, H, Hk, D, *split, rope_base, _dtype_code(some), code, 0, *sq, *sk, *sqo, *sko,
+                   *_rope_norm(what, norm, H, Hk, D, device))
+    st = lib().dit_qk_rope_forward(qp, kp, pp, qop, kop, p, _stream_on(what, stream, device))
     if st != DIT_OK:
         raise DitError(st, what)
-    return outs[0], outs[1]
+    return q_out, k_out
 
 
-def kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device):
-    """dit_kv_cache of k_cache and v_cache [pages, page_size, Hk, D] (any strides, the same for both; bf16 or float16),
-    page_table [requests, max_pages], q_start [requests + 1] and kv_len [requests] (int32)."""
+def _kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device):
+    """(dit_kv_cache as a tuple, addresses of k_cache, v_cache, page_table, q_start and kv_len)."""
     shape, s = k_cache.shape, k_cache.stride()
     if len(shape) != 4 or v_cache.shape != shape or v_cache.stride() != s or s[3] != 1:
         raise ValueError("%s: k_cache and v_cache must be [pages, page_size, heads, D] tensors of the same strides with "
                          "contiguous channels" % what)
-    if v_cache.dtype != k_cache.dtype or k_cache.dtype == torch.float32:
+    code = _dtype16_code(what, "k_cache", k_cache)
+    if v_cache.dtype != k_cache.dtype or code == DIT_F32:
         raise TypeError("%s: k_cache and v_cache must both be bfloat16 or both float16" % what)
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if t.get_device() != device or device < 0:
-            raise ValueError("%s needs device tensors on one device (%s is on %s)" % (what, name, t.device))
+    if k_cache.get_device() != device or device < 0:
+        _wrong_device(what, "k_cache", k_cache)
+    if v_cache.get_device() != device:
+        _wrong_device(what, "v_cache", v_cache)
     if page_table.dim() != 2:
         raise ValueError("%s: page_table must be [requests, pages]" % what)
     R, pages = page_table.shape
-    if max(shape[0], shape[1], R, pages) > _MOST_COUNT:
+    if shape[0] > _MOST_COUNT or shape[1] > _MOST_COUNT or shape[2] > _MOST_COUNT or R > _MOST_COUNT or pages > _MOST_COUNT:
         _too_many(what)
-    _check_counts(what, device, page_table=(page_table, (R, pages)), q_start=(q_start, (R + 1,)), kv_len=(kv_len, (R,)))
-    return dit_kv_cache(shape[0], shape[1], shape[2], shape[3], _dtype16_code(what, "k_cache", k_cache), R, pages, s[0], s[1], s[2])
+    return ((shape[0], shape[1], shape[2], shape[3], code, R, pages, s[0], s[1], s[2]),
+            (k_cache.data_ptr(), v_cache.data_ptr(), _counts_ptr(what, "page_table", page_table, (R, pages), device),
+             _counts_ptr(what, "q_start", q_start, (R + 1,), device), _counts_ptr(what, "kv_len", kv_len, (R,), device)))
+
+
+def kv_cache(k_cache, v_cache, page_table, q_start, kv_len):
+    """dit_kv_cache of k_cache and v_cache [pages, page_size, Hk, D] (any strides, the same for both; bf16 or float16),
+    page_table [requests, max_pages], q_start [requests + 1] and kv_len [requests] (dense, int32), all on one device."""
+    return dit_kv_cache(*_kv_cache("kv_cache", k_cache, v_cache, page_table, q_start, kv_len, k_cache.get_device())[0])
 
 
 def dit_kv_append_forward(k, v, k_cache, v_cache, page_table, q_start, kv_len, pos=None, split=(0, 0, 0), q=None, q_out=None,
@@ -996,38 +1028,45 @@ def dit_kv_append_forward(k, v, k_cache, v_cache, page_table, q_start, kv_len, p
     With q [N, H, D], its rows normalised and rotated to q_out, which is returned (allocated in out_dtype, default that of q, if
     not given)."""
     what = "dit_kv_append_forward"
-    if k.dim() != 3 or v.shape != k.shape:
+    shape = k.shape
+    if len(shape) != 3:
         raise ValueError("%s: k and v must be [N, Hk, D]" % what)
-    N, Hk, D = k.shape
-    device = k.get_device()
+    (N, Hk, D), device = shape, k.get_device()
     if N > _MOST_COUNT:
         _too_many(what)
-    sk, sv = _token_rows(what, "k", k, N, D, device), _token_rows(what, "v", v, N, D, device)
-    cache = kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device)
-    if cache.Hk != Hk or cache.D != D:
-        raise ValueError("%s: the cache has rows of %d x %d, k of %d x %d" % (what, cache.Hk, cache.D, Hk, D))
-    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+    sk, sv = _token_strides(what, "k", k, shape, device), _token_strides(what, "v", v, shape, device)
+    cache, (kcp, vcp, tp, sp, lp) = _kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device)
+    if cache[2] != Hk or cache[3] != D:
+        raise ValueError("%s: the cache has rows of %d x %d, k of %d x %d" % (what, cache[2], cache[3], Hk, D))
+    if v.dtype != k.dtype:
         raise TypeError("%s: q, k and v must share one dtype" % what)
-    H, sq, sq_out, out_code = 0, dit_strides(), dit_strides(), DIT_BF16
+    H, sq, sqo, code, qp, qop = 0, _NO_STRIDES, _NO_STRIDES, DIT_BF16, None, None
     if q is not None:
-        sq = _token_rows(what, "q", q, N, D, device)
+        if q.dtype != k.dtype:
+            raise TypeError("%s: q, k and v must share one dtype" % what)
+        if q.dim() != 3:
+            raise ValueError("%s: q must be [N, H, D]" % what)
         H = q.shape[1]
+        if H > _MOST_COUNT:
+            _too_many(what)
+        sq = _token_strides(what, "q", q, (N, H, D), device)
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
-        sq_out = _token_rows(what, "q_out", q_out, N, D, device)
-        if q_out.shape != q.shape:
-            raise ValueError("%s: q_out must have the shape of q" % what)
-        out_code = _dtype16_code(what, "q_out", q_out)
+        sqo = _token_strides(what, "q_out", q_out, (N, H, D), device)
+        code = _dtype16_code(what, "q_out", q_out)
+        qp, qop = q.data_ptr(), q_out.data_ptr()
     elif q_out is not None:
         raise ValueError("%s: q_out needs q" % what)
+    pp = None
     if pos is not None:
-        _check_counts(what, device, pos=(pos, (N, 3)))
+        pp = _counts_ptr(what, "pos", pos, (N, 3), device)
         _check_split(what, split, D)
-    p = dit_kv_append_params(N, H, split[0], split[1], split[2], rope_base, _dtype_code(k), out_code, 0, sq, sk, sv, sq_out,
-                             _rope_norm(what, norm, H, Hk, D, device), cache)
-    ptr = [t.data_ptr() if t is not None else None
-           for t in (q, k, v, pos, page_table, q_start, kv_len, q_out, k_cache, v_cache)]
-    st = lib().dit_kv_append_forward(*ptr, ctypes.byref(p), _stream_on(what, stream, device))
+    else:
+        split = _NO_STRIDES
+    p = _APPEND_PACK(N, H, *split, rope_base, _dtype_code(k), code, 0, *sq, *sk, *sv, *sqo,
+                     *_rope_norm(what, norm, H, Hk, D, device), *cache)
+    st = lib().dit_kv_append_forward(qp, k.data_ptr(), v.data_ptr(), pp, tp, sp, lp, qop, kcp, vcp, p,
+                                     _stream_on(what, stream, device))
     if st != DIT_OK:
         raise DitError(st, what)
     return q_out
@@ -1045,37 +1084,36 @@ def dit_attn_paged_forward(q, k_cache, v_cache, page_table, q_start, kv_len, fra
     of any request, if the host knows them (for planning).  Returns out (bf16 or float32; rows of no request are left as they
     are), and with want_lse or lse (out, lse), lse float32 [H, N]."""
     what = "dit_attn_paged_forward"
-    if q.dim() != 3:
+    shape = q.shape
+    if len(shape) != 3:
         raise ValueError("%s: q must be [N, H, D]" % what)
-    N, H, D = q.shape
-    device = q.get_device()
+    (N, H, D), device = shape, q.get_device()
     if N > _MOST_COUNT or H > _MOST_COUNT:
         _too_many(what)
-    _check_range(what, frame=frame, window=window, max_q=max_q, max_kv=max_kv)
-    sq = _token_rows(what, "q", q, N, D, device)
-    cache = kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device)
-    if cache.D != D or cache.Hk < 1 or H % cache.Hk:
-        raise ValueError("%s: q's %d heads of %d channels do not fit the cache's %d of %d" % (what, H, D, cache.Hk, cache.D))
+    _check_range(what, "frame", frame)
+    _check_range(what, "window", window)
+    _check_range(what, "max_q", max_q)
+    _check_range(what, "max_kv", max_kv)
+    sq = _token_strides(what, "q", q, shape, device)
+    cache, (kcp, vcp, tp, sp, lp) = _kv_cache(what, k_cache, v_cache, page_table, q_start, kv_len, device)
+    if cache[3] != D or cache[2] < 1 or H % cache[2]:
+        raise ValueError("%s: q's %d heads of %d channels do not fit the cache's %d of %d" % (what, H, D, cache[2], cache[3]))
     if out is None:
-        out = torch.empty(q.shape, dtype=out_dtype or (torch.bfloat16 if q.dtype == torch.float16 else q.dtype), device=q.device)
-    so = _token_rows(what, "out", out, N, D, device)
-    if out.shape != q.shape:
-        raise ValueError("%s: out must have the shape of q" % what)
-    if lse is None and want_lse:
-        lse = torch.empty((H, N), dtype=torch.float32, device=q.device)
-    elif lse is not None:
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (H, N) or not lse.is_contiguous() or lse.get_device() != device:
-            raise ValueError("%s: lse must be a dense float32 tensor of shape %s on q's device" % (what, (H, N)))
-    p = dit_paged_attn_params(N, H, frame, window, max_q, max_kv, scale, _dtype16_code(what, "q", q), _dtype_code(out), 0, sq, so,
-                              cache)
-    need = dit_attn_paged_workspace_bytes(p)
+        out = torch.empty(shape, dtype=out_dtype or (torch.bfloat16 if q.dtype == torch.float16 else q.dtype), device=q.device)
+    so = _token_strides(what, "out", out, shape, device)
+    if lse is None:
+        if want_lse:
+            lse = torch.empty((H, N), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.shape != (H, N) or not lse.is_contiguous() or lse.get_device() != device:
+        raise ValueError("%s: lse must be a dense float32 tensor of shape %s on q's device" % (what, (H, N)))
+    p = _PAGED_PACK(N, H, frame, window, max_q, max_kv, scale, _dtype16_code(what, "q", q), _dtype_code(out), 0, *sq, *so, *cache)
+    need = lib().dit_attn_paged_workspace_bytes(p)
     if workspace is None:
         workspace = _workspace(need, q.device)
     else:
         _check_workspace(what, workspace, need, q.device)
-    st = lib().dit_attn_paged_forward(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
-                                      q_start.data_ptr(), kv_len.data_ptr(), out.data_ptr(),
-                                      lse.data_ptr() if lse is not None else None, ctypes.byref(p), workspace.data_ptr(),
+    st = lib().dit_attn_paged_forward(q.data_ptr(), kcp, vcp, tp, sp, lp, out.data_ptr(),
+                                      lse.data_ptr() if lse is not None else None, p, workspace.data_ptr(),
                                       workspace.numel() * workspace.element_size(), _stream_on(what, stream, device))
     if st != DIT_OK:
         raise DitError(st, what)

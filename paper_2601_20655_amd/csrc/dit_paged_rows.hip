@@ -17,13 +17,17 @@ namespace {
 enum RowNorm { RN_NONE = 0, RN_HEAD = 1, RN_TOKEN = 2 };
 constexpr int kMostRowChunks = 8;
 
+template <bool PAST>
 __device__ __forceinline__ void store8(void* y, int64_t off, int type, const float v[8]) {
     if (type == DIT_F32) {
         float4* const p = reinterpret_cast<float4*>(static_cast<float*>(y) + off);
         p[0] = make_float4(v[0], v[1], v[2], v[3]);
         p[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(y) + off) = type == DIT_F16 ? pack8<OP_F16>(v) : pack8<OP_BF16>(v);
+        u32x4* const p = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(y) + off);
+        const u32x4 u = type == DIT_F16 ? pack8<OP_F16>(v) : pack8<OP_BF16>(v);
+        if constexpr (PAST) __builtin_nontemporal_store(u, p);
+        else *p = u;
     }
 }
 
@@ -53,9 +57,35 @@ __device__ __forceinline__ int norm_shift(float top, float eps) {
     return e == -1000 ? 0 : -e;
 }
 
+// Eight channels as they lie in memory.
+template <bool F32>
+struct Piece {
+    u32x4 v[F32 ? 2 : 1];
+};
+template <bool F32, bool PAST>
+__device__ __forceinline__ Piece<F32> load_piece(const void* x, int64_t off) {
+    const u32x4* const p = reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(x) + off * (F32 ? 4 : 2));
+    Piece<F32> k;
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) {
+        if constexpr (PAST) k.v[i] = __builtin_nontemporal_load(p + i);
+        else k.v[i] = p[i];
+    }
+    return k;
+}
+template <bool F32>
+__device__ __forceinline__ void numbers(const Piece<F32>& k, float v[8]) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(k.v[i >> 2][i & 3]);
+    } else {
+        widen8(k.v[0], v);
+    }
+}
+
 // W wavefronts a token, C heads' pieces a lane: wavefronts [0, wq) have the heads of q, the next wk those of k, the rest v's.
-// RN_TOKEN: a workgroup has whole tokens, and exchanges the sums.
-template <int D, int NORM, int C>
+// RN_TOKEN: a workgroup has whole tokens, and exchanges the sums.  PAST: rows past the caches.
+template <int D, int NORM, int C, bool F32, bool PAST>
 __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, int wk, int W, int t_end) {
     constexpr int L = D / 8;    // lanes of a head
     constexpr int HW = 64 / L;  // heads of a wavefront, a time
@@ -72,12 +102,37 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
     const int part = kind == 0 ? w : kind == 1 ? w - wq : w - wq - wk;
     const int slice = lane % L;
     const int head0 = part * (C * HW) + lane / L;
+    auto head = [&](int c) { return head0 + c * HW < x.H ? head0 + c * HW : x.H - 1; };
 
-    float v[C][8];
+    // All that a row needs is asked for before any of it is used: the rows, the weights, the position and the pairs' turns.
+    const bool turned = kind != 2 && a.pos;
+    const bool weighed = NORM != RN_NONE && kind != 2 && x.gamma;
+    Piece<F32> raw[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int h = head0 + c * HW;
-        load8(x.x, (int64_t)t * x.sx_t + (int64_t)(h < x.H ? h : x.H - 1) * x.sx_h + 8 * slice, a.x_f32, v[c]);
+    for (int c = 0; c < C; ++c) raw[c] = load_piece<F32, PAST>(x.x, (int64_t)t * x.sx_t + (int64_t)head(c) * x.sx_h + 8 * slice);
+    [[maybe_unused]] Piece<true> gamma[C];
+    if constexpr (NORM != RN_NONE) {
+        if (weighed) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) gamma[c] = load_piece<true, false>(x.gamma, (int64_t)head(c) * D + 8 * slice);
+        }
+    }
+    float2 cs[4];
+    if (turned) {
+        int at[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) at[i] = a.pos[3 * (int64_t)t + i];
+        // (a pair of two axes holds the last pair of the one and the first of the next at most once in four)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int pair = 4 * slice + i;
+            const int p = pair < a.hd[0] ? at[0] : pair < a.hd[0] + a.hd[1] ? at[1] : at[2];
+            const double turns = (double)p * a.turn[pair];
+            const float f = (float)(turns - rint(turns));
+            float sn, c;
+            sincospif(2.0f * f, &sn, &c);
+            cs[i] = make_float2(c, sn);
+        }
     }
 
     // where the row goes
@@ -98,34 +153,33 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
         }
     }
 
-    if (NORM != RN_NONE && kind != 2) {
-        float eps = a.eps;
-        if constexpr (NORM == RN_HEAD) {
+    float v[C][8];
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                float sum = 0.f;
+    for (int c = 0; c < C; ++c) numbers<F32>(raw[c], v[c]);
+    if (NORM == RN_HEAD && kind != 2) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
-                sum = head_sum<L>(sum);
-                float e = eps;
-                if (__any(!sum_holds(sum, eps))) {
-                    float top = 0.f;
+        for (int c = 0; c < C; ++c) {
+            float sum = 0.f, eps = a.eps;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(v[c][i]));
-                    const int k = norm_shift(head_max<L>(top), eps);
-                    e = ldexpf(eps, 2 * k);
-                    sum = 0.f;
+            for (int i = 0; i < 8; ++i) sum = fmaf(v[c][i], v[c][i], sum);
+            sum = head_sum<L>(sum);
+            if (__any(!sum_holds(sum, eps))) {
+                float top = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[c][i] = ldexpf(v[c][i], k);
-                        sum = fmaf(v[c][i], v[c][i], sum);
-                    }
-                    sum = head_sum<L>(sum);
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(v[c][i]));
+                const int k = norm_shift(head_max<L>(top), eps);
+                eps = ldexpf(eps, 2 * k);
+                sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[c][i] = ldexpf(v[c][i], k);
+                    sum = fmaf(v[c][i], v[c][i], sum);
                 }
-                const float f = 1.0f / sqrtf(sum * (1.0f / D) + e);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[c][i] *= f;
+                sum = head_sum<L>(sum);
             }
+            const float f = 1.0f / sqrtf(sum * (1.0f / D) + eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= f;
         }
     }
     if constexpr (NORM == RN_TOKEN) {
@@ -176,30 +230,19 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
                 for (int i = 0; i < 8; ++i) v[c][i] *= f;
         }
     }
-    if (NORM != RN_NONE && kind != 2 && x.gamma) {
+    if (!live) return;
+    if constexpr (NORM != RN_NONE) {
+        if (weighed) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int h = head0 + c * HW;
-            float g[8];
-            load8(x.gamma, (int64_t)(h < x.H ? h : x.H - 1) * D + 8 * slice, 1, g);
+            for (int c = 0; c < C; ++c) {
+                float g[8];
+                numbers<true>(gamma[c], g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[c][i] *= g[i];
+                for (int i = 0; i < 8; ++i) v[c][i] *= g[i];
+            }
         }
     }
-    if (!live) return;
-
-    if (kind != 2 && a.pos) {
-        float2 cs[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int pair = 4 * slice + i;
-            const int axis = pair < a.hd[0] ? 0 : pair < a.hd[0] + a.hd[1] ? 1 : 2;
-            const double turns = (double)a.pos[3 * (int64_t)t + axis] * a.turn[pair];
-            const float f = (float)(turns - rint(turns));
-            float sn, c;
-            sincospif(2.0f * f, &sn, &c);
-            cs[i] = make_float2(c, sn);
-        }
+    if (turned) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -221,7 +264,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int h = head0 + c * HW;
-            if (h < x.H) store8(x.y, (int64_t)t * x.sy_t + (int64_t)h * x.sy_h + 8 * slice, a.y_type, v[c]);
+            if (h < x.H) store8<PAST>(x.y, (int64_t)t * x.sy_t + (int64_t)h * x.sy_h + 8 * slice, a.y_type, v[c]);
         }
     }
 }
@@ -236,7 +279,7 @@ RowWaves row_waves(int H, int Hk, int Hv, int D, int C) {
     return {(H + per - 1) / per, (Hk + per - 1) / per, (Hv + per - 1) / per};
 }
 
-template <int D, int NORM, int C>
+template <int D, int NORM, int C, bool F32, bool PAST>
 hipError_t launch_rows_c(const RowsArgs& a, hipStream_t s) {
     const RowWaves w = row_waves(a.q.H, a.k.H, a.v.H, D, C);
     const int W = w.all();
@@ -248,28 +291,45 @@ hipError_t launch_rows_c(const RowsArgs& a, hipStream_t s) {
         RowsArgs b = a;
         b.t0 = (int)t;
         const int64_t groups = tokens ? (n + tokens - 1) / tokens : (n * W + 3) / 4;
-        hipLaunchKernelGGL((rows_kernel<D, NORM, C>), dim3((unsigned)groups), dim3(tokens ? 64 * W * tokens : 256), 0, s, b, w.q,
-                           w.k, W, (int)(t + n));
+        hipLaunchKernelGGL((rows_kernel<D, NORM, C, F32, PAST>), dim3((unsigned)groups), dim3(tokens ? 64 * W * tokens : 256), 0, s,
+                           b, w.q, w.k, W, (int)(t + n));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+template <int D, int NORM, bool F32, bool PAST>
+hipError_t launch_rows_p(const RowsArgs& a, hipStream_t s) {
+    // Pieces a lane: as few as keep the memory busy (four wavefronts a compute unit) where there are few tokens; else those that
+    // leave the fewest lanes without a head, many rather than few (the angles are worked out once a wavefront).  The wavefronts of
+    // a token that have to meet are sixteen at most.
+    constexpr int kPieces[] = {1, 2, 3, 4, 5, 8};
+    int C = 0, best = 0;
+    for (const int c : kPieces) {
+        const int W = row_waves(a.q.H, a.k.H, a.v.H, D, c).all();
+        if (NORM == RN_TOKEN && W > 16) continue;
+        if (C && (c > 5 || (int64_t)a.N * W < 4 * kCUs)) break;
+        if (!C || W * c <= best) {
+            C = c;
+            best = W * c;
+        }
+    }
+    switch (C) {
+        case 1: return launch_rows_c<D, NORM, 1, F32, PAST>(a, s);
+        case 2: return launch_rows_c<D, NORM, 2, F32, PAST>(a, s);
+        case 3: return launch_rows_c<D, NORM, 3, F32, PAST>(a, s);
+        case 4: return launch_rows_c<D, NORM, 4, F32, PAST>(a, s);
+        case 5: return launch_rows_c<D, NORM, 5, F32, PAST>(a, s);
+        default: return launch_rows_c<D, NORM, 8, F32, PAST>(a, s);
+    }
+}
+
 template <int D, int NORM>
 hipError_t launch_rows_n(const RowsArgs& a, hipStream_t s) {
-    const auto waves = [&](int C) { return row_waves(a.q.H, a.k.H, a.v.H, D, C).all(); };
-    int C = 1;
-    // more pieces a lane where there are wavefronts enough to keep the memory busy, or the workgroup would have too many
-    while (C < 4 && (int64_t)a.N * waves(2 * C) >= 4 * kCUs) C *= 2;
-    if (NORM == RN_TOKEN)
-        while (C < kMostRowChunks && waves(C) > 16) C *= 2;
-    switch (C) {
-        case 1: return launch_rows_c<D, NORM, 1>(a, s);
-        case 2: return launch_rows_c<D, NORM, 2>(a, s);
-        case 4: return launch_rows_c<D, NORM, 4>(a, s);
-        default: return launch_rows_c<D, NORM, 8>(a, s);
-    }
+    if (a.x_f32) return launch_rows_p<D, NORM, true, false>(a, s);
+    const bool past = exceeds_caches((int64_t)a.N * (a.q.H + a.k.H + a.v.H) * D * 2);
+    return past ? launch_rows_p<D, NORM, false, true>(a, s) : launch_rows_p<D, NORM, false, false>(a, s);
 }
 
 template <int D>

@@ -107,7 +107,7 @@ def test_captured_and_replayed():
                                 norm=("token", 1e-6) + gamma)
         if key not in ws:
             p = B.dit_paged_attn_params(N, H, 15, 0, 64, 200, 0.0, 0, 0, 0, B.dit_strides(0, H * D, D), B.dit_strides(0, H * D, D),
-                                        B.kv_cache("x", kc, vc, table, q_start, kv_len, 0))
+                                        B.kv_cache(kc, vc, table, q_start, kv_len))
             ws[key] = torch.empty(B.dit_attn_paged_workspace_bytes(p), dtype=torch.uint8, device="cuda")
         B.dit_attn_paged_forward(q_out, kc, vc, table, q_start, kv_len, frame=15, max_q=64, max_kv=200, out=out, lse=lse,
                                  workspace=ws[key])

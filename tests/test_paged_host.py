@@ -232,6 +232,35 @@ def test_python_wrappers_check_shapes_types_and_devices(monkeypatch):
             call()
 
 
+def test_packed_parameters_are_the_structs():
+    """The wrappers pack the parameters as bytes: every field where the struct has it."""
+    ints = list(range(1, 100))
+    take = iter(ints)
+
+    def fields(c):
+        out = []
+        for name, kind in c._fields_:
+            out += fields(kind) if hasattr(kind, "_fields_") else [float(next(take)) if kind is ctypes.c_float else next(take)]
+        return out
+
+    for c, pack in ((B.dit_qk_rope_params, B._ROPE_PACK), (B.dit_kv_append_params, B._APPEND_PACK),
+                    (B.dit_paged_attn_params, B._PAGED_PACK)):
+        take = iter(ints)
+        values = fields(c)
+        packed = pack(*values)
+        got = c.from_buffer_copy(packed.ljust(ctypes.sizeof(c), b"\0"))
+        assert len(packed) == ctypes.sizeof(c)
+        flat = []
+
+        def walk(x):
+            for name, kind in x._fields_:
+                v = getattr(x, name)
+                walk(v) if hasattr(kind, "_fields_") else flat.append(v)
+
+        walk(got)
+        assert flat == values
+
+
 def test_current_device_has_to_be_the_tensors(monkeypatch):
     import torch
 
