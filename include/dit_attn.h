@@ -625,7 +625,7 @@ dit_status dit_kv_append_forward(const void *q, const void *k, const void *v, co
  * Deterministic: the same arguments give the same bits.  A row's bits depend on the other requests' counts too (pieces).
  * workspace: dit_attn_paged_workspace_bytes(p) bytes (the same for any counts), 256-byte aligned.
  * Errors: NULL q, caches, page_table, q_start, kv_len, out or p, N < 0, H no multiple of Hk, a negative frame, window, max_q or max_kv, window
- * without frame, a bad dtype, nonzero flags, rows that overlap -> DIT_ERR_INVALID_ARG; D other than 64 or 128, N * H / Hk of 2^31
+ * without frame, a bad dtype, nonzero flags, rows that overlap -> DIT_ERR_INVALID_ARG; D other than 64 or 128, N * H + n_requests * Hk of 2^30
  * or more, a cache of more than 64 GiB -> DIT_ERR_UNSUPPORTED; alignment (4 bytes for counts, table and lse) -> DIT_ERR_ALIGNMENT; DIT_ERR_WORKSPACE.  N = 0 does nothing.
  */
 typedef struct {

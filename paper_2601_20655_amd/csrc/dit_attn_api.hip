@@ -1594,7 +1594,7 @@ dit_status check_paged(const dit_paged_attn_params* p, dit::PagedPlan* plan) {
     if (st != DIT_OK) return st;
     if (p->H % p->cache.Hk) return DIT_ERR_INVALID_ARG;
     if (!rows_ok(p->sq, p->H, p->cache.D, p->N) || !rows_ok(p->so, p->H, p->cache.D, p->N)) return DIT_ERR_INVALID_ARG;
-    if ((int64_t)p->N * (p->H / p->cache.Hk) > 0x7fffffff) return DIT_ERR_UNSUPPORTED;
+    if ((int64_t)p->N * p->H + (int64_t)p->cache.n_requests * p->cache.Hk >= 1 << 30) return DIT_ERR_UNSUPPORTED;
     int64_t keys = (int64_t)p->cache.max_pages * p->cache.page_size;
     if (p->max_kv && p->max_kv < keys) keys = p->max_kv;
     if (keys > 0x7fffffff) keys = 0x7fffffff;

@@ -134,12 +134,18 @@ __device__ __forceinline__ Load load_of(const PagedAttnArgs& a, int r, bool live
     return l;
 }
 
-__device__ __forceinline__ int scan_add(int x, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+// Sums of the lanes up to each: within rows of 16 lanes, then row to row (a lane that has no neighbour there adds 0).
+template <class T>
+__device__ __forceinline__ T scan_add(T x) {
+#define DIT_ADD_LANE(ctrl, rows, zero) \
+    x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, rows, 0xf, zero))
+    DIT_ADD_LANE(0x111, 0xf, true);   // row_shr:1
+    DIT_ADD_LANE(0x112, 0xf, true);   // row_shr:2
+    DIT_ADD_LANE(0x114, 0xf, true);   // row_shr:4
+    DIT_ADD_LANE(0x118, 0xf, true);   // row_shr:8
+    DIT_ADD_LANE(0x142, 0xa, false);  // row_bcast:15, to rows 1 and 3
+    DIT_ADD_LANE(0x143, 0xc, false);  // row_bcast:31, to rows 2 and 3
+#undef DIT_ADD_LANE
     return x;
 }
 
@@ -154,10 +160,9 @@ struct Requests {
         l = load_of<BQ>(a, r0 + lane, r0 + lane < a.pages.n_requests, q0, n, keys);
     }
 };
-__device__ __forceinline__ int sum_of_lanes(int x) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return __builtin_amdgcn_readfirstlane(x);
+template <class T>
+__device__ __forceinline__ T sum_of_lanes(T x) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scan_add(x)), 63));
 }
 
 // The key head's units: `c` key tiles of a piece, at most, units in all, tiles in all.  c is such that all tiles' keys make no
@@ -168,7 +173,9 @@ struct Units {
 template <int BQ>
 __device__ __forceinline__ Units count_units(const PagedAttnArgs& a, const Requests<BQ>& first, int lane) {
     auto total = [&](auto&& of) {
-        int all = of(first);
+        auto all = of(first);
+        if (a.pages.n_requests == 1)
+            return __builtin_bit_cast(decltype(all), __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, all)));
         for (int r0 = 64; r0 < a.pages.n_requests; r0 += 64) {
             Requests<BQ> r;
             r.read(a, r0, lane);
@@ -180,14 +187,7 @@ __device__ __forceinline__ Units count_units(const PagedAttnArgs& a, const Reque
     u.tiles = u.units = total([](const Requests<BQ>& r) { return r.l.tiles; });
     u.c = 0x7fffffff;
     if (!a.pieces || u.tiles >= a.pieces) return u;
-    float keys = (float)first.l.tiles * (float)first.l.key_tiles;
-    for (int r0 = 64; r0 < a.pages.n_requests; r0 += 64) {
-        Requests<BQ> r;
-        r.read(a, r0, lane);
-        keys += (float)r.l.tiles * (float)r.l.key_tiles;
-    }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) keys += __shfl_xor(keys, d);
+    const float keys = total([](const Requests<BQ>& r) { return (float)r.l.tiles * (float)r.l.key_tiles; });
     float c = ceilf(keys / (float)a.pieces);
     c = c < (float)a.least ? (float)a.least : c;
     for (int k = 0; k < 4; ++k) {
@@ -203,13 +203,27 @@ __device__ __forceinline__ Units count_units(const PagedAttnArgs& a, const Reque
 // Unit u of a key head's (WHOLE: tile u of its tiles, whatever their pieces): false if there are not so many.
 template <int BQ, bool WHOLE>
 __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, const Requests<BQ>& first, int c, int u, int lane, Unit* out) {
+    if (a.pages.n_requests == 1) {
+        auto of = [&](int x) { return __builtin_amdgcn_readfirstlane(x); };
+        const int tiles = of(first.l.tiles), pieces = of(pieces_of(first.l.key_tiles, c));
+        if (u >= (WHOLE ? tiles : tiles * pieces)) return false;
+        out->r = 0;
+        out->q0 = of(first.q0);
+        out->new_ = of(first.n);
+        out->keys = of(first.keys);
+        out->pieces = pieces;
+        out->piece = WHOLE || pieces == 1 ? 0 : u / tiles;
+        out->tile = u - out->piece * tiles;
+        out->slot = u;
+        return true;
+    }
     int units_before = 0, slots_before = 0;
     for (int r0 = 0; r0 < a.pages.n_requests; r0 += 64) {
         Requests<BQ> r = first;
         if (r0) r.read(a, r0, lane);
         const int pieces = pieces_of(r.l.key_tiles, c);
         const int slots = r.l.tiles * pieces, units = WHOLE ? r.l.tiles : slots;
-        const int upto = scan_add(units, lane), slots_upto = WHOLE ? scan_add(slots, lane) : upto;
+        const int upto = scan_add(units), slots_upto = WHOLE ? scan_add(slots) : upto;
         const uint64_t b = __ballot(u - units_before < upto);
         if (b) {
             const int at = __builtin_ctzll(b);
@@ -220,6 +234,7 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, const Requests
             out->keys = of(r.keys);
             out->pieces = of(pieces);
             const int in = u - units_before - (of(upto) - of(units)), tiles = of(r.l.tiles);
+            if ((uint32_t)in >= (uint32_t)of(units)) return false;  // (counts that make no sense, of more units than 31 bits hold)
             // pieces of the same keys next to each other
             out->piece = WHOLE ? 0 : in / tiles;
             out->tile = WHOLE ? in : in - out->piece * tiles;
@@ -234,11 +249,11 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, const Requests
 
 // The n-th of a workgroup's units: workgroups go round the eight XCDs, each of which gets a run of neighbouring units, that
 // is of the same head's keys.  -1: none left.
-__device__ __forceinline__ int64_t nth_unit(int64_t total, int n) {
-    const int64_t run = (total + 7) / 8, at = (int64_t)(blockIdx.x >> 3) + (int64_t)n * (gridDim.x >> 3);
+__device__ __forceinline__ int nth_unit(int total, int n) {
+    const uint32_t run = ((uint32_t)total + 7) / 8, at = (blockIdx.x >> 3) + (uint32_t)n * (gridDim.x >> 3);
     if (at >= run) return -1;
-    const int64_t u = (blockIdx.x & 7) * run + at;
-    return u < total ? u : -1;
+    const uint32_t u = (blockIdx.x & 7) * run + at;
+    return u < (uint32_t)total ? (int)u : -1;
 }
 
 // Keys [first, past) that the token at place p sees of `keys`.
@@ -514,20 +529,24 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
     seen_by(a, place + div_by((uint32_t)row0, a.group), u.keys, lo, none);
     seen_by(a, place + div_by((uint32_t)row1, a.group), u.keys, none, hi);
     const int b = lo / kBK, e = hi > lo ? (hi + kBK - 1) / kBK : b;
-    begin = b + (int)((int64_t)(e - b) * u.piece / u.pieces);
-    end = b + (int)((int64_t)(e - b) * (u.piece + 1) / u.pieces);
+    begin = b;
+    end = e;
+    if (u.pieces > 1) {  // (below 2^26 tiles, at most 64 pieces)
+        begin = b + (int)((uint32_t)(e - b) * (uint32_t)u.piece / (uint32_t)u.pieces);
+        end = b + (int)((uint32_t)(e - b) * (uint32_t)(u.piece + 1) / (uint32_t)u.pieces);
+    }
 }
 
 // ---- few rows: each wavefront of a workgroup has keys of its own ----
-// 16 QB rows; the unit's keys go to the four wavefronts 32 at a time, each of which has LDS of its own for 32 rows of K and V.
+// 16 QB rows; the unit's keys go to the NW wavefronts 32 at a time, each of which has LDS of its own for 32 rows of K and V.
 // Memory bounds it: a wavefront reads its fragments into registers as soon as the rows have landed, and asks for the next ones
-// before it multiplies.  Two workgroups a compute unit then keep up to 128 KiB on their way.  The four results are joined in LDS.
-constexpr int kFewWaves = 4;
-template <int D>
-constexpr int few_lds() { return kFewWaves * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
+// before it multiplies.  Two workgroups of 4 wavefronts a compute unit, or one of 8 (where there are few: half as many keys one
+// after the other), keep up to 128 KiB on their way.  Their results are joined in LDS.
+template <int D, int NW>
+constexpr int few_lds() { return NW * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
 
-template <int D, int OP, int QB, bool RUNS>
-__global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const PagedAttnArgs a) {
+template <int D, int OP, int QB, bool RUNS, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) attn_paged_few_kernel(const PagedAttnArgs a) {
     using R = Rows<D>;
     constexpr int BQ = 16 * QB, KEYS = 32, RPI = R::RPL, NL = KEYS / RPI, NKF = D / 16, NCB = D / 16;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
@@ -538,20 +557,19 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
     Requests<BQ> requests;
     requests.read(a, 0, lane);
     const Units all = count_units<BQ>(a, requests, lane);
-    const int per_head = all.units;
-    const int64_t total = (int64_t)per_head * a.Hk;
+    const int per_head = all.units, total = per_head * a.Hk;
     for (int n = 0;; ++n) {
-        const int64_t id = nth_unit(total, n);
+        const int id = nth_unit(total, n);
         if (id < 0) return;
-        const int hk = (int)(id / per_head);
+        const int hk = id / per_head;
         Unit u;
-        if (!find_unit<BQ, false>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        if (!find_unit<BQ, false>(a, requests, all.c, id - hk * per_head, lane, &u)) return;
         int begin, end;
         key_tiles_of<BQ>(a, u, begin, end);
         const int32_t* const table = a.pages.table + (int64_t)u.r * a.pages.max_pages;
         const uint8_t* const kc = a.k_cache + (int64_t)hk * a.pages.head16 * 16;
         const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
-        // the wavefront's blocks of 32 keys: from b on, every kFewWaves-th
+        // the wavefront's blocks of 32 keys: from b on, every NW-th
         int b = 2 * begin + wave;
         const int blocks = 2 * end;
         // RUNS: lane x knows where run x % 2 (16 keys) of the wavefront's block x / 2 from `first` on begins; else lane x knows row x
@@ -561,16 +579,16 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
         uint64_t ok = 0;
         auto locate = [&](int block) {
             first = block;
-            const int key = RUNS ? KEYS * (block + kFewWaves * (lane >> 1)) + 16 * (lane & 1) : KEYS * block + (lane & 31);
+            const int key = RUNS ? KEYS * (block + NW * (lane >> 1)) + 16 * (lane & 1) : KEYS * block + (lane & 31);
             if (RUNS) entry = entry_of(a.pages, table, key, u.keys);
             const KeyRow kr = row_of(a.pages, entry, key, u.keys);
             ok = __ballot(kr.there);
             off16 = kr.off16;
-            if (!RUNS) entry = entry_of(a.pages, table, key + KEYS * kFewWaves, u.keys);
+            if (!RUNS) entry = entry_of(a.pages, table, key + KEYS * NW, u.keys);
         };
         auto fetch = [&](int block) {
-            if (!RUNS || block - first >= 32 * kFewWaves) locate(block);
-            const int at = RUNS ? (block - first) / kFewWaves * 2 : 0;
+            if (!RUNS || block - first >= 32 * NW) locate(block);
+            const int at = RUNS ? (block - first) / NW * 2 : 0;
             const int left = u.keys - KEYS * block;
             there = RUNS ? ((uint32_t)(ok >> at) & 1 ? 0xffffu : 0u) | ((uint32_t)(ok >> at) & 2 ? 0xffff0000u : 0u) : (uint32_t)ok;
             there = left >= KEYS ? there : left <= 0 ? 0u : there & ((1u << left) - 1);
@@ -633,11 +651,11 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
         }
         lo = __builtin_amdgcn_readfirstlane(lo);
         hi = __builtin_amdgcn_readfirstlane(hi);
-        for (; b < blocks; b += kFewWaves) {
+        for (; b < blocks; b += NW) {
             __builtin_amdgcn_s_waitcnt(0);  // (its own rows: no other wavefront waits for them)
             const int key0 = KEYS * b;
             const uint32_t t = there;
-            const bool more = b + kFewWaves < blocks;
+            const bool more = b + NW < blocks;
             if (t != 0xffffffffu || key0 < lo || key0 + KEYS > hi) {
                 if (t) {
                     int ln = lane;
@@ -648,7 +666,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
                         [&](int cb) { return v_fragment<D>(vt, 0, cb, i, g); }, vt, key0, t, a.scale_log2, i, g);
                 }
                 __builtin_amdgcn_s_waitcnt(0);
-                if (more) fetch(b + kFewWaves);
+                if (more) fetch(b + NW);
                 continue;
             }
             u32x4 kf[NKF], vf[NCB];
@@ -658,12 +676,12 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
             for (int cb = 0; cb < NCB; ++cb) vf[cb] = v_fragment<D>(vt, 0, cb, i, g);
             __builtin_amdgcn_s_waitcnt(0);
             __builtin_amdgcn_sched_barrier(0);
-            if (more) fetch(b + kFewWaves);
+            if (more) fetch(b + NW);
             __builtin_amdgcn_sched_barrier(0);
             block_step<D, OP, QB, false>(st, Q, [&](int f) { return kf[f]; }, [&](int cb) { return vf[cb]; }, vt, key0, t,
                                          a.scale_log2, i, g);
         }
-        // the four wavefronts' rows: maxima, then sums and O relative to the largest
+        // the wavefronts' rows: maxima, then sums and O relative to the largest
         float l[QB];
         __syncthreads();
         float2* const ml = reinterpret_cast<float2*>(smem);  // [wave][row]
@@ -676,24 +694,25 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
         float f[QB];
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
-            float2 x[kFewWaves];
+            float2 x[NW];
             float top = kNoScore;
 #pragma unroll
-            for (int w = 0; w < kFewWaves; ++w) {
+            for (int w = 0; w < NW; ++w) {
                 x[w] = ml[w * BQ + 16 * q + i];
                 top = fmaxf(top, x[w].x);
             }
             l[q] = 0.f;
 #pragma unroll
-            for (int w = 0; w < kFewWaves; ++w) l[q] += x[w].y * __builtin_amdgcn_exp2f((x[w].x - top) * a.scale_log2);
+            for (int w = 0; w < NW; ++w) l[q] += x[w].y * __builtin_amdgcn_exp2f((x[w].x - top) * a.scale_log2);
             f[q] = __builtin_amdgcn_exp2f((st.m[q] - top) * a.scale_log2);
             st.m[q] = top;
         }
         // O: wavefront w > 0 leaves its own, wavefront 0 adds them up in order
-        float* const area = reinterpret_cast<float*>(smem + 1024);  // [wave - 1][lane][4]
+        static_assert(2048 + (NW - 1) * D * 64 <= few_lds<D, NW>() && NW * BQ * 8 <= 2048, "room for the results");
+        float* const area = reinterpret_cast<float*>(smem + 2048);  // [wave - 1][channel block][lane][4]
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
-            // (a block of 16 rows at a time: three wavefronts' D / 16 pieces of 1 KiB)
+            // (a block of 16 rows at a time: D / 16 pieces of 1 KiB a wavefront)
             if (q > 0) __syncthreads();
 #pragma unroll
             for (int cb = 0; cb < D / 16; ++cb) {
@@ -706,7 +725,7 @@ __global__ void __launch_bounds__(64 * kFewWaves, 2) attn_paged_few_kernel(const
 #pragma unroll
                 for (int cb = 0; cb < D / 16; ++cb)
 #pragma unroll
-                    for (int w = 0; w < kFewWaves - 1; ++w) {
+                    for (int w = 0; w < NW - 1; ++w) {
                         const f32x4 x = *reinterpret_cast<const f32x4*>(area + ((w * (D / 16) + cb) * 64 + lane) * 4);
 #pragma unroll
                         for (int r = 0; r < 4; ++r) st.O[q][cb][r] += x[r];
@@ -747,8 +766,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
     Requests<BQ> requests;
     requests.read(a, 0, lane);
     const Units all = count_units<BQ>(a, requests, lane);
-    const int per_head = all.units;
-    const int64_t total = (int64_t)per_head * a.Hk;
+    const int per_head = all.units, total = per_head * a.Hk;
     const float scale = a.scale_log2, thr = kRescaleThr / scale;
     // K buffers 0 and 1, then V's
     auto kbuf = [&](int b) { return dyn + b * R::k_bytes(kBK); };
@@ -761,11 +779,11 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
         return x;
     };
     for (int n = 0;; ++n) {
-        const int64_t id = nth_unit(total, n);
+        const int id = nth_unit(total, n);
         if (id < 0) return;
-        const int hk = (int)(id / per_head);
+        const int hk = id / per_head;
         Unit u;
-        if (!find_unit<BQ, false>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
+        if (!find_unit<BQ, false>(a, requests, all.c, id - hk * per_head, lane, &u)) return;
         u32x4 Q[QB][NKS];
         f32x16 O[NOG][QB], S0, S1;  // scores: quarter 2 q + kb = row block q, keys 16 kb .. of the half
         float m[QB], top[QB], off[QB];  // maximum, what a score has to top to raise it, what its exponent is short of
@@ -1156,68 +1174,112 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
 }
 
 // ---- tiles in pieces put together ----
-// A workgroup a tile; 16 rows at a time, 16 lanes a row.
-template <int D, int BQ>
+__device__ __forceinline__ float max_of_lanes(float x) {
+#define DIT_MAX_LANE(ctrl, rows) \
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), ctrl, rows, 0xf, false)))
+    DIT_MAX_LANE(0x111, 0xf);
+    DIT_MAX_LANE(0x112, 0xf);
+    DIT_MAX_LANE(0x114, 0xf);
+    DIT_MAX_LANE(0x118, 0xf);
+    DIT_MAX_LANE(0x142, 0xa);
+    DIT_MAX_LANE(0x143, 0xc);
+#undef DIT_MAX_LANE
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
+
+// A wavefront a row, RW rows one after the other: lane s has the maximum and the sum of piece s, and D / 64 channels.
+template <int D, int BQ, int RW>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a) {
-    constexpr int CL = D / 16;  // channels a lane
+    constexpr int CL = D / 64, PER = 4 * RW, PARTS = BQ / PER;  // channels a lane, rows of a workgroup, workgroups of a tile
+    typedef float chans_t __attribute__((ext_vector_type(CL)));
     const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Requests<BQ> requests;
     requests.read(a, 0, lane);
     const Units all = count_units<BQ>(a, requests, lane);
     const int per_head = all.tiles;
-    const int64_t total = (int64_t)per_head * a.Hk;
+    const int64_t total = (int64_t)per_head * a.Hk * PARTS;
     for (int64_t id = blockIdx.x; id < total; id += gridDim.x) {
-        const int hk = (int)(id / per_head);
+        const int tile_id = (int)(id / PARTS), part = (int)(id % PARTS), hk = tile_id / per_head;
         Unit u;
-        if (!find_unit<BQ, true>(a, requests, all.c, (int)(id - (int64_t)hk * per_head), lane, &u)) return;
-        if (u.pieces < 2) continue;
+        if (!find_unit<BQ, true>(a, requests, all.c, tile_id - hk * per_head, lane, &u)) return;
         // piece s of the tile is tiles-of-the-request slots behind piece s - 1; u.slot counts from the request's first
-        const int64_t rows = (int64_t)u.new_ * a.G;
+        const int64_t rows = (int64_t)u.new_ * a.G, row0 = (int64_t)u.tile * BQ;
         const int tiles = (int)((rows + BQ - 1) / BQ);
-        for (int row = threadIdx.x >> 4; row < BQ; row += 16) {
-            const RowPlace p = place_of(a, u, hk, (int64_t)u.tile * BQ + row);
-            if (!p.live) continue;
-            const int ch = (threadIdx.x & 15) * CL;
-            float top = -INFINITY, sum = 0.f, o[CL];
+        if (u.pieces < 2 || u.slot + (u.pieces - 1) * tiles >= a.part_cap) continue;
+        for (int k = 0; k < RW; ++k) {
+            const int row = part * PER + wave * RW + k;
+            const RowPlace p = place_of(a, u, hk, row0 + row);
+            if (!p.live) break;
             auto at = [&](int s) { return ((int64_t)hk * a.part_cap + u.slot + (int64_t)s * tiles) * BQ + row; };
-            const int pieces = u.slot + (u.pieces - 1) * tiles < a.part_cap ? u.pieces : 0;
-            for (int s = 0; s < pieces; ++s) top = fmaxf(top, a.part_ml[at(s)].x);
+            auto stats = [&](int s) { return s < u.pieces ? a.part_ml[at(s)] : make_float2(-INFINITY, 0.f); };
+            float2 ml = stats(lane);
+            float top = max_of_lanes(ml.x);
+            for (int s0 = 64; s0 < u.pieces; s0 += 64) top = fmaxf(top, max_of_lanes(stats(s0 + lane).x));
+            float sum = 0.f;
+            chans_t o;
 #pragma unroll
-            for (int k = 0; k < CL; ++k) o[k] = 0.f;
-            for (int s = 0; s < pieces; ++s) {
-                const float2 ml = a.part_ml[at(s)];
+            for (int r = 0; r < CL; ++r) o[r] = 0.f;
+            for (int s0 = 0; s0 < u.pieces; s0 += 64) {
+                if (s0) ml = stats(s0 + lane);
                 const float w = __builtin_amdgcn_exp2f(ml.x - top);
-                sum = fmaf(ml.y, w, sum);
-                const f32x4* const src = reinterpret_cast<const f32x4*>(a.part_o + at(s) * D + ch);
+                sum += sum_of_lanes(ml.y * w);
+                const int n = u.pieces - s0 < 64 ? u.pieces - s0 : 64;
+                const chans_t* src = reinterpret_cast<const chans_t*>(a.part_o + at(s0) * D) + lane;
+                const int64_t step = (int64_t)tiles * BQ * D / CL;
+                for (int s = 0; s < n; s += 8) {
+                    chans_t x[8];
 #pragma unroll
-                for (int k = 0; k < CL; k += 4) {
-                    const f32x4 x = src[k / 4];
+                    for (int e = 0; e < 8; ++e) x[e] = src[(s + e < n ? s + e : n - 1) * step];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o[k + r] = fmaf(x[r], w, o[k + r]);
+                    for (int e = 0; e < 8; ++e) {
+                        if (s + e >= n) break;
+                        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s + e));
+#pragma unroll
+                        for (int r = 0; r < CL; ++r) o[r] = fmaf(x[e][r], ws, o[r]);
+                    }
                 }
             }
             const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-            const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + ch;
+            const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + CL * lane;
 #pragma unroll
-            for (int k = 0; k < CL; k += 4)
-                store4(a.out, off + k, a.out_type, f32x4{o[k] * inv, o[k + 1] * inv, o[k + 2] * inv, o[k + 3] * inv});
-            if (a.lse && (threadIdx.x & 15) == 0)
+            for (int r = 0; r < CL; ++r) o[r] *= inv;
+            if (a.out_type == DIT_F32) {
+                *reinterpret_cast<chans_t*>(static_cast<float*>(a.out) + off) = o;
+            } else {
+                uint16_t* const to = static_cast<uint16_t*>(a.out) + off;
+                if constexpr (CL == 2) *reinterpret_cast<uint32_t*>(to) = pack2<OP_BF16>(o[0], o[1]);
+                else *to = (uint16_t)pack2<OP_BF16>(o[0], 0.f);
+            }
+            if (a.lse && lane == 0)
                 a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
         }
     }
 }
-
-template <int D, int OP, int QB>
-hipError_t launch_few(const PagedAttnArgs& a, int units, hipStream_t s) {
-    static std::atomic<uint64_t> done_runs{0}, done_rows{0};
-    const auto kern = a.pages.runs ? attn_paged_few_kernel<D, OP, QB, true> : attn_paged_few_kernel<D, OP, QB, false>;
-    hipError_t e = allow_dynamic_lds(kern, few_lds<D>(), a.pages.runs ? done_runs : done_rows);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kFewWaves), few_lds<D>(), s, a);
-    e = hipGetLastError();
-    if (e != hipSuccess || !a.pieces) return e;
-    hipLaunchKernelGGL((attn_paged_join_kernel<D, 16 * QB>), dim3(units), dim3(256), 0, s, a);
+// Its launch, for so many tiles as are known of.
+template <int D, int BQ, int RW>
+hipError_t launch_join(const PagedAttnArgs& a, int units, hipStream_t s) {
+    const int64_t n = (int64_t)units / a.pieces_each * (BQ / (4 * RW));
+    hipLaunchKernelGGL((attn_paged_join_kernel<D, BQ, RW>), dim3((unsigned)(n < 1 ? 1 : n < 65536 ? n : 65536)), dim3(256), 0, s, a);
     return hipGetLastError();
+}
+
+template <int D, int OP, int QB, bool RUNS, int NW>
+hipError_t launch_few_n(const PagedAttnArgs& a, int units, hipStream_t s) {
+    static std::atomic<uint64_t> done{0};
+    const auto kern = attn_paged_few_kernel<D, OP, QB, RUNS, NW>;
+    constexpr int lds = few_lds<D, NW>();
+    hipError_t e = allow_dynamic_lds(kern, lds, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * NW), lds, s, a);
+    return hipGetLastError();
+}
+template <int D, int OP, int QB>
+hipError_t launch_few(const PagedAttnArgs& a, int units, int nw, hipStream_t s) {
+    hipError_t e;
+    if (nw == 8) e = a.pages.runs ? launch_few_n<D, OP, QB, true, 8>(a, units, s) : launch_few_n<D, OP, QB, false, 8>(a, units, s);
+    else e = a.pages.runs ? launch_few_n<D, OP, QB, true, 4>(a, units, s) : launch_few_n<D, OP, QB, false, 4>(a, units, s);
+    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB, 1>(a, units, s);
 }
 template <int D, int OP>
 hipError_t launch_big(const PagedAttnArgs& a, int units, hipStream_t s) {
@@ -1229,15 +1291,15 @@ hipError_t launch_big(const PagedAttnArgs& a, int units, hipStream_t s) {
     hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kBigWaves), big_lds<D>(), s, a);
     e = hipGetLastError();
     if (e != hipSuccess || !a.pieces) return e;
-    hipLaunchKernelGGL((attn_paged_join_kernel<D, kPagedBigRows>), dim3(units), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return launch_join<D, kPagedBigRows, 4>(a, units, s);
 }
 
 template <int D, int OP>
 hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_t* ws, hipStream_t s) {
     PagedAttnArgs a = args;
-    auto parts = [&](int pieces, int cap, int rows) {
+    auto parts = [&](int pieces, int each, int cap, int rows) {
         a.pieces = pieces;
+        a.pieces_each = each;
         a.part_cap = cap;
         a.part_o = reinterpret_cast<float*>(ws);
         a.part_ml = reinterpret_cast<float2*>(ws + (size_t)a.Hk * cap * rows * D * sizeof(float));
@@ -1247,15 +1309,15 @@ hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_
         a.rows_lo = 1;
         a.rows_hi = plan.big ? 16 * plan.few_qb : 0x7fffffff;
         a.least = 2;
-        parts(plan.few_pieces, plan.few_cap, 16 * plan.few_qb);
-        e = plan.few_qb == 1 ? launch_few<D, OP, 1>(a, plan.few_units, s) : launch_few<D, OP, 2>(a, plan.few_units, s);
+        parts(plan.few_pieces, plan.few_each, plan.few_cap, 16 * plan.few_qb);
+        e = plan.few_qb == 1 ? launch_few<D, OP, 1>(a, plan.few_units, plan.few_waves, s) : launch_few<D, OP, 2>(a, plan.few_units, plan.few_waves, s);
     }
     if (e == hipSuccess && plan.big) {
         a.rows_lo = plan.few ? 16 * plan.few_qb + 1 : 1;
         a.rows_hi = 0x7fffffff;
         a.least = 4;
         ws += plan.few_bytes;
-        parts(plan.big_pieces, plan.big_cap, kPagedBigRows);
+        parts(plan.big_pieces, plan.big_each, plan.big_cap, kPagedBigRows);
         e = launch_big<D, OP>(a, plan.big_units, s);
     }
     return e;
@@ -1272,32 +1334,54 @@ PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int m
     p.few = most_q * G <= 32 || !uniform;
     p.big = most_q * G > 32;
     const int64_t key_tiles = max_keys > 0 ? (max_keys + kBK - 1) / kBK : 1;
-    // Two workgroups a compute unit.  Time in key tiles of a workgroup: rounds of workgroups, each as long as its keys and its two
+    // Time in key tiles of a workgroup: rounds of workgroups (`slots` at a time), each as long as its keys (`step` a tile) and its two
     // ends; tiles in pieces need the launch that joins them.
-    auto layout = [&](int BQ, int least, double ends, double join, int& units, int& pieces, int& cap, size_t& bytes) {
-        constexpr int64_t slots = 2 * kCUs;
+    struct Layout {
+        double time;
+        int units, pieces, each, cap;
+        size_t bytes;
+    };
+    auto layout = [&](int BQ, int64_t slots, double step, double ends, int least, double join) {
         // tiles of a key head: at most (whatever q_start says, with what is left over of each request), and as far as is known
         const int64_t most = (rows + some * (BQ - 1)) / BQ;
         const int64_t each = (most_q * G + BQ - 1) / BQ, tiles = some * each < most ? some * each : most;
         auto time = [&](int n) {
             const int64_t rounds = (tiles * Hk * n + slots - 1) / slots;
-            return (double)rounds * ((double)((key_tiles + n - 1) / n) + ends) + (n > 1 ? join : 0.0);
+            return (double)rounds * (step * (double)((key_tiles + n - 1) / n) + ends) + (n > 1 ? join : 0.0);
         };
         int best = 1;
         for (int n = 2; n <= 64 && n * (int64_t)least <= key_tiles; ++n) {
             if ((tiles * n + most) * Hk * BQ > (int64_t)1 << 19) break;  // rows of pieces: 272 MB at head_dim 128
             if (time(n) < 0.97 * time(best)) best = n;
         }
+        Layout l{time(best), 0, 0, best, 0, 0};
         if (best > 1) {
-            pieces = (int)(tiles * best);
-            cap = (int)(tiles * best + most);
-            bytes = ((size_t)Hk * cap * BQ * (D * sizeof(float) + sizeof(float2)) + 255) / 256 * 256;
+            l.pieces = (int)(tiles * best);
+            l.cap = (int)(tiles * best + most);
+            l.bytes = ((size_t)Hk * l.cap * BQ * (D * sizeof(float) + sizeof(float2)) + 255) / 256 * 256;
         }
         const int64_t n = tiles * Hk * best;
-        units = (int)(n < 65536 ? n : 65536);
+        l.units = (int)(n < 65536 ? n : 65536);
+        return l;
     };
-    if (p.few) layout(16 * p.few_qb, 2, 6.0, 4.0, p.few_units, p.few_pieces, p.few_cap, p.few_bytes);
-    if (p.big) layout(kPagedBigRows, 4, 6.0, 6.0, p.big_units, p.big_pieces, p.big_cap, p.big_bytes);
+    if (p.few) {
+        const Layout four = layout(16 * p.few_qb, 2 * kCUs, 1.0, 8.0, 2, 6.0), eight = layout(16 * p.few_qb, kCUs, 0.55, 8.0, 4, 6.0);
+        const Layout& l = eight.time < four.time ? eight : four;
+        p.few_waves = eight.time < four.time ? 8 : 4;
+        p.few_units = l.units;
+        p.few_pieces = l.pieces;
+        p.few_each = l.each;
+        p.few_cap = l.cap;
+        p.few_bytes = l.bytes;
+    }
+    if (p.big) {
+        const Layout l = layout(kPagedBigRows, 2 * kCUs, 1.0, 6.0, 4, 6.0);
+        p.big_units = l.units;
+        p.big_pieces = l.pieces;
+        p.big_each = l.each;
+        p.big_cap = l.cap;
+        p.big_bytes = l.bytes;
+    }
     return p;
 }
 

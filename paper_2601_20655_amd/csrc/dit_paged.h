@@ -88,7 +88,7 @@ struct PagedAttnArgs {
     void* out;
     float* lse;  // nullable [H, N]
     PageArgs pages;
-    int N, H, Hk, G;  // G = H / Hk; N G < 2^31
+    int N, H, Hk, G;  // G = H / Hk; N H + n_requests Hk < 2^30: so are all units' numbers
     FastDiv group;    // G
     int64_t sq_t, sq_h, so_t, so_h;
     int q_type, out_type;  // dit_dtype
@@ -99,6 +99,7 @@ struct PagedAttnArgs {
     // few tiles; requests of fewer than rows_lo or more than rows_hi rows are another launch's
     int rows_lo, rows_hi;
     int pieces;      // work units wanted, per key head; 0: every tile whole
+    int pieces_each; // of a tile, as far as the host knows (the joining launch's size goes by it)
     int least;       // key tiles of a piece, at least
     int part_cap;    // tiles' pieces per key head that part_o, part_ml have room for
     float* part_o;   // [Hk][piece][row][D] unnormalised
@@ -106,9 +107,10 @@ struct PagedAttnArgs {
 };
 struct PagedPlan {
     bool few, big;
-    int few_qb;                   // 16-row blocks of a few-row tile
+    int few_qb, few_waves;        // 16-row blocks of a few-row tile; wavefronts of its workgroup
     int few_units, big_units;     // workgroups
-    int few_pieces, big_pieces;   // as above; 0: no
+    int few_pieces, big_pieces;   // units wanted per key head; 0: every tile whole
+    int few_each, big_each;       // of a tile, as far as is known
     int few_cap, big_cap;
     size_t few_bytes, big_bytes;  // of workspace
 };

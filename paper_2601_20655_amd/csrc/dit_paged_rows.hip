@@ -104,7 +104,13 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
     const int head0 = part * (C * HW) + lane / L;
     auto head = [&](int c) { return head0 + c * HW < x.H ? head0 + c * HW : x.H - 1; };
 
-    // All that a row needs is asked for before any of it is used: the rows, the weights, the position and the pairs' turns.
+    // All that a row needs is asked for before any of it is used: the counts (first: what is asked for later need not have come
+    // when they have), the rows, the weights, the position and the pairs' turns.
+    int start = 0, length = 0;  // of request `lane`
+    if (a.cached) {
+        start = a.pages.q_start[lane <= a.pages.n_requests ? lane : a.pages.n_requests];
+        length = a.pages.kv_len[lane < a.pages.n_requests ? lane : a.pages.n_requests - 1];
+    }
     const bool turned = kind != 2 && a.pos;
     const bool weighed = NORM != RN_NONE && kind != 2 && x.gamma;
     Piece<F32> raw[C];
@@ -117,6 +123,31 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
             for (int c = 0; c < C; ++c) gamma[c] = load_piece<true, false>(x.gamma, (int64_t)head(c) * D + 8 * slice);
         }
     }
+    // where the row goes
+    int64_t place = -1;  // of the token in its request
+    int entry = -1, r = -1;
+    if (a.cached) {
+        int past = 0, keys = 0;  // one past the request's last new token, its tokens
+        if (a.pages.n_requests < 64) {
+            const uint64_t b = __ballot(lane <= a.pages.n_requests && start <= t);
+            r = b ? 63 - __builtin_clzll(b) : -1;
+            if (r == a.pages.n_requests) r = -1;
+            if (r >= 0) {
+                past = __builtin_amdgcn_readlane(start, r + 1);
+                keys = __builtin_amdgcn_readlane(length, r);
+            }
+        } else {
+            r = request_of(a.pages, t, lane);
+            if (r >= 0) {
+                past = a.pages.q_start[r + 1];
+                keys = a.pages.kv_len[r];
+            }
+        }
+        place = r < 0 || kind == 0 ? -1 : (int64_t)keys - past + t;
+        if (place < 0 || place >= (int64_t)a.pages.max_pages * a.pages.page.d || place > 0x7fffffff) place = -1;
+        if (place >= 0) entry = a.pages.table[(int64_t)r * a.pages.max_pages + div_by((uint32_t)place, a.pages.page)];
+    }
+    const bool live = there && !(a.cached && r < 0);
     float2 cs[4];
     if (turned) {
         int at[3];
@@ -132,24 +163,6 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
             float sn, c;
             sincospif(2.0f * f, &sn, &c);
             cs[i] = make_float2(c, sn);
-        }
-    }
-
-    // where the row goes
-    int64_t off16 = -1;  // of the token in the cache, in 16 bytes
-    bool live = there;
-    if (a.cached) {
-        const int r = request_of(a.pages, t, lane);
-        live = live && r >= 0;
-        if (r >= 0 && kind != 0) {
-            const int64_t at = (int64_t)a.pages.kv_len[r] - a.pages.q_start[r + 1] + t;
-            if (at >= 0 && at < (int64_t)a.pages.max_pages * a.pages.page.d) {
-                const uint32_t n = (uint32_t)at < 0x80000000u ? (uint32_t)at : 0u;
-                const uint32_t page = div_by(n, a.pages.page);
-                const int e = a.pages.table[(int64_t)r * a.pages.max_pages + page];
-                if (e >= 0 && e < a.pages.n_pages)
-                    off16 = (int64_t)e * a.pages.page16 + (int64_t)(n - page * a.pages.page.d) * a.pages.token16;
-            }
         }
     }
 
@@ -253,7 +266,9 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
             }
     }
     if (a.cached && kind != 0) {
-        if (off16 < 0) return;
+        if (place < 0 || entry < 0 || entry >= a.pages.n_pages) return;
+        const uint32_t slot = (uint32_t)place - div_by((uint32_t)place, a.pages.page) * a.pages.page.d;
+        const int64_t off16 = (int64_t)entry * a.pages.page16 + (int64_t)slot * a.pages.token16;
         u32x4* const rows = reinterpret_cast<u32x4*>(kind == 1 ? a.k_cache : a.v_cache) + off16;
 #pragma unroll
         for (int c = 0; c < C; ++c) {

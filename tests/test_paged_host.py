@@ -89,6 +89,7 @@ CACHE_OTHER = [(dict(D=96), UNSUPPORTED), (dict(D=256), UNSUPPORTED), (dict(page
                                      dict(out_dtype=2), dict(flags=1), dict(token=128), dict(head=8), dict(out_token=500))
       + tuple(CACHE_INVALID)],
     (attn, dict(N=2 ** 31 - 1, H=4), UNSUPPORTED),
+    (attn, dict(N=1 << 27, H=8), UNSUPPORTED),
     *[(attn, kw, want) for kw, want in CACHE_OTHER],
     *[(attn, kw, ALIGNMENT) for kw in (dict(q=FAKE + 8), dict(kc=FAKE + 8), dict(vc=FAKE + 2), dict(out=FAKE + 4), dict(lse=FAKE + 2),
                                        dict(table=FAKE + 1), dict(q_start=FAKE + 2), dict(kv_len=FAKE + 2), dict(token=516),
@@ -129,7 +130,7 @@ def test_workspace_size():
 def plan(N, R, H, Hk, D, keys, max_q):
     class Plan(ctypes.Structure):
         _fields_ = [("few", ctypes.c_bool), ("big", ctypes.c_bool)] + [(n, ctypes.c_int) for n in (
-            "few_qb", "few_units", "big_units", "few_pieces", "big_pieces", "few_cap", "big_cap")] + [
+            "few_qb", "few_waves", "few_units", "big_units", "few_pieces", "big_pieces", "few_each", "big_each", "few_cap", "big_cap")] + [
             ("few_bytes", ctypes.c_size_t), ("big_bytes", ctypes.c_size_t)]
 
     f = B.lib()._ZN3dit10plan_pagedEiiiiili
@@ -140,7 +141,7 @@ def plan(N, R, H, Hk, D, keys, max_q):
 
 @pytest.mark.parametrize("N,R,H,Hk,max_q,few,big", [
     (1, 1, 40, 8, 0, True, False), (32, 32, 40, 8, 1, True, False), (4680, 1, 40, 40, 4680, False, True),
-    (200, 5, 6, 3, 196, True, True), (200, 5, 6, 3, 0, True, True), (2 ** 31 - 1, 2 ** 31 - 1, 1, 1, 1, True, False)])
+    (200, 5, 6, 3, 196, True, True), (200, 5, 6, 3, 0, True, True), (2 ** 29 - 1, 2 ** 29 - 1, 1, 1, 1, True, False)])
 def test_which_kernels(N, R, H, Hk, max_q, few, big):
     p = plan(N, R, H, Hk, 128, 32768, max_q)
     assert (p.few, p.big) == (few, big)
