@@ -1174,26 +1174,11 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
 }
 
 // ---- tiles in pieces put together ----
-__device__ __forceinline__ float max_of_lanes(float x) {
-#define DIT_MAX_LANE(ctrl, rows) \
-    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(x), __float_as_uint(x), ctrl, rows, 0xf, false)))
-    DIT_MAX_LANE(0x111, 0xf);
-    DIT_MAX_LANE(0x112, 0xf);
-    DIT_MAX_LANE(0x114, 0xf);
-    DIT_MAX_LANE(0x118, 0xf);
-    DIT_MAX_LANE(0x142, 0xa);
-    DIT_MAX_LANE(0x143, 0xc);
-#undef DIT_MAX_LANE
-    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
-}
-
-// A wavefront a row, RW rows one after the other: lane s has the maximum and the sum of piece s, and D / 64 channels.
-template <int D, int BQ, int RW>
+// D / 4 lanes a row, four channels each, in one pass: UN pieces at a time, all that is read of them asked for before any is used.
+template <int D, int BQ, int UN>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a) {
-    constexpr int CL = D / 64, PER = 4 * RW, PARTS = BQ / PER;  // channels a lane, rows of a workgroup, workgroups of a tile
-    typedef float chans_t __attribute__((ext_vector_type(CL)));
+    constexpr int LANES = D / 4, PER = 256 / LANES, PARTS = BQ / PER;  // of a row, rows of a workgroup, workgroups of a tile
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Requests<BQ> requests;
     requests.read(a, 0, lane);
     const Units all = count_units<BQ>(a, requests, lane);
@@ -1207,60 +1192,50 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArg
         const int64_t rows = (int64_t)u.new_ * a.G, row0 = (int64_t)u.tile * BQ;
         const int tiles = (int)((rows + BQ - 1) / BQ);
         if (u.pieces < 2 || u.slot + (u.pieces - 1) * tiles >= a.part_cap) continue;
-        for (int k = 0; k < RW; ++k) {
-            const int row = part * PER + wave * RW + k;
-            const RowPlace p = place_of(a, u, hk, row0 + row);
-            if (!p.live) break;
-            auto at = [&](int s) { return ((int64_t)hk * a.part_cap + u.slot + (int64_t)s * tiles) * BQ + row; };
-            auto stats = [&](int s) { return s < u.pieces ? a.part_ml[at(s)] : make_float2(-INFINITY, 0.f); };
-            float2 ml = stats(lane);
-            float top = max_of_lanes(ml.x);
-            for (int s0 = 64; s0 < u.pieces; s0 += 64) top = fmaxf(top, max_of_lanes(stats(s0 + lane).x));
-            float sum = 0.f;
-            chans_t o;
+        const int row = part * PER + threadIdx.x / LANES, ch = threadIdx.x % LANES * 4;
+        const RowPlace p = place_of(a, u, hk, row0 + row);
+        if (!p.live) continue;
+        const int64_t first = ((int64_t)hk * a.part_cap + u.slot) * BQ + row, step = (int64_t)tiles * BQ;
+        float top = kNoScore, sum = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < u.pieces; s += UN) {
+            float2 ml[UN];
+            f32x4 x[UN];
 #pragma unroll
-            for (int r = 0; r < CL; ++r) o[r] = 0.f;
-            for (int s0 = 0; s0 < u.pieces; s0 += 64) {
-                if (s0) ml = stats(s0 + lane);
-                const float w = __builtin_amdgcn_exp2f(ml.x - top);
-                sum += sum_of_lanes(ml.y * w);
-                const int n = u.pieces - s0 < 64 ? u.pieces - s0 : 64;
-                const chans_t* src = reinterpret_cast<const chans_t*>(a.part_o + at(s0) * D) + lane;
-                const int64_t step = (int64_t)tiles * BQ * D / CL;
-                for (int s = 0; s < n; s += 8) {
-                    chans_t x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = src[(s + e < n ? s + e : n - 1) * step];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (s + e >= n) break;
-                        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s + e));
-#pragma unroll
-                        for (int r = 0; r < CL; ++r) o[r] = fmaf(x[e][r], ws, o[r]);
-                    }
-                }
+            for (int e = 0; e < UN; ++e) {
+                const int64_t at = first + (s + e < u.pieces ? s + e : u.pieces - 1) * step;
+                ml[e] = a.part_ml[at];
+                x[e] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + ch);
             }
-            const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
-            const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + CL * lane;
+            float m = top;
 #pragma unroll
-            for (int r = 0; r < CL; ++r) o[r] *= inv;
-            if (a.out_type == DIT_F32) {
-                *reinterpret_cast<chans_t*>(static_cast<float*>(a.out) + off) = o;
-            } else {
-                uint16_t* const to = static_cast<uint16_t*>(a.out) + off;
-                if constexpr (CL == 2) *reinterpret_cast<uint32_t*>(to) = pack2<OP_BF16>(o[0], o[1]);
-                else *to = (uint16_t)pack2<OP_BF16>(o[0], 0.f);
+            for (int e = 0; e < UN; ++e) m = fmaxf(m, ml[e].x);
+            const float before = __builtin_amdgcn_exp2f(top - m);
+            top = m;
+            sum *= before;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] *= before;
+#pragma unroll
+            for (int e = 0; e < UN; ++e) {
+                if (s + e >= u.pieces) break;
+                const float w = __builtin_amdgcn_exp2f(ml[e].x - m);
+                sum = fmaf(ml[e].y, w, sum);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = fmaf(x[e][r], w, o[r]);
             }
-            if (a.lse && lane == 0)
-                a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
         }
+        const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+        store4(a.out, (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + ch, a.out_type,
+               f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
+        if (a.lse && ch == 0)
+            a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
 }
 // Its launch, for so many tiles as are known of.
-template <int D, int BQ, int RW>
+template <int D, int BQ, int UN>
 hipError_t launch_join(const PagedAttnArgs& a, int units, hipStream_t s) {
-    const int64_t n = (int64_t)units / a.pieces_each * (BQ / (4 * RW));
-    hipLaunchKernelGGL((attn_paged_join_kernel<D, BQ, RW>), dim3((unsigned)(n < 1 ? 1 : n < 65536 ? n : 65536)), dim3(256), 0, s, a);
+    const int64_t n = (int64_t)units / a.pieces_each * (BQ * D / 1024);
+    hipLaunchKernelGGL((attn_paged_join_kernel<D, BQ, UN>), dim3((unsigned)(n < 1 ? 1 : n < 65536 ? n : 65536)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -1279,7 +1254,7 @@ hipError_t launch_few(const PagedAttnArgs& a, int units, int nw, hipStream_t s) 
     hipError_t e;
     if (nw == 8) e = a.pages.runs ? launch_few_n<D, OP, QB, true, 8>(a, units, s) : launch_few_n<D, OP, QB, false, 8>(a, units, s);
     else e = a.pages.runs ? launch_few_n<D, OP, QB, true, 4>(a, units, s) : launch_few_n<D, OP, QB, false, 4>(a, units, s);
-    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB, 1>(a, units, s);
+    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB, 8>(a, units, s);
 }
 template <int D, int OP>
 hipError_t launch_big(const PagedAttnArgs& a, int units, hipStream_t s) {
