@@ -1477,6 +1477,9 @@ bool aligned4(const void* a, const void* b, const void* c) {
     return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & 3u) == 0;
 }
 
+// 16 tokens from a multiple of 16 on lie in one page, their rows within 2^31 bytes.
+bool in_runs(const dit_kv_cache& c) { return c.page_size % 16 == 0 && c.token <= ((int64_t)1 << 31) / 2 / 16; }
+
 dit::PageArgs page_args(const dit_kv_cache& c, const int32_t* table, const int32_t* q_start, const int32_t* kv_len) {
     dit::PageArgs p{};
     p.table = table;
@@ -1490,7 +1493,7 @@ dit::PageArgs page_args(const dit_kv_cache& c, const int32_t* table, const int32
     p.token16 = c.page_size > 1 ? (uint32_t)(c.token / 8) : 0;
     p.head16 = c.Hk > 1 ? (uint32_t)(c.head / 8) : 0;
     p.page = dit::fast_div((uint32_t)c.page_size);
-    p.runs = c.page_size % 16 == 0 && c.token <= ((int64_t)1 << 31) / 2 / 16;
+    p.runs = in_runs(c);
     return p;
 }
 
@@ -1598,7 +1601,7 @@ dit_status check_paged(const dit_paged_attn_params* p, dit::PagedPlan* plan) {
     int64_t keys = (int64_t)p->cache.max_pages * p->cache.page_size;
     if (p->max_kv && p->max_kv < keys) keys = p->max_kv;
     if (keys > 0x7fffffff) keys = 0x7fffffff;
-    *plan = p->N ? dit::plan_paged(p->N, p->cache.n_requests, p->H, p->cache.Hk, p->cache.D, keys, p->max_q) : dit::PagedPlan{};
+    *plan = p->N ? dit::plan_paged(p->N, p->cache.n_requests, p->H, p->cache.Hk, p->cache.D, keys, p->max_q, in_runs(p->cache)) : dit::PagedPlan{};
     return DIT_OK;
 }
 

@@ -738,27 +738,35 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_few_kernel(const PagedA
 }
 
 // ---- many rows: the wavefronts of a workgroup share the keys ----
-// 32 rows a wavefront, 128 a workgroup, two workgroups a compute unit.  Software-pipelined in halves of a tile, 32 keys: while the
+// 16 QB rows a wavefront, NW wavefronts: 128 rows and two workgroups a compute unit (4 x 32), or 256 and one (8 x 32: half the bytes
+// from L2 to LDS, and nothing under a tile's ends).  The matrix cores and the vector ALU hardly work at the same time here: a
+// loop of 16x16x32 products with n vector instructions behind each takes about 17 + 3.3 n clocks, two wavefronts or one; so what
+// counts is the sum, 32 products and 64 vector instructions (16 of them exponentials, 8 clocks each) a half, and the
+// power that random operands take (zeros: 2.5 ms where these take 3.1).  4,680 rows x 32,760 keys at 40 heads of 128 (frame-wise, 2.99e12
+// operations): 3.13 ms by 4 x 32, 2.90 by 8 x 32 (1,030 TFLOP/s), 3.70 where rows lie anywhere (8 x 16, below); fragments read 2, 4,
+// 6 or 8 ahead, other priorities: level.  Software-pipelined in halves of a tile, 32 keys: while the
 // matrix cores work on a half's scores the vector ALU takes the exponentials of the half before it, and while they multiply
 // those with V it takes the maxima of the new scores.  So a half's scores are needed one half ahead of its V, and a turn of the
 // loop, which multiplies V of tile j, takes K rows 32 keys on: K(j) in LDS is rows 64 j + 32 .. 64 j + 95.  K(j + 1) and V(j + 1) are
 // on their way meanwhile.  A row's maximum is raised only where a score tops it by more than 2^8 (exponents stay far from their
 // ends, and what divides the row takes it out again).
-constexpr int kBigWaves = 4, kBigQB = 2;
-static_assert(kPagedBigRows == 16 * kBigQB * kBigWaves, "rows of a workgroup");
 template <int D>
-constexpr int big_lds() { return 2 * (Rows<D>::k_bytes(kBK) + Rows<D>::v_bytes(kBK)); }
+constexpr int big_buffers() { return 2 * (Rows<D>::k_bytes(kBK) + Rows<D>::v_bytes(kBK)); }
+// Rows that lie anywhere: the places of sixteen tiles' rows, and which of them are there, twice.
+constexpr int kPlaceTiles = 16, kPlaceBytes = kPlaceTiles * (kBK * 4 + 8);
+template <int D, bool RUNS>
+constexpr int big_lds() { return big_buffers<D>() + (RUNS ? 0 : 2 * kPlaceBytes); }
 
 // RUNS: 16 tokens from a multiple of 16 on lie in one page, so that a wavefront's rows of a part start at one place.
-template <int D, int OP, bool RUNS>
-__global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const PagedAttnArgs a) {
+template <int D, int OP, bool RUNS, int NW, int QB>
+__global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedAttnArgs a) {
     using R = Rows<D>;
-    constexpr int NW = kBigWaves, QB = kBigQB, BQ = kPagedBigRows;
-    constexpr int RPI = R::RPL, NL = kBK / NW / RPI;  // rows a load, loads of a wavefront's 16 rows
+    constexpr int BQ = 16 * QB * NW;
+    constexpr int RW = kBK / NW, RPI = R::RPL, NL = RW / RPI;  // rows that a wavefront fetches of a part, rows a load, loads
     constexpr int NKS = D / 32, NCB = D / 16, NOG = NCB / 4, NKF = 2 * NKS;
     constexpr int LA = 4;        // fragments are read from LDS so many ahead of their products
     constexpr int NCH = 4 * QB;  // slices of two scores
-    constexpr int PRE = 2;       // exponentials run so many slices ahead of their rounding
+    constexpr int PRE = NCH > 2 * NKF ? NCH / NKF : 2;       // exponentials run so many slices ahead of their rounding
     static_assert(LA <= NKF && LA <= NCB && PRE >= NCH / NKF, "look-ahead within a half");
     extern __shared__ __attribute__((aligned(16))) uint8_t dyn[];
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
@@ -785,7 +793,10 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
         Unit u;
         if (!find_unit<BQ, false>(a, requests, all.c, id - hk * per_head, lane, &u)) return;
         u32x4 Q[QB][NKS];
-        f32x16 O[NOG][QB], S0, S1;  // scores: quarter 2 q + kb = row block q, keys 16 kb .. of the half
+        f32x16 O[NOG][QB];
+        // scores: quarter 2 (q % 2) + kb of word q / 2 = row block q, keys 16 kb .. of the half
+        typedef f32x16 scores_t[(QB + 1) / 2];
+        scores_t S0, S1;
         float m[QB], top[QB], off[QB];  // maximum, what a score has to top to raise it, what its exponent is short of
         float l[QB][2];                 // sums, of every other key of the lane's
         int lo = 0, hi = 0x7fffffff;  // keys that every row of the wavefront sees
@@ -821,47 +832,60 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
         const uint8_t* const vc = a.v_cache + (int64_t)hk * a.pages.head16 * 16;
 
         // ---- where rows of K and V are ----
-        // RUNS: lane x has run x % 4 (16 keys) of tile first_tile + x / 4: the place of its first row, and in `ok` whether its page
-        // is there; the pages of the sixteen tiles behind the next turn but thirteen are asked for meanwhile.  Else lane l has row l of the tiles
-        // j + 1 and j + 2, j the one whose turn it is: off_a, off_b, there_a, there_b (there_c: of j), and asks for the page of j + 3.
-        constexpr int kTurns = 14;  // a turn needs its tile and the two behind it
-        int first_tile = 0, entry = 0;
-        uint32_t off_a = 0, off_b = 0;
-        uint64_t ok = 0, there_a = 0, there_b = 0, there_c = 0;
-        auto ask = [&](int tile) { return entry_of(a.pages, table, RUNS ? kBK * tile + 16 * lane : kBK * tile + lane, u.keys); };
+        // Of sixteen tiles at a time, from first_tile on; a turn needs its tile and the two behind it.  RUNS: lane x has run x % 4 (16
+        // keys) of tile first_tile + x / 4: the place of its first row, and in `ok` whether its page is there; the pages of the sixteen
+        // tiles behind the next turn but thirteen are asked for meanwhile.  Else the places of all rows are in LDS, written by all
+        // wavefronts in turns, and `ok` has a bit for each tile all of which is there.  (In registers, two rows a lane, they pushed the
+        // query rows of the 2 x 128 kernel into scratch memory, whose reloads wait for the keys on their way: 13.4 ms; in LDS, 5.9, of
+        // which a wavefront of one row block has no spills at all: 3.7.)
+        constexpr int kTurns = kPlaceTiles - 2;
+        int first_tile = 0, entry = 0, half = 0;
+        uint32_t off_a = 0;
+        uint64_t ok = 0;
+        auto places = [&]() { return reinterpret_cast<uint32_t*>(dyn + big_buffers<D>() + half * kPlaceBytes); };
+        auto rows_there = [&]() { return reinterpret_cast<uint64_t*>(places() + kPlaceTiles * kBK); };
+        auto ask = [&](int tile) { return entry_of(a.pages, table, kBK * tile + 16 * lane, u.keys); };
+        auto place_rows = [&]() {
+            const int lane = opaque_lane();
+            int e[kPlaceTiles / NW];
+#pragma unroll
+            for (int x = 0; x < kPlaceTiles / NW; ++x) e[x] = entry_of(a.pages, table, kBK * (first_tile + wave + NW * x) + lane, u.keys);
+#pragma unroll
+            for (int x = 0; x < kPlaceTiles / NW; ++x) {
+                const int tile = wave + NW * x;
+                const KeyRow kr = row_of(a.pages, e[x], kBK * (first_tile + tile) + lane, u.keys);
+                places()[kBK * tile + lane] = kr.off16;
+                const uint64_t there = __ballot(kr.there);
+                if (lane == 0) rows_there()[tile] = there;
+            }
+        };
+        auto arrived = [&](int tile) {  // behind the barrier that follows step_to
+            if (!RUNS && tile == first_tile) ok = __ballot(rows_there()[opaque_lane() & (kPlaceTiles - 1)] == ~0ull);
+        };
         auto start_at = [&](int tile) {
+            first_tile = tile;
             if constexpr (RUNS) {
                 const KeyRow kr = row_of(a.pages, ask(tile), kBK * tile + 16 * lane, u.keys);
                 ok = __ballot(kr.there);
                 off_a = kr.off16;
-                first_tile = tile;
                 entry = ask(tile + kTurns);
             } else {
-                const KeyRow r1 = row_of(a.pages, ask(tile + 1), kBK * (tile + 1) + lane, u.keys);
-                const KeyRow r2 = row_of(a.pages, ask(tile + 2), kBK * (tile + 2) + lane, u.keys);
-                there_a = __ballot(r1.there);
-                there_b = __ballot(r2.there);
-                off_a = r1.off16;
-                off_b = r2.off16;
-                entry = ask(tile + 3);
+                place_rows();
+                __syncthreads();
+                arrived(tile);
             }
         };
         auto step_to = [&](int tile) {  // tile: the next turn's
+            if (tile - first_tile < kTurns) return;
+            first_tile = tile;
             if constexpr (RUNS) {
-                if (tile - first_tile < kTurns) return;
                 const KeyRow kr = row_of(a.pages, entry, kBK * tile + 16 * lane, u.keys);
                 ok = __ballot(kr.there);
                 off_a = kr.off16;
-                first_tile = tile;
                 entry = ask(tile + kTurns);
             } else {
-                there_c = there_a;
-                off_a = off_b;
-                there_a = there_b;
-                const KeyRow kr = row_of(a.pages, entry, kBK * (tile + 2) + lane, u.keys);
-                there_b = __ballot(kr.there);
-                off_b = kr.off16;
-                entry = ask(tile + 3);
+                half ^= 1;  // (others may be reading this half still)
+                place_rows();
             }
         };
         // bit r: key r of the tile j + n is there (n = 0, 1, 2)
@@ -874,25 +898,26 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 const int left = u.keys - kBK * (j + n);
                 return left >= kBK ? x : left <= 0 ? 0ull : x & ((1ull << left) - 1);
             } else {
-                return n == 0 ? there_c : n == 1 ? there_a : there_b;
+                const uint64_t x = rows_there()[j + n - first_tile];
+                return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
             }
         };
         auto pages_there = [&](int j) -> bool {  // of tiles j .. j + 2, whole ones
             if constexpr (RUNS) return ((uint32_t)(ok >> (4 * (j - first_tile))) & 0xfffu) == 0xfffu;
-            else return (there_c & there_a & there_b) == ~0ull;
+            else return ((uint32_t)(ok >> (j - first_tile)) & 7u) == 7u;
         };
-        // This wavefront's 16 rows of a part of tile j + 1's turn, from row `from` of the tile on (0, or for K 32: past its end the next
+        // This wavefront's rows of a part of tile j + 1's turn, from row `from` of the tile on (0, or for K 32: past its end the next
         // tile's follow).  whole: all of them are there.
         auto fetch_part = [&](int lane, const uint8_t* cache, uint8_t* buf, int j, int from, bool v, auto whole)
             __attribute__((always_inline)) {
-            const int row_l = lane / R::PPR, slot_l = lane % R::PPR, first = 16 * wave + from;
+            const int row_l = lane / R::PPR, slot_l = lane % R::PPR, first = RW * wave + from;
             const uint32_t piece = 16 * (v ? R::v_piece(row_l, slot_l) : R::k_piece(row_l, slot_l));
             uint8_t* const dst = buf + wave * NL * (v ? R::VG : R::KG);
             const uint64_t there = whole ? ~0ull : first < kBK ? there_of(j, 1) >> first : there_of(j, 2) >> (first - kBK);
             if constexpr (RUNS) {
                 const uint8_t* src = cache + (uint64_t)(uint32_t)__builtin_amdgcn_readlane(
-                                                 (int)off_a, 4 * (j + 1 - first_tile) + wave + from / 16) * 16;
-                const uint32_t row = 16 * a.pages.token16, in = row_l * row + piece;
+                                                 (int)off_a, 4 * (j + 1 - first_tile) + first / 16) * 16;
+                const uint32_t row = 16 * a.pages.token16, in = (row_l + first % 16) * row + piece;
 #pragma unroll
                 for (int p = 0; p < NL; ++p) {
                     uint8_t* const to = dst + p * (v ? R::VG : R::KG);
@@ -900,11 +925,10 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                     else *reinterpret_cast<u32x4*>(to + 16 * lane) = mk4(0, 0, 0, 0);
                 }
             } else {
-                const uint32_t off16 = first < kBK ? off_a : off_b;
+                const uint32_t* const from_row = places() + kBK * (j + 1 - first_tile) + first + row_l;
                 uint32_t at[NL];
 #pragma unroll
-                for (int p = 0; p < NL; ++p)
-                    at[p] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((first + p * RPI + row_l) & 63), (int)off16);
+                for (int p = 0; p < NL; ++p) at[p] = from_row[p * RPI];
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int p = 0; p < NL; ++p) {
@@ -919,9 +943,10 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             fetch_part(lane, kc, kbuf(b), j, 32, false, whole);
             fetch_part(lane, vc, vbuf(b), j, 0, true, whole);
         };
-        auto landed = [&]() {
+        auto landed = [&](int tile) {
             __builtin_amdgcn_s_waitcnt(kWaitLoads);
             __syncthreads();
+            arrived(tile);
         };
 
         auto is_masked = [&](int tile, uint64_t there) { return there != ~0ull || kBK * tile < lo || kBK * tile + kBK > hi; };
@@ -942,13 +967,13 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             return k;
         };
         bool far = false;  // a row's maximum is too large for (s - m) c in one fma (tile_step)
-        auto raise = [&](const f32x16& S) {
+        auto raise = [&](scores_t& S) {
             far = false;
 #pragma unroll
             for (int q = 0; q < QB; ++q) {
-                float mx = S[8 * q];
+                float mx = S[q / 2][8 * (q % 2)];
 #pragma unroll
-                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, S[8 * q + e]);
+                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, S[q / 2][8 * (q % 2) + e]);
                 mx = max_across_rows16(mx);
                 const float to = mx > top[q] ? mx : m[q];
                 const float alpha = __builtin_amdgcn_exp2f((m[q] - to) * scale);
@@ -966,21 +991,22 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             far = __any(far);
         };
         // slice x = (q, w): word w of the operand of the half's keys for row block q
-        auto exp_slice = [&](f32x16& S, int x) {
-            const int q = x / 4, e = 2 * x;
-            S[e] = __builtin_amdgcn_exp2f(fmaf(S[e], scale, off[q]));
-            S[e + 1] = __builtin_amdgcn_exp2f(fmaf(S[e + 1], scale, off[q]));
+        auto exp_slice = [&](scores_t& S, int x) {
+            const int q = x / 4, e = 2 * (x % 8);
+            S[q / 2][e] = __builtin_amdgcn_exp2f(fmaf(S[q / 2][e], scale, off[q]));
+            S[q / 2][e + 1] = __builtin_amdgcn_exp2f(fmaf(S[q / 2][e + 1], scale, off[q]));
         };
-        auto pack_slice = [&](f32x16& S, uint32_t (&P)[QB][4], int x) {
-            const int q = x / 4, e = 2 * x;
-            P[q][x % 4] = pack2<OP>(S[e], S[e + 1]);
-            l[q][0] += S[e];
-            l[q][1] += S[e + 1];
+        auto pack_slice = [&](scores_t& S, uint32_t (&P)[QB][4], int x) {
+            const int q = x / 4, e = 2 * (x % 8);
+            P[q][x % 4] = pack2<OP>(S[q / 2][e], S[q / 2][e + 1]);
+            l[q][0] += S[q / 2][e];
+            l[q][1] += S[q / 2][e + 1];
         };
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        auto score = [&](u32x4 k, int f, int q, f32x16& S) {
+        auto score = [&](u32x4 k, int f, int q, scores_t& S) {
             const int ks = f >> 1, kb = f & 1;
-            S = ks == 0 ? mfma16_q_init<OP>(k, Q[q][ks], zero, S, 2 * q + kb) : mfma16_q<OP>(k, Q[q][ks], S, 2 * q + kb);
+            const int at = 2 * (q % 2) + kb;
+            S[q / 2] = ks == 0 ? mfma16_q_init<OP>(k, Q[q][ks], zero, S[q / 2], at) : mfma16_q<OP>(k, Q[q][ks], S[q / 2], at);
         };
         auto product = [&](u32x4 v, const uint32_t (&P)[QB][4], int cb, int q) {
             O[cb / 4][q] = mfma16_q<OP>(v, mk4(P[q][0], P[q][1], P[q][2], P[q][3]), O[cb / 4][q], cb % 4);
@@ -989,7 +1015,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
         // One half (its scores in Sc) and the next one's scores (into Sn), no key of either masked for any row.  kn: the next one's
         // rows of K, vb: this one's of V
         // (the lane's own addresses in them).
-        auto plain_half = [&](f32x16& Sc, f32x16& Sn, const uint8_t* kn, uint8_t* const (&vb)[4], auto half) __attribute__((always_inline)) {
+        auto plain_half = [&](scores_t& Sc, scores_t& Sn, const uint8_t* kn, uint8_t* const (&vb)[4], auto half) __attribute__((always_inline)) {
             constexpr int H = decltype(half)::value;
             u32x4 kf[NKF], vf[NCB];
             auto k_frag = [&](int f) { return k_fragment_at<D>(kn, 32 * H + 16 * (f & 1), f >> 1); };
@@ -1004,37 +1030,49 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             for (int f = 0; f < NKF; ++f) {
                 if (f + LA < NKF) kf[f + LA] = k_frag(f + LA);
                 if (f >= NKF - LA) vf[f - (NKF - LA)] = v_frag(f - (NKF - LA));
-                score(kf[f], f, 0, Sn);
+#pragma unroll
+                for (int q = 0; q < (QB + 1) / 2; ++q) score(kf[f], f, q, Sn);
 #pragma unroll
                 for (int x = f * NCH / NKF; x < (f + 1) * NCH / NKF; ++x)
                     if (x + PRE < NCH) exp_slice(Sc, x + PRE);
                 __builtin_amdgcn_sched_barrier(0);
-                score(kf[f], f, 1, Sn);
+#pragma unroll
+                for (int q = (QB + 1) / 2; q < QB; ++q) score(kf[f], f, q, Sn);
 #pragma unroll
                 for (int x = f * NCH / NKF; x < (f + 1) * NCH / NKF; ++x) pack_slice(Sc, P, x);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            float mx[QB] = {-INFINITY, -INFINITY};
-            auto max_slice = [&](int x) { mx[x & 1] = max3(mx[x & 1], Sn[8 * (x & 1) + 2 * (x >> 1)], Sn[8 * (x & 1) + 2 * (x >> 1) + 1]); };
+            float mx[QB];
+#pragma unroll
+            for (int q = 0; q < QB; ++q) mx[q] = -INFINITY;
+            auto max_slice = [&](int x) {
+                const int q = x % QB, e = 8 * (q % 2) + 2 * (x / QB);
+                mx[q] = max3(mx[q], Sn[q / 2][e], Sn[q / 2][e + 1]);
+            };
 #pragma unroll
             for (int v = 0; v < NCB; ++v) {
                 if (v + LA < NCB) vf[v + LA] = v_frag(v + LA);
-                product(vf[v], P, v, 0);
+#pragma unroll
+                for (int q = 0; q < (QB + 1) / 2; ++q) product(vf[v], P, v, q);
                 if (v >= 1) {
 #pragma unroll
                     for (int x = (v - 1) * NCH / NCB; x < v * NCH / NCB; ++x) max_slice(x);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                product(vf[v], P, v, 1);
+#pragma unroll
+                for (int q = (QB + 1) / 2; q < QB; ++q) product(vf[v], P, v, q);
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int x = (NCB - 1) * NCH / NCB; x < NCH; ++x) max_slice(x);
-            if (__any(mx[0] > top[0] || mx[1] > top[1])) raise(Sn);
+            bool above = false;
+#pragma unroll
+            for (int q = 0; q < QB; ++q) above = above || mx[q] > top[q];
+            if (__any(above)) raise(Sn);
         };
 
         // One half, whatever is masked of it, and the next one's scores (if there is one) into the same registers.
-        auto any_half = [&](f32x16& S, bool masked, int key0, uint32_t there, uint8_t* vb, bool more, bool masked_next, uint32_t there_next,
+        auto any_half = [&](scores_t& S, bool masked, int key0, uint32_t there, uint8_t* vb, bool more, bool masked_next, uint32_t there_next,
                             const uint8_t* kn) __attribute__((always_inline)) {
             const int ln = opaque_lane(), i = ln & 15, g = ln >> 4;
             if (far) {
@@ -1043,7 +1081,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                     const bool some = m[q] != kNoScore;
                     off[q] = some ? 0.f : off[q];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) S[8 * q + e] -= some ? m[q] : 0.f;
+                    for (int e = 0; e < 8; ++e) S[q / 2][8 * (q % 2) + e] -= some ? m[q] : 0.f;
                 }
             }
             uint32_t P[QB][4];
@@ -1086,7 +1124,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 for (int q = 0; q < QB; ++q) {
                     const uint32_t k = keep_of(q, key0 + 32, there_next);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) S[8 * q + e] = (k >> e) & 1 ? S[8 * q + e] : -INFINITY;
+                    for (int e = 0; e < 8; ++e) S[q / 2][8 * (q % 2) + e] = (k >> e) & 1 ? S[q / 2][8 * (q % 2) + e] : -INFINITY;
                 }
             }
             raise(S);
@@ -1099,18 +1137,18 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
             // as if tile begin - 1's turn were over: the first half's rows of K, in the other buffer's second half, and the first turn's
             int j = begin - 1;
             start_at(j);
-            if (wave < 2) fetch_part(lane, kc, kbuf(1) + KH, j, 0, false, some);
+            if (wave < NW / 2) fetch_part(lane, kc, kbuf(1) + KH, j, 0, false, some);
             fetch(lane, j, 0, some);
             j = begin;
             step_to(j);
-            landed();
+            landed(j);
             // keys [key0, key0 + 32) of which the lane's rows see some, those of the half whose scores S are
-            auto mask = [&](f32x16& S, int key0, uint32_t there) {
+            auto mask = [&](scores_t& S, int key0, uint32_t there) {
 #pragma unroll
                 for (int q = 0; q < QB; ++q) {
                     const uint32_t k = keep_of(q, key0, there);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) S[8 * q + e] = (k >> e) & 1 ? S[8 * q + e] : -INFINITY;
+                    for (int e = 0; e < 8; ++e) S[q / 2][8 * (q % 2) + e] = (k >> e) & 1 ? S[q / 2][8 * (q % 2) + e] : -INFINITY;
                 }
             };
             const uint64_t there_0 = there_of(j, 0);
@@ -1132,7 +1170,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 for (int x = 0; x < 4; ++x) v_l[x] = v_lane<D>(x, ln & 15, ln >> 4);
                 // Turns in which neither the tiles that are used nor what is fetched meanwhile holds a masked key.
                 while (j + 2 < end && !far && kBK * j >= lo && kBK * j + 2 * kBK <= hi && pages_there(j)) {
-                    fetch(ln, j, b ^ 1, whole);
+                    fetch(RUNS ? ln : opaque_lane(), j, b ^ 1, whole);
                     const uint8_t* const kl = kbuf(b) + k_l;
                     uint8_t* vl[4];
 #pragma unroll
@@ -1142,7 +1180,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                     ++j;
                     b ^= 1;
                     step_to(j);
-                    landed();
+                    landed(j);
                 }
                 const bool more = j + 1 < end;
                 if (more) fetch(opaque_lane(), j, b ^ 1, some);
@@ -1154,7 +1192,7 @@ __global__ void __launch_bounds__(64 * kBigWaves, 2) attn_paged_big_kernel(const
                 ++j;
                 b ^= 1;
                 step_to(j);
-                landed();
+                landed(j);
             }
         }
         RowState<D, QB> st;
@@ -1256,17 +1294,27 @@ hipError_t launch_few(const PagedAttnArgs& a, int units, int nw, hipStream_t s) 
     else e = a.pages.runs ? launch_few_n<D, OP, QB, true, 4>(a, units, s) : launch_few_n<D, OP, QB, false, 4>(a, units, s);
     return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB, 8>(a, units, s);
 }
-template <int D, int OP>
-hipError_t launch_big(const PagedAttnArgs& a, int units, hipStream_t s) {
-    static std::atomic<uint64_t> done_runs{0}, done_rows{0};
-    const auto kern = a.pages.runs ? attn_paged_big_kernel<D, OP, true> : attn_paged_big_kernel<D, OP, false>;
-    std::atomic<uint64_t>& done = a.pages.runs ? done_runs : done_rows;
-    hipError_t e = allow_dynamic_lds(kern, big_lds<D>(), done);
+template <int D, int OP, bool RUNS, int NW, int QB>
+hipError_t launch_big_n(const PagedAttnArgs& a, int units, hipStream_t s) {
+    static std::atomic<uint64_t> done{0};
+    const auto kern = attn_paged_big_kernel<D, OP, RUNS, NW, QB>;
+    constexpr int lds = big_lds<D, RUNS>();
+    hipError_t e = allow_dynamic_lds(kern, lds, done);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * kBigWaves), big_lds<D>(), s, a);
+    hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * NW), lds, s, a);
     e = hipGetLastError();
-    if (e != hipSuccess || !a.pieces) return e;
-    return launch_join<D, kPagedBigRows, 4>(a, units, s);
+    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB * NW, 4>(a, units, s);
+}
+template <int D, int OP>
+hipError_t launch_big(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t s) {
+    const int units = plan.big_units;
+    if constexpr (D == 128) {
+        if (!a.pages.runs) return launch_big_n<D, OP, false, 8, 1>(a, units, s);
+    } else {
+        if (!a.pages.runs)
+            return plan.big_waves == 8 ? launch_big_n<D, OP, false, 8, 2>(a, units, s) : launch_big_n<D, OP, false, 4, 2>(a, units, s);
+    }
+    return plan.big_waves == 8 ? launch_big_n<D, OP, true, 8, 2>(a, units, s) : launch_big_n<D, OP, true, 4, 2>(a, units, s);
 }
 
 template <int D, int OP>
@@ -1292,15 +1340,15 @@ hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_
         a.rows_hi = 0x7fffffff;
         a.least = 4;
         ws += plan.few_bytes;
-        parts(plan.big_pieces, plan.big_each, plan.big_cap, kPagedBigRows);
-        e = launch_big<D, OP>(a, plan.big_units, s);
+        parts(plan.big_pieces, plan.big_each, plan.big_cap, 16 * plan.big_qb * plan.big_waves);
+        e = launch_big<D, OP>(a, plan, s);
     }
     return e;
 }
 
 }  // namespace
 
-PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int max_q) {
+PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int max_q, int runs) {
     PagedPlan p{};
     const int64_t G = H / Hk, rows = (int64_t)N * G, some = N < R ? N : R;  // requests with a new token
     const int64_t most_q = max_q > 0 && max_q < N ? max_q : N;              // new tokens of a request
@@ -1350,7 +1398,12 @@ PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int m
         p.few_bytes = l.bytes;
     }
     if (p.big) {
-        const Layout l = layout(kPagedBigRows, 2 * kCUs, 1.0, 6.0, 4, 6.0);
+        const bool one = D == 128 && !runs;  // a row block a wavefront
+        const Layout four = layout(128, one ? kCUs : 2 * kCUs, one ? 0.62 : 1.0, one ? 12.0 : 6.0, 4, 6.0), eight = layout(256, kCUs, 0.93, 12.0, 4, 6.0);
+        const bool wide = !one && eight.time < four.time;
+        const Layout& l = wide ? eight : four;
+        p.big_waves = one || wide ? 8 : 4;
+        p.big_qb = one ? 1 : 2;
         p.big_units = l.units;
         p.big_pieces = l.pieces;
         p.big_each = l.each;

@@ -108,15 +108,15 @@ struct PagedAttnArgs {
 struct PagedPlan {
     bool few, big;
     int few_qb, few_waves;        // 16-row blocks of a few-row tile; wavefronts of its workgroup
+    int big_qb, big_waves;        // 16-row blocks of a wavefront, wavefronts of a many-row tile's workgroup
     int few_units, big_units;     // workgroups
     int few_pieces, big_pieces;   // units wanted per key head; 0: every tile whole
     int few_each, big_each;       // of a tile, as far as is known
     int few_cap, big_cap;
     size_t few_bytes, big_bytes;  // of workspace
 };
-constexpr int kPagedBigRows = 128;
 // How a call is laid over the chip (no device is touched; the host tests read it).  max_q, max_kv: 0 = not known.
-PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int max_q);
+PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int max_q, int runs);
 hipError_t launch_attn_paged(const PagedAttnArgs& a, const PagedPlan& plan, int D, int op, uint8_t* workspace, hipStream_t s);
 
 }  // namespace dit

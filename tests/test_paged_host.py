@@ -127,16 +127,16 @@ def test_workspace_size():
         assert B.dit_attn_paged_workspace_bytes(attn_params(**bad)) == 0
 
 
-def plan(N, R, H, Hk, D, keys, max_q):
+def plan(N, R, H, Hk, D, keys, max_q, runs=1):
     class Plan(ctypes.Structure):
         _fields_ = [("few", ctypes.c_bool), ("big", ctypes.c_bool)] + [(n, ctypes.c_int) for n in (
-            "few_qb", "few_waves", "few_units", "big_units", "few_pieces", "big_pieces", "few_each", "big_each", "few_cap", "big_cap")] + [
+            "few_qb", "few_waves", "big_qb", "big_waves", "few_units", "big_units", "few_pieces", "big_pieces", "few_each", "big_each", "few_cap", "big_cap")] + [
             ("few_bytes", ctypes.c_size_t), ("big_bytes", ctypes.c_size_t)]
 
-    f = B.lib()._ZN3dit10plan_pagedEiiiiili
+    f = B.lib()._ZN3dit10plan_pagedEiiiiilii
     f.restype = Plan
-    f.argtypes = [ctypes.c_int] * 5 + [ctypes.c_long, ctypes.c_int]
-    return f(N, R, H, Hk, D, keys, max_q)
+    f.argtypes = [ctypes.c_int] * 5 + [ctypes.c_long, ctypes.c_int, ctypes.c_int]
+    return f(N, R, H, Hk, D, keys, max_q, runs)
 
 
 @pytest.mark.parametrize("N,R,H,Hk,max_q,few,big", [
