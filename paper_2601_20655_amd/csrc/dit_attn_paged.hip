@@ -1317,6 +1317,7 @@ hipError_t launch_big(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
     return plan.big_waves == 8 ? launch_big_n<D, OP, true, 8, 2>(a, units, s) : launch_big_n<D, OP, true, 4, 2>(a, units, s);
 }
 
+constexpr int kFewRows = 64;  // of a request, by the kernel for few
 template <int D, int OP>
 hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_t* ws, hipStream_t s) {
     PagedAttnArgs a = args;
@@ -1330,13 +1331,13 @@ hipError_t launch_paged(const PagedAttnArgs& args, const PagedPlan& plan, uint8_
     hipError_t e = hipSuccess;
     if (plan.few) {
         a.rows_lo = 1;
-        a.rows_hi = plan.big ? 16 * plan.few_qb : 0x7fffffff;
+        a.rows_hi = plan.big ? kFewRows : 0x7fffffff;
         a.least = 2;
         parts(plan.few_pieces, plan.few_each, plan.few_cap, 16 * plan.few_qb);
         e = plan.few_qb == 1 ? launch_few<D, OP, 1>(a, plan.few_units, plan.few_waves, s) : launch_few<D, OP, 2>(a, plan.few_units, plan.few_waves, s);
     }
     if (e == hipSuccess && plan.big) {
-        a.rows_lo = plan.few ? 16 * plan.few_qb + 1 : 1;
+        a.rows_lo = plan.few ? kFewRows + 1 : 1;
         a.rows_hi = 0x7fffffff;
         a.least = 4;
         ws += plan.few_bytes;
@@ -1354,26 +1355,44 @@ PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int m
     const int64_t most_q = max_q > 0 && max_q < N ? max_q : N;              // new tokens of a request
     p.few_qb = most_q * G > 16 ? 2 : 1;
     const bool uniform = most_q * some <= 2 * (int64_t)N;  // few requests have far fewer new tokens than that
-    p.few = most_q * G <= 32 || !uniform;
-    p.big = most_q * G > 32;
+    // (33 to 64 rows, by 32-row tiles and by those of many rows: 1 to 16 requests, 1,024 to 8,192 keys 31 and 40 us, 34 and 44, 41 and
+    // 48; 80 rows 64 and 49)
+    p.few = most_q * G <= kFewRows || !uniform;
+    p.big = most_q * G > kFewRows;
     const int64_t key_tiles = max_keys > 0 ? (max_keys + kBK - 1) / kBK : 1;
-    // Time in key tiles of a workgroup: rounds of workgroups (`slots` at a time), each as long as its keys (`step` a tile) and its two
-    // ends; tiles in pieces need the launch that joins them.
+    // Time in key tiles of one of two 4-wavefront workgroups of a compute unit: rounds of workgroups (`slots` at a time), each as long as
+    // its keys (`step` a tile, `alone` where a compute unit has no second workgroup) and its two ends; tiles in pieces need the launch
+    // that joins them, and room.  The constants are those under which, of 42 calls (1 to 4,680 new tokens, 257 to 100,000 keys, 1 to 256
+    // requests, measured in every layout), the layout chosen is the fastest or up to 9 % from it; bytes bound the few-row kernel, so
+    // that its steps are short against its ends.
+    struct Costs {
+        int BQ;
+        int64_t slots;
+        double step, alone, ends;
+        int least;
+        double join, room;  // once, and for 10^6 numbers
+        bool even;          // of several requests, whose lengths may differ: fill the slots where pieces have 48 tiles left
+    };
     struct Layout {
         double time;
         int units, pieces, each, cap;
         size_t bytes;
     };
-    auto layout = [&](int BQ, int64_t slots, double step, double ends, int least, double join) {
+    auto layout = [&](const Costs& c) {
+        const int BQ = c.BQ;
         // tiles of a key head: at most (whatever q_start says, with what is left over of each request), and as far as is known
         const int64_t most = (rows + some * (BQ - 1)) / BQ;
         const int64_t each = (most_q * G + BQ - 1) / BQ, tiles = some * each < most ? some * each : most;
         auto time = [&](int n) {
-            const int64_t rounds = (tiles * Hk * n + slots - 1) / slots;
-            return (double)rounds * (step * (double)((key_tiles + n - 1) / n) + ends) + (n > 1 ? join : 0.0);
+            const int64_t units = tiles * Hk * n, rounds = units / c.slots, rest = units % c.slots;
+            const double keys = (double)((key_tiles + n - 1) / n);
+            return (double)rounds * (c.step * keys + c.ends) + (rest ? (rest > kCUs ? c.step : c.alone) * keys + c.ends : 0.0) +
+                   (n > 1 ? c.join + c.room * 1e-6 * (double)(units * BQ * D) : 0.0);
         };
         int best = 1;
-        for (int n = 2; n <= 64 && n * (int64_t)least <= key_tiles; ++n) {
+        // (one new token each, 16 to 8,190 keys: with 2 x 4,096 110 us, else 123)
+        while (c.even && some > 1 && tiles * Hk * best < c.slots && key_tiles >= 48 * (best + 1)) ++best;
+        for (int n = best + 1; n <= 64 && n * (int64_t)c.least <= key_tiles; ++n) {
             if ((tiles * n + most) * Hk * BQ > (int64_t)1 << 19) break;  // rows of pieces: 272 MB at head_dim 128
             if (time(n) < 0.97 * time(best)) best = n;
         }
@@ -1388,9 +1407,12 @@ PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int m
         return l;
     };
     if (p.few) {
-        const Layout four = layout(16 * p.few_qb, 2 * kCUs, 1.0, 8.0, 2, 6.0), eight = layout(16 * p.few_qb, kCUs, 0.55, 8.0, 4, 6.0);
-        const Layout& l = eight.time < four.time ? eight : four;
-        p.few_waves = eight.time < four.time ? 8 : 4;
+        const Layout four = layout({16 * p.few_qb, 2 * kCUs, 1.0, 0.25, 49.0, 2, 1.9, 0.006, true});
+        const Layout eight = layout({16 * p.few_qb, kCUs, 0.09, 0.09, 57.0, 4, 1.9, 0.006, false});
+        // (whole tiles, no more of them than compute units: 257 keys x 40/8 heads 10.7 us by 8 wavefronts, 11.0 by 4; 700 x 40 13.5, 14.1)
+        const bool wide = (some == 1 && eight.time < four.time) || (four.each == 1 && eight.each == 1 && four.units <= kCUs);
+        const Layout& l = wide ? eight : four;
+        p.few_waves = wide ? 8 : 4;
         p.few_units = l.units;
         p.few_pieces = l.pieces;
         p.few_each = l.each;
@@ -1399,7 +1421,8 @@ PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int m
     }
     if (p.big) {
         const bool one = D == 128 && !runs;  // a row block a wavefront
-        const Layout four = layout(128, one ? kCUs : 2 * kCUs, one ? 0.62 : 1.0, one ? 12.0 : 6.0, 4, 6.0), eight = layout(256, kCUs, 0.93, 12.0, 4, 6.0);
+        const Layout four = layout(one ? Costs{128, kCUs, 0.62, 0.62, 12.0, 4, 4.0, 0.011, false} : Costs{128, 2 * kCUs, 1.0, 0.53, 7.0, 4, 4.0, 0.011, false});
+        const Layout eight = layout({256, kCUs, 0.7, 0.7, 41.0, 4, 4.0, 0.011, false});
         const bool wide = !one && eight.time < four.time;
         const Layout& l = wide ? eight : four;
         p.big_waves = one || wide ? 8 : 4;
