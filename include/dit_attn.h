@@ -533,8 +533,8 @@ dit_status dit_linear_quant_forward(const int8_t *x, const float *x_scale, const
  * every step.  What the host tells besides (max_q, max_kv) is for planning only.
  *
  * Tokens of all requests are packed: rows [N, heads, D] (dit_strides, batch ignored).  Positions: int32 [N, 3] DEVICE, dense,
- * (t, h, w) of every token, any integer; rotation as in dit_self_attn_params.  cos and sin are within 2^-22 of the formula's at
- * every position; the arithmetic is fp32, rounded once to the type that is written.  fp16 saturates at +-65504.
+ * (t, h, w) of every token, any integer; rotation as in dit_self_attn_params.  cos and sin are those of an angle
+ * within 2^-22, and 2^-51 of itself, of the formula's; the arithmetic is fp32, rounded once to the type that is written.  fp16 saturates at +-65504.
  * Normalisation: dit_qk_norm as above (q_gamma: H*D weights, k_gamma: Hk*D; DIT_NORM_TOKEN: over the H*D, or Hk*D, channels of
  * the token), ahead of the rotation.  Rows whose squares fp32 does not hold are scaled by a power of two first.
  */
@@ -574,8 +574,9 @@ dit_status dit_qk_rope_forward(const void *q, const void *k, const int32_t *pos,
  *               share pages.
  *   q_start     int32 [n_requests + 1] DEVICE, ascending from 0: rows q_start[r] .. q_start[r+1]-1 are request r's new tokens.
  *               Rows from q_start[n_requests] on are of no request: neither read nor, where they are outputs, written.
- *   kv_len      int32 [n_requests] DEVICE: tokens of the request, the new ones (its last) included; at most max_pages*page_size count.
- * Counts that are out of range lead to no access out of range: q_start is clamped to 0 .. N, kv_len to 0 .. max_pages*page_size.
+ *   kv_len      int32 [n_requests] DEVICE: tokens of the request, the new ones (its last) included.
+ * Counts that are out of range lead to no access out of range: q_start is clamped to 0 .. N; the attention clamps kv_len to 0 .. the
+ * lesser of max_pages*page_size and 2^31 - 65,536, and no token is written behind the table.
  */
 typedef struct {
     int32_t n_pages, page_size, Hk, D;

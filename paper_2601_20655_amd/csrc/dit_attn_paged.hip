@@ -531,9 +531,10 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
     const int b = lo / kBK, e = hi > lo ? (hi + kBK - 1) / kBK : b;
     begin = b;
     end = e;
-    if (u.pieces > 1) {  // (below 2^26 tiles, at most 64 pieces)
-        begin = b + (int)((uint32_t)(e - b) * (uint32_t)u.piece / (uint32_t)u.pieces);
-        end = b + (int)((uint32_t)(e - b) * (uint32_t)(u.piece + 1) / (uint32_t)u.pieces);
+    if (u.pieces > 1) {  // (the first ones a tile longer than the rest)
+        const int each = (int)((uint32_t)(e - b) / (uint32_t)u.pieces), rest = (e - b) - each * u.pieces;
+        begin = b + u.piece * each + (u.piece < rest ? u.piece : rest);
+        end = begin + each + (u.piece < rest ? 1 : 0);
     }
 }
 

@@ -30,12 +30,14 @@ struct PageArgs {
     int runs;      // 16 tokens from a multiple of 16 on lie in one page, their rows within 2^31 bytes
 };
 
-// Tokens that the table of a request has room for, and those of them that are there.
+// Tokens of a request that attend: those that are there, that its table has room for, and that a few tiles past the last one still
+// have numbers for in 31 bits.
+constexpr int kMostKeys = 0x7fff0000;
 __device__ __forceinline__ int keys_of(const PageArgs& p, int r) {
-    const int64_t room = (int64_t)p.max_pages * p.page.d;
+    const int64_t room = (int64_t)p.max_pages * p.page.d, most = room < kMostKeys ? room : kMostKeys;
     int n = p.kv_len[r];
     n = n < 0 ? 0 : n;
-    return n < room ? n : (int)room;
+    return n < most ? n : (int)most;
 }
 
 // Request of new token t: the last r with q_start[r] <= t, by the wavefront together, 64 entries at a time; -1: of none.

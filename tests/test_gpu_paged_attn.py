@@ -284,3 +284,29 @@ def test_no_tokens():
     q = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
     out, lse = B.dit_attn_paged_forward(q, *c.args([0]), want_lse=True)
     assert out.shape == (0, 2, 64) and lse.shape == (2, 0)
+
+
+def test_one_request_of_almost_all_keys():
+    """500 requests of one token, planned with 22 pieces each, of which one has 2^31 - 65,536 keys (a page of 65,536, over and
+    over): it gets some 11,000 pieces.  Its sum of exponentials is 32,767 times the page's."""
+    import torch
+
+    n, page, D, columns = 500, 65536, 64, 32767
+    k, v = (randn(i, (2, page, 1, D), "bf16") for i in (1, 2))
+    table = np.full((n, columns), 1, np.int32)
+    table[7] = 0
+    lens = np.full(n, 3)
+    lens[7] = columns * page
+    q = randn(3, (n, 1, D), "bf16")
+    out, lse = B.dit_attn_paged_forward(q, k, v, ints(table), ints(np.arange(n + 1)), ints(lens), frame=0, max_q=1, want_lse=True,
+                                        out=torch.empty((n, 1, D), device="cuda"))
+    s = k[0, :, 0].double() @ q[7, 0].double() / 8
+    p = (s - s.max()).exp()
+    want = (p @ v[0, :, 0].double()) / p.sum()
+    # P rounded by 2^-9 of itself (half a step), sums over 2^17 keys a piece and lane and over the pieces
+    assert (out[7, 0].double() - want).abs().max() <= (2.0 ** -8 + 2.0 ** -10) * (p @ v[0, :, 0].double().abs() / p.sum()).max()
+    assert abs(float(lse[0, 7]) - float(s.max() + p.sum().log()) - np.log(columns)) <= 2.0 ** -9
+    s = (k[1, :3, 0].double() @ q[:, 0].double().T).T / 8
+    want = s.softmax(1) @ v[1, :3, 0].double()
+    others = [r for r in range(n) if r != 7]
+    assert (out[others, 0].double() - want[others]).abs().max() <= (2.0 ** -8 + 2.0 ** -18) * v[1, :3].abs().max().double()
