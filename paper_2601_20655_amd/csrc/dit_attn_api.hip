@@ -1672,6 +1672,6 @@ const char* dit_strerror(dit_status s) {
 
 const char* dit_last_hip_error(void) { return g_hip_error; }
 
-int dit_attn_version(void) { return 10901; }  // 1.9.1
+int dit_attn_version(void) { return 11000; }  // 1.10.0
 
 }  // extern "C"
