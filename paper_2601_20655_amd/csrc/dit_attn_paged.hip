@@ -542,7 +542,9 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
 // 16 QB rows; the unit's keys go to the NW wavefronts 32 at a time, each of which has LDS of its own for 32 rows of K and V.
 // Memory bounds it: a wavefront reads its fragments into registers as soon as the rows have landed, and asks for the next ones
 // before it multiplies.  Two workgroups of 4 wavefronts a compute unit, or one of 8 (where there are few: half as many keys one
-// after the other), keep up to 128 KiB on their way.  Their results are joined in LDS.
+// after the other), keep up to 128 KiB on their way.  Their results are joined in LDS.  Measured, one new token a request: 40 heads with
+// keys of their own x 32,760 keys 114 us = 5.9 TB/s, 32 requests of 16 to 8,190 keys x 8 key heads 104 us = 5.2 TB/s, 8 key heads x 257 keys
+// 11.6 (counts, page, rows, products, join and store one after the other).
 template <int D, int NW>
 constexpr int few_lds() { return NW * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
 
@@ -1214,6 +1216,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
 
 // ---- tiles in pieces put together ----
 // D / 4 lanes a row, four channels each, in one pass: UN pieces at a time, all that is read of them asked for before any is used.
+// 1,560 x 12 rows of 128 channels in three pieces 10.2 us, 40 rows in five 5.4 (a wavefront a row: 14.0, 7.5).
 template <int D, int BQ, int UN>
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a) {
     constexpr int LANES = D / 4, PER = 256 / LANES, PARTS = BQ / PER;  // of a row, rows of a workgroup, workgroups of a tile
