@@ -487,35 +487,33 @@ __device__ __forceinline__ void load_rows(const PagedAttnArgs& a, const Unit& u,
     }
 }
 
-// Rows out: normalised, or (a tile in pieces) as they are with their maxima and sums.  l: summed over the row's lanes.
-template <int D, int QB>
-__device__ __forceinline__ void store_rows_of(const PagedAttnArgs& a, const Unit& u, int hk, int rows_of_tile, int row_in_tile,
-                                              int64_t row0, int i, int g, const RowState<D, QB>& st, const float (&l)[QB]) {
+// Channel blocks cb0 .. of row `row` out: normalised, or (a tile in pieces) as they are with their maximum and sum.  l: summed over the
+// row's lanes.  at_tile: the row's place in its tile.
+template <int N>
+__device__ __forceinline__ void store_blocks(const PagedAttnArgs& a, const Unit& u, int hk, int D, int rows_of_tile, int at_tile, int64_t row,
+                                             int g, int cb0, const f32x4 (&O)[N], float m, float l) {
+    const RowPlace p = place_of(a, u, hk, row);
+    if (!p.live) return;
+    if (u.pieces > 1) {
+        if (u.slot >= a.part_cap) return;
+        const int64_t at = ((int64_t)hk * a.part_cap + u.slot) * rows_of_tile + at_tile;
+        float* const o = a.part_o + at * D + 16 * cb0 + 4 * g;
 #pragma unroll
-    for (int q = 0; q < QB; ++q) {
-        const RowPlace p = place_of(a, u, hk, row0 + 16 * q + i);
-        if (u.pieces > 1) {
-            if (u.slot >= a.part_cap || !p.live) continue;
-            const int64_t at = ((int64_t)hk * a.part_cap + u.slot) * rows_of_tile + row_in_tile + 16 * q + i;
-            float* const o = a.part_o + at * D + 4 * g;
-#pragma unroll
-            for (int cb = 0; cb < D / 16; ++cb) *reinterpret_cast<f32x4*>(o + 16 * cb) = st.O[q][cb];
-            if (g == 0) a.part_ml[at] = make_float2(st.m[q] * a.scale_log2, l[q]);
-            continue;
-        }
-        if (!p.live) continue;
-        const float inv = l[q] > 0.f || l[q] != l[q] ? 1.0f / l[q] : 0.f;
-        const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + 4 * g;
-#pragma unroll
-        for (int cb = 0; cb < D / 16; ++cb) {
-            f32x4 v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = st.O[q][cb][r] * inv;
-            store4(a.out, off + 16 * cb, a.out_type, v);
-        }
-        if (a.lse && g == 0)
-            a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (st.m[q] * a.scale_log2 + __builtin_amdgcn_logf(l[q])) * 0.6931471805599453f;
+        for (int cb = 0; cb < N; ++cb) *reinterpret_cast<f32x4*>(o + 16 * cb) = O[cb];
+        if (g == 0 && cb0 == 0) a.part_ml[at] = make_float2(m * a.scale_log2, l);
+        return;
     }
+    const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+    const int64_t off = (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + 16 * cb0 + 4 * g;
+#pragma unroll
+    for (int cb = 0; cb < N; ++cb) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = O[cb][r] * inv;
+        store4(a.out, off + 16 * cb, a.out_type, v);
+    }
+    if (a.lse && g == 0 && cb0 == 0)
+        a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (m * a.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // Key tiles of the unit: from the first key that its first token sees to the last that its last token sees, and of those its
@@ -710,9 +708,11 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_few_kernel(const PagedA
             f[q] = __builtin_amdgcn_exp2f((st.m[q] - top) * a.scale_log2);
             st.m[q] = top;
         }
-        // O: wavefront w > 0 leaves its own, wavefront 0 adds them up in order
-        static_assert(2048 + (NW - 1) * D * 64 <= few_lds<D, NW>() && NW * BQ * 8 <= 2048, "room for the results");
-        float* const area = reinterpret_cast<float*>(smem + 2048);  // [wave - 1][channel block][lane][4]
+        // O: every wavefront leaves its own, and adds up all of them, in order, of channel blocks of its own
+        constexpr int NB = D / 16 < NW ? 1 : D / 16 / NW;
+        static_assert(2048 + NW * D * 64 <= few_lds<D, NW>() && NW * BQ * 8 <= 2048, "room for the results");
+        float* const area = reinterpret_cast<float*>(smem + 2048);  // [wave][channel block][lane][4]
+        const int cb0 = wave * NB;
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
             // (a block of 16 rows at a time: D / 16 pieces of 1 KiB a wavefront)
@@ -721,21 +721,22 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_few_kernel(const PagedA
             for (int cb = 0; cb < D / 16; ++cb) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) st.O[q][cb][r] *= f[q];
-                if (wave > 0) *reinterpret_cast<f32x4*>(area + (((wave - 1) * (D / 16) + cb) * 64 + lane) * 4) = st.O[q][cb];
+                *reinterpret_cast<f32x4*>(area + ((wave * (D / 16) + cb) * 64 + lane) * 4) = st.O[q][cb];
             }
             __syncthreads();
-            if (wave == 0) {
+            if (cb0 < D / 16) {
+                f32x4 sum[NB];
 #pragma unroll
-                for (int cb = 0; cb < D / 16; ++cb)
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int w = 0; w < NW - 1; ++w) {
-                        const f32x4 x = *reinterpret_cast<const f32x4*>(area + ((w * (D / 16) + cb) * 64 + lane) * 4);
+                    for (int w = 0; w < NW; ++w) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(area + ((w * (D / 16) + cb0 + n) * 64 + lane) * 4);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) st.O[q][cb][r] += x[r];
+                        for (int r = 0; r < 4; ++r) sum[n][r] = w ? sum[n][r] + x[r] : x[r];
                     }
+                store_blocks(a, u, hk, D, BQ, 16 * q + i, row0 + 16 * q + i, g, cb0, sum, st.m[q], l[q]);
             }
         }
-        if (wave == 0) store_rows_of<D, QB>(a, u, hk, BQ, 0, row0, i, g, st, l);
         __syncthreads();
     }
 }
@@ -1198,18 +1199,15 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
                 landed(j);
             }
         }
-        RowState<D, QB> st;
-        float sums[QB];
 #pragma unroll
         for (int q = 0; q < QB; ++q) {
-            st.m[q] = m[q];
-            sums[q] = sum_across_rows16(l[q][0] + l[q][1]);
+            f32x4 o[NCB];
 #pragma unroll
             for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) st.O[q][cb][r] = O[cb / 4][q][4 * (cb % 4) + r];
+                for (int r = 0; r < 4; ++r) o[cb][r] = O[cb / 4][q][4 * (cb % 4) + r];
+            store_blocks(a, u, hk, D, BQ, (wave * QB + q) * 16 + i, row0 + 16 * q + i, g, 0, o, m[q], sum_across_rows16(l[q][0] + l[q][1]));
         }
-        store_rows_of<D, QB>(a, u, hk, BQ, wave * 16 * QB, row0, i, g, st, sums);
         __syncthreads();
     }
 }
@@ -1395,12 +1393,17 @@ PagedPlan plan_paged(int N, int R, int H, int Hk, int D, int64_t max_keys, int m
         };
         int best = 1;
         // (one new token each, 16 to 8,190 keys: with 2 x 4,096 110 us, else 123)
-        while (c.even && some > 1 && tiles * Hk * best < c.slots && key_tiles >= 48 * (best + 1)) ++best;
+        auto room = [&](int n) { return (tiles * n + most) * Hk * BQ <= (int64_t)1 << 19; };  // rows of pieces: 272 MB at head_dim 128
+        while (c.even && some > 1 && tiles * Hk * best < c.slots && key_tiles >= 48 * (best + 1) && room(best + 1)) ++best;
+        double least = time(best);
         for (int n = best + 1; n <= 64 && n * (int64_t)c.least <= key_tiles; ++n) {
-            if ((tiles * n + most) * Hk * BQ > (int64_t)1 << 19) break;  // rows of pieces: 272 MB at head_dim 128
-            if (time(n) < 0.97 * time(best)) best = n;
+            if (!room(n)) break;
+            const double t = time(n);
+            if (t >= 0.97 * least) continue;
+            best = n;
+            least = t;
         }
-        Layout l{time(best), 0, 0, best, 0, 0};
+        Layout l{least, 0, 0, best, 0, 0};
         if (best > 1) {
             l.pieces = (int)(tiles * best);
             l.cap = (int)(tiles * best + most);
