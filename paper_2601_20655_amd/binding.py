@@ -882,6 +882,15 @@ def _stream_on(what, stream, device):
     return _stream_ptr(stream)
 
 
+def _empty(stream, shape, dtype, device):
+    """A new tensor that is free to be written on that stream (None: the current one): the allocator hands out again what work
+    queued on its own stream is still using, so another stream's has to come from that stream's share."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _check_range(what, name, n):
     """A whole number that the library holds in 32 bits; packing would refuse a larger one with another error."""
     if not 0 <= n <= _MOST_COUNT:
@@ -953,7 +962,7 @@ def dit_qk_rope_forward(q, k, pos, split=(0, 0, 0), q_out=None, k_out=None, out_
         H = q.shape[1]
         sq = _token_strides(what, "q", q, (N, H, D), device)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+            q_out = _empty(stream, q.shape, out_dtype or q.dtype, q.device)
         sqo = _token_strides(what, "q_out", q_out, (N, H, D), device)
         code = _dtype16_code(what, "q_out", q_out)
         qp, qop = q.data_ptr(), q_out.data_ptr()
@@ -967,7 +976,7 @@ def dit_qk_rope_forward(q, k, pos, split=(0, 0, 0), q_out=None, k_out=None, out_
             raise TypeError("%s: q and k must share one dtype" % what)
         sk = _token_strides(what, "k", k, (N, Hk, D), device)
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=out_dtype or k.dtype, device=k.device)
+            k_out = _empty(stream, k.shape, out_dtype or k.dtype, k.device)
         sko = _token_strides(what, "k_out", k_out, (N, Hk, D), device)
         k_code = _dtype16_code(what, "k_out", k_out)
         if q is not None and k_code != code:
@@ -1051,7 +1060,7 @@ def dit_kv_append_forward(k, v, k_cache, v_cache, page_table, q_start, kv_len, p
             _too_many(what)
         sq = _token_strides(what, "q", q, (N, H, D), device)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+            q_out = _empty(stream, q.shape, out_dtype or q.dtype, q.device)
         sqo = _token_strides(what, "q_out", q_out, (N, H, D), device)
         code = _dtype16_code(what, "q_out", q_out)
         qp, qop = q.data_ptr(), q_out.data_ptr()
@@ -1099,17 +1108,17 @@ def dit_attn_paged_forward(q, k_cache, v_cache, page_table, q_start, kv_len, fra
     if cache[3] != D or cache[2] < 1 or H % cache[2]:
         raise ValueError("%s: q's %d heads of %d channels do not fit the cache's %d of %d" % (what, H, D, cache[2], cache[3]))
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype or (torch.bfloat16 if q.dtype == torch.float16 else q.dtype), device=q.device)
+        out = _empty(stream, shape, out_dtype or (torch.bfloat16 if q.dtype == torch.float16 else q.dtype), q.device)
     so = _token_strides(what, "out", out, shape, device)
     if lse is None:
         if want_lse:
-            lse = torch.empty((H, N), dtype=torch.float32, device=q.device)
+            lse = _empty(stream, (H, N), torch.float32, q.device)
     elif lse.dtype != torch.float32 or lse.shape != (H, N) or not lse.is_contiguous() or lse.get_device() != device:
         raise ValueError("%s: lse must be a dense float32 tensor of shape %s on q's device" % (what, (H, N)))
     p = _PAGED_PACK(N, H, frame, window, max_q, max_kv, scale, _dtype16_code(what, "q", q), _dtype_code(out), 0, *sq, *so, *cache)
     need = lib().dit_attn_paged_workspace_bytes(p)
     if workspace is None:
-        workspace = _workspace(need, q.device)
+        workspace = _empty(stream, max(need, 256), torch.uint8, q.device)
     else:
         _check_workspace(what, workspace, need, q.device)
     st = lib().dit_attn_paged_forward(q.data_ptr(), kcp, vcp, tp, sp, lp, out.data_ptr(),

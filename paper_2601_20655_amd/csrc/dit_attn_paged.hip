@@ -542,7 +542,7 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
 // before it multiplies.  Two workgroups of 4 wavefronts a compute unit, or one of 8 (where there are few: half as many keys one
 // after the other), keep up to 128 KiB on their way.  Their results are joined in LDS.  Measured, one new token a request: 40 heads with
 // keys of their own x 32,760 keys 114 us = 5.9 TB/s, 32 requests of 16 to 8,190 keys x 8 key heads 104 us = 5.2 TB/s, 8 key heads x 257 keys
-// 11.6 (counts, page, rows, products, join and store one after the other).
+// 9.9 (counts, page, rows, products, join and store one after the other; 11.6 where one wavefront joined and stored).
 template <int D, int NW>
 constexpr int few_lds() { return NW * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
 

@@ -166,3 +166,29 @@ def test_two_streams():
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert np.array_equal(host(a), b)
+
+
+def test_memory_of_another_stream():
+    """What a call on another stream allocates is none that work queued on the current stream still writes."""
+    import torch
+
+    c = Cache([5000], 2, 128, 64, "bf16", "head", 4)
+    q = randn(5, (4, 8, 128), "bf16")
+    call = c.args([4])
+    want, want_lse = B.dit_attn_paged_forward(q, *call, frame=1, want_lse=True)  # (in pieces: a workspace)
+    need = 64 << 20
+    side = torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for _ in range(20):
+            busy = busy @ busy * 1e-3
+        late = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (need, want.numel() * 2, want_lse.numel() * 4)]
+        for x in late:
+            x.fill_(255)  # runs when the products have
+        del late, x
+        got, lse = B.dit_attn_paged_forward(q, *call, frame=1, want_lse=True, stream=side)
+        side.synchronize()
+        kept = got.clone(), lse.clone()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(kept + (got, lse), (want, want_lse) * 2))
