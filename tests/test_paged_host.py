@@ -150,6 +150,24 @@ def test_which_kernels(N, R, H, Hk, max_q, few, big):
         assert not on or 1 <= units <= 1 << 20
 
 
+@pytest.mark.parametrize("runs", [0, 1])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,Hk", [(1, 1), (8, 1), (40, 8), (40, 40)])
+def test_workspace_is_bounded(H, Hk, D, runs):
+    """Whatever the counts and hints: room for 2^19 rows of pieces a kernel, at most, and for every tile's pieces as planned."""
+    for N in (1, 17, 500, 4680, 1_000_000):
+        for requests in (1, 3, 100, 700):
+            for keys in (1, 257, 8190, 100_000, 2 ** 31 - 65536):
+                for max_q in (0, 1, 40, N):
+                    p = plan(N, requests, H, Hk, D, keys, max_q, runs)
+                    for on, size, rows, each, pieces, cap in (
+                            (p.few, p.few_bytes, 16 * p.few_qb, p.few_each, p.few_pieces, p.few_cap),
+                            (p.big, p.big_bytes, 16 * p.big_qb * p.big_waves, p.big_each, p.big_pieces, p.big_cap)):
+                        assert size <= 2 ** 19 * (4 * D + 8) + 256 and (on or size == 0)
+                        if on and each > 1:
+                            assert size >= Hk * cap * rows * (4 * D + 8) and cap > pieces >= each >= 2 and each <= 512
+
+
 def test_python_wrappers_check_extents_before_any_call():
     import torch
 
