@@ -970,7 +970,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
                 }
             return k;
         };
-        bool far = false;  // a row's maximum is too large for (s - m) c in one fma (tile_step)
+        bool far = false;  // a row's maximum is too large for (s - m) c in one fma (see block_step)
         auto raise = [&](scores_t& S) {
             far = false;
 #pragma unroll
@@ -993,6 +993,16 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
                     for (int r = 0; r < 16; ++r) O[og][q][r] *= alpha;
             }
             far = __any(far);
+        };
+        // A half's scores of such rows: the difference first.  (off is that of the half: the next raise, or this again, sets it anew.)
+        auto take_maxima = [&](scores_t& S) {
+#pragma unroll
+            for (int q = 0; q < QB; ++q) {
+                const bool some = m[q] != kNoScore;
+                off[q] = some ? 0.f : off[q];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) S[q / 2][8 * (q % 2) + e] -= some ? m[q] : 0.f;
+            }
         };
         // slice x = (q, w): word w of the operand of the half's keys for row block q
         auto exp_slice = [&](scores_t& S, int x) {
@@ -1079,15 +1089,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
         auto any_half = [&](scores_t& S, bool masked, int key0, uint32_t there, uint8_t* vb, bool more, bool masked_next, uint32_t there_next,
                             const uint8_t* kn) __attribute__((always_inline)) {
             const int ln = opaque_lane(), i = ln & 15, g = ln >> 4;
-            if (far) {
-#pragma unroll
-                for (int q = 0; q < QB; ++q) {
-                    const bool some = m[q] != kNoScore;
-                    off[q] = some ? 0.f : off[q];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) S[q / 2][8 * (q % 2) + e] -= some ? m[q] : 0.f;
-                }
-            }
+            if (far) take_maxima(S);
             uint32_t P[QB][4];
 #pragma unroll
             for (int x = 0; x < NCH; ++x) exp_slice(S, x);
@@ -1180,6 +1182,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
 #pragma unroll
                     for (int x = 0; x < 4; ++x) vl[x] = vbuf(b) + v_l[x];
                     plain_half(S0, S1, kl, vl, std::integral_constant<int, 0>{});
+                    if (far) take_maxima(S1);  // (since the half before; the turn's end leaves the loop)
                     plain_half(S1, S0, kl, vl, std::integral_constant<int, 1>{});
                     ++j;
                     b ^= 1;
