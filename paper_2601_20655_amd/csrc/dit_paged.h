@@ -105,7 +105,7 @@ struct PagedAttnArgs {
     int least;       // key tiles of a piece, at least
     int part_cap;    // tiles' pieces per key head that part_o, part_ml have room for
     float* part_o;   // [Hk][piece][row][D] unnormalised
-    float2* part_ml; // [Hk][piece][row]: maximum (base 2), sum
+    float2* part_ml; // [Hk][piece][row]: maximum of the products, sum
 };
 struct PagedPlan {
     bool few, big;
