@@ -23,7 +23,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* ltr_t;
 
 constexpr int kWaitLoads = 0x0f70;  // s_waitcnt vmcnt(0), the other counters at their most
-constexpr float kNoScore = -1e30f;  // running maximum of a row that has none (finite: differences stay numbers)
+constexpr float kNoScore = -0x1.fffffep127f;  // running maximum of a row that has none (finite: its difference to itself is 0)
 
 // ---- rows of K and V in LDS ----
 // A wavefront-wide load brings 1 KiB: 4 rows of 128 channels or 8 of 64, in lane order.  So that a fragment's read takes each
@@ -1090,6 +1090,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
                             const uint8_t* kn) __attribute__((always_inline)) {
             const int ln = opaque_lane(), i = ln & 15, g = ln >> 4;
             if (far) take_maxima(S);
+#pragma unroll
+            for (int q = 0; q < QB; ++q) off[q] = fminf(off[q], -kNoScore);  // (a row without a score: all of its exponents are to be -infinity)
             uint32_t P[QB][4];
 #pragma unroll
             for (int x = 0; x < NCH; ++x) exp_slice(S, x);
