@@ -621,8 +621,9 @@ dit_status dit_kv_append_forward(const void *q, const void *k, const void *v, co
  *   scale <= 0 selects 1/sqrt(D)
  *   max_q, max_kv  the most new tokens and the most keys of any request, as far as the host knows (0: not); results are right
  *         whatever they are, and their bits depend on them: they choose the kernels, and where tiles are few, the pieces that their keys are taken in
- * Products are exact, scores, softmax and sums in fp32; probabilities are rounded to the cache's type for the product with V, the
- * sums that divide it and lse are over the unrounded ones.  A masked key may hold anything, an infinity or a NaN too.
+ * Products are exact, scores, softmax and sums in fp32; probabilities are rounded to the cache's type for the product with V (half a
+ * step of it; in fp16 one below 2^-21 of the row's largest by 2^-32 of that at the most), the sums that divide it and lse are over the
+ * unrounded ones.  A masked key may hold anything, an infinity or a NaN too.
  * Deterministic: the same arguments give the same bits.  A row's bits depend on the other requests' counts too (pieces).
  * workspace: dit_attn_paged_workspace_bytes(p) bytes (the same for any counts), 256-byte aligned.
  * Errors: NULL q, caches, page_table, q_start, kv_len, out or p, N < 0, H no multiple of Hk, a negative frame, window, max_q or max_kv, window

@@ -25,6 +25,13 @@ typedef __attribute__((address_space(3))) s16x4* ltr_t;
 constexpr int kWaitLoads = 0x0f70;  // s_waitcnt vmcnt(0), the other counters at their most
 constexpr float kNoScore = -0x1.fffffep127f;  // running maximum of a row that has none (finite: its difference to itself is 0)
 
+// Probabilities are formed times 2^bits, which the division by their sum takes out again (lse and nothing else has to know).  fp16 holds
+// numbers from 2^-24 up to 2^16, so that of a row with a large one many small ones would be lost: with as many bits as the kernel's largest
+// probability leaves (1 with few rows, 2^8 where a maximum is raised late) those down to 2^-39 or 2^-31 of the row's largest keep
+// all or some of theirs, and a smaller one is off by 2^-40 or 2^-32.  bf16 has fp32's range.
+template <int OP>
+constexpr int prob_bits(bool few) { return OP == OP_F16 ? (few ? 15 : 7) : 0; }
+
 // ---- rows of K and V in LDS ----
 // A wavefront-wide load brings 1 KiB: 4 rows of 128 channels or 8 of 64, in lane order.  So that a fragment's read takes each
 // bank once, a row's 16-byte pieces lie in an order of the row's own (the order is in which piece a lane fetches), and each
@@ -415,9 +422,10 @@ __device__ __forceinline__ void block_step(RowState<D, QB>& st, const u32x4 (&Q)
         }
         // (s - m) c as one fma(s, c, -m c).  -m c is rounded: by 2^-13 at most below 2^12; beyond, where it would be by more
         // than an exponent holds, the difference is taken first.
-        float off = -mx * scale_log2;
+        constexpr float bits = prob_bits<OP>(true);
+        float off = fmaf(-mx, scale_log2, bits);
         if (__any(__builtin_fabsf(off) > 4096.0f)) {
-            off = 0.f;
+            off = bits;
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -488,10 +496,10 @@ __device__ __forceinline__ void load_rows(const PagedAttnArgs& a, const Unit& u,
 }
 
 // Channel blocks cb0 .. of row `row` out: normalised, or (a tile in pieces) as they are with their maximum (of the products, not scaled) and sum.  l: summed over the
-// row's lanes.  at_tile: the row's place in its tile.
+// row's lanes.  at_tile: the row's place in its tile.  bits: as of prob_bits.
 template <int N>
 __device__ __forceinline__ void store_blocks(const PagedAttnArgs& a, const Unit& u, int hk, int D, int rows_of_tile, int at_tile, int64_t row,
-                                             int g, int cb0, const f32x4 (&O)[N], float m, float l) {
+                                             int g, int cb0, const f32x4 (&O)[N], float m, float l, int bits) {
     const RowPlace p = place_of(a, u, hk, row);
     if (!p.live) return;
     if (u.pieces > 1) {
@@ -513,7 +521,7 @@ __device__ __forceinline__ void store_blocks(const PagedAttnArgs& a, const Unit&
         store4(a.out, off + 16 * cb, a.out_type, v);
     }
     if (a.lse && g == 0 && cb0 == 0)
-        a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (m * a.scale_log2 + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (m * a.scale_log2 + (__builtin_amdgcn_logf(l) - (float)bits)) * 0.6931471805599453f;
 }
 
 // Key tiles of the unit: from the first key that its first token sees to the last that its last token sees, and of those its
@@ -734,7 +742,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_few_kernel(const PagedA
 #pragma unroll
                         for (int r = 0; r < 4; ++r) sum[n][r] = w ? sum[n][r] + x[r] : x[r];
                     }
-                store_blocks(a, u, hk, D, BQ, 16 * q + i, row0 + 16 * q + i, g, cb0, sum, st.m[q], l[q]);
+                store_blocks(a, u, hk, D, BQ, 16 * q + i, row0 + 16 * q + i, g, cb0, sum, st.m[q], l[q], prob_bits<OP>(true));
             }
         }
         __syncthreads();
@@ -780,6 +788,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
     const Units all = count_units<BQ>(a, requests, lane);
     const int per_head = all.units, total = per_head * a.Hk;
     const float scale = a.scale_log2, thr = kRescaleThr / scale;
+    constexpr float bits = prob_bits<OP>(false);
+    static_assert(kRescaleThr + prob_bits<OP>(false) <= 15 || OP != OP_F16, "the largest probability is an fp16 number");
     // K buffers 0 and 1, then V's
     auto kbuf = [&](int b) { return dyn + b * R::k_bytes(kBK); };
     auto vbuf = [&](int b) { return dyn + 2 * R::k_bytes(kBK) + b * R::v_bytes(kBK); };
@@ -982,8 +992,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
                 const float to = mx > top[q] ? mx : m[q];
                 const float alpha = __builtin_amdgcn_exp2f((m[q] - to) * scale);
                 m[q] = to;
-                top[q] = to + thr;
-                off[q] = -to * scale;
+                // (a large one's sum is rounded, by as much as thr: more than fp16 has room for)
+                top[q] = OP == OP_F16 && __builtin_fabsf(to * scale) > 4096.0f ? to : to + thr;
+                off[q] = OP == OP_F16 ? fmaf(-to, scale, bits) : -to * scale;
                 l[q][0] *= alpha;
                 l[q][1] *= alpha;
                 far = far || (to != kNoScore && __builtin_fabsf(off[q]) > 4096.0f);
@@ -999,7 +1010,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
 #pragma unroll
             for (int q = 0; q < QB; ++q) {
                 const bool some = m[q] != kNoScore;
-                off[q] = some ? 0.f : off[q];
+                off[q] = some ? bits : off[q];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) S[q / 2][8 * (q % 2) + e] -= some ? m[q] : 0.f;
             }
@@ -1211,7 +1222,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
             for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[cb][r] = O[cb / 4][q][4 * (cb % 4) + r];
-            store_blocks(a, u, hk, D, BQ, (wave * QB + q) * 16 + i, row0 + 16 * q + i, g, 0, o, m[q], sum_across_rows16(l[q][0] + l[q][1]));
+            store_blocks(a, u, hk, D, BQ, (wave * QB + q) * 16 + i, row0 + 16 * q + i, g, 0, o, m[q], sum_across_rows16(l[q][0] + l[q][1]),
+                         prob_bits<OP>(false));
         }
         __syncthreads();
     }
@@ -1222,7 +1234,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
 // piece's weight is of its maximum's difference, taken before the scale (their products differ by a rounding each, 2^-24 of themselves).
 // 1,560 x 12 rows of 128 channels in three pieces 10.2 us, 40 rows in five 5.4 (a wavefront a row: 14.0, 7.5).
 template <int D, int BQ, int UN>
-__global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArgs a, int bits) {
     constexpr int LANES = D / 4, PER = 256 / LANES, PARTS = BQ / PER;  // of a row, rows of a workgroup, workgroups of a tile
     const int lane = threadIdx.x & 63;
     Requests<BQ> requests;
@@ -1274,14 +1286,14 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const PagedAttnArg
         store4(a.out, (int64_t)(u.q0 + p.token) * a.so_t + (int64_t)p.head * a.so_h + ch, a.out_type,
                f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv});
         if (a.lse && ch == 0)
-            a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (top * a.scale_log2 + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+            a.lse[(int64_t)p.head * a.N + u.q0 + p.token] = (top * a.scale_log2 + (__builtin_amdgcn_logf(sum) - (float)bits)) * 0.6931471805599453f;
     }
 }
 // Its launch, for so many tiles as are known of.
 template <int D, int BQ, int UN>
-hipError_t launch_join(const PagedAttnArgs& a, int units, hipStream_t s) {
+hipError_t launch_join(const PagedAttnArgs& a, int units, int bits, hipStream_t s) {
     const int64_t n = (int64_t)units / a.pieces_each * (BQ * D / 1024);
-    hipLaunchKernelGGL((attn_paged_join_kernel<D, BQ, UN>), dim3((unsigned)(n < 1 ? 1 : n < 65536 ? n : 65536)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attn_paged_join_kernel<D, BQ, UN>), dim3((unsigned)(n < 1 ? 1 : n < 65536 ? n : 65536)), dim3(256), 0, s, a, bits);
     return hipGetLastError();
 }
 
@@ -1300,7 +1312,7 @@ hipError_t launch_few(const PagedAttnArgs& a, int units, int nw, hipStream_t s) 
     hipError_t e;
     if (nw == 8) e = a.pages.runs ? launch_few_n<D, OP, QB, true, 8>(a, units, s) : launch_few_n<D, OP, QB, false, 8>(a, units, s);
     else e = a.pages.runs ? launch_few_n<D, OP, QB, true, 4>(a, units, s) : launch_few_n<D, OP, QB, false, 4>(a, units, s);
-    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB, 8>(a, units, s);
+    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB, 8>(a, units, prob_bits<OP>(true), s);
 }
 template <int D, int OP, bool RUNS, int NW, int QB>
 hipError_t launch_big_n(const PagedAttnArgs& a, int units, hipStream_t s) {
@@ -1311,7 +1323,7 @@ hipError_t launch_big_n(const PagedAttnArgs& a, int units, hipStream_t s) {
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kern, dim3((units + 7) / 8 * 8), dim3(64 * NW), lds, s, a);
     e = hipGetLastError();
-    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB * NW, 4>(a, units, s);
+    return e != hipSuccess || !a.pieces ? e : launch_join<D, 16 * QB * NW, 4>(a, units, prob_bits<OP>(false), s);
 }
 template <int D, int OP>
 hipError_t launch_big(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t s) {
