@@ -573,10 +573,12 @@ dit_status dit_qk_rope_forward(const void *q, const void *k, const int32_t *pos,
  *               was dropped to bound the cache, say): nothing is written to it, and its keys attend no more.  Requests may
  *               share pages.
  *   q_start     int32 [n_requests + 1] DEVICE, ascending from 0: rows q_start[r] .. q_start[r+1]-1 are request r's new tokens.
- *               Rows from q_start[n_requests] on are of no request: neither read nor, where they are outputs, written.
+ *               Rows from q_start[n_requests] on are of no request: what they hold does not matter (dit_kv_append_forward may load
+ *               them), and where they are outputs they are not written.
  *   kv_len      int32 [n_requests] DEVICE: tokens of the request, the new ones (its last) included.
- * Counts that are out of range lead to no access out of range: q_start is clamped to 0 .. N; the attention clamps kv_len to 0 .. the
- * lesser of max_pages*page_size and 2^31 - 65,536, and no token is written behind the table.
+ * Counts that are out of range lead to no access out of range: both calls clamp q_start to 0 .. N (so that the new tokens of a request whose
+ * end is behind N are those up to N); the attention clamps kv_len to 0 .. the lesser of max_pages*page_size and 2^31 - 65,536, and no
+ * token is written behind the table.
  */
 typedef struct {
     int32_t n_pages, page_size, Hk, D;

@@ -149,6 +149,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(const RowsArgs a, int wq, in
                 keys = a.pages.kv_len[r];
             }
         }
+        past = past < a.N ? past : a.N;  // (as the attention has it: a place is counted from the request's last row that is there)
         place = r < 0 || kind == 0 ? -1 : (int64_t)keys - past + t;
         if (place < 0 || place >= (int64_t)a.pages.max_pages * a.pages.page.d || place > 0x7fffffff) place = -1;
         if (place >= 0) entry = a.pages.table[(int64_t)r * a.pages.max_pages + div_by((uint32_t)place, a.pages.page)];
