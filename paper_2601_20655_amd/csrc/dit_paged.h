@@ -42,18 +42,19 @@ __device__ __forceinline__ int keys_of(const PageArgs& p, int r) {
 
 // Request of new token t: the last r with q_start[r] <= t, by the wavefront together, 64 entries at a time; -1: of none.
 __device__ __forceinline__ int request_of(const PageArgs& p, int t, int lane) {
-    int lo = 0, n = p.n_requests + 1;  // the answer is among entries lo .. lo + n - 1, or lo is 0 and there is none
+    // the answer is among entries lo .. lo + n - 1, or lo is 0 and there is none (unsigned: n is 2^31 at the most)
+    const uint32_t entries = (uint32_t)p.n_requests + 1;
+    uint32_t lo = 0, n = entries;
     while (true) {
-        const int step = (n + 63) >> 6;
-        const int at = lo + lane * step;
-        const uint64_t b = __ballot(lane * step < n && p.q_start[at <= p.n_requests ? at : p.n_requests] <= t);
+        const uint32_t step = (n + 63) >> 6, mine = (uint32_t)lane * step;
+        const uint64_t b = __ballot(mine < n && p.q_start[lo + mine < entries ? lo + mine : entries - 1] <= t);
         if (b == 0) return -1;
-        const int last = 63 - __builtin_clzll(b);
+        const uint32_t last = 63 - __builtin_clzll(b);
         lo += last * step;
         n = n - last * step < step ? n - last * step : step;
         if (step == 1) break;
     }
-    return lo < p.n_requests ? lo : -1;
+    return lo + 1 < entries ? (int)lo : -1;
 }
 
 // ---- rows normalised and rotated, to rows or to pages (dit_paged_rows.hip) ----
