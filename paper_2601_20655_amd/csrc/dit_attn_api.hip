@@ -1526,6 +1526,7 @@ dit_status dit_qk_rope_forward(const void* q, const void* k, const int32_t* pos,
     if (st != DIT_OK) return st;
     if (q && !(rows_ok(p->sq, p->H, p->D, p->N) && rows_ok(p->sq_out, p->H, p->D, p->N))) return DIT_ERR_INVALID_ARG;
     if (k && !(rows_ok(p->sk, p->Hk, p->D, p->N) && rows_ok(p->sk_out, p->Hk, p->D, p->N))) return DIT_ERR_INVALID_ARG;
+    if (!dit::rows_heads_fit(p->H, p->Hk, 0)) return DIT_ERR_UNSUPPORTED;
     if (p->norm.mode == DIT_NORM_TOKEN && !dit::rows_fit(p->H, p->Hk, 0, p->D)) return DIT_ERR_UNSUPPORTED;
     if (!aligned4(pos, nullptr, nullptr)) return DIT_ERR_ALIGNMENT;
     if (q && !(rows_aligned(q, p->sq, p->H, p->N, p->in_dtype) && rows_aligned(q_out, p->sq_out, p->H, p->N, p->out_dtype)))
@@ -1561,6 +1562,7 @@ dit_status dit_kv_append_forward(const void* q, const void* k, const void* v, co
     if (st != DIT_OK) return st;
     if (q && !(rows_ok(p->sq, p->H, D, p->N) && rows_ok(p->sq_out, p->H, D, p->N))) return DIT_ERR_INVALID_ARG;
     if (!rows_ok(p->sk, Hk, D, p->N) || !rows_ok(p->sv, Hk, D, p->N)) return DIT_ERR_INVALID_ARG;
+    if (!dit::rows_heads_fit(p->H, Hk, Hk)) return DIT_ERR_UNSUPPORTED;
     if (p->norm.mode == DIT_NORM_TOKEN && !dit::rows_fit(p->H, Hk, Hk, D)) return DIT_ERR_UNSUPPORTED;
     if (!aligned4(pos, page_table, q_start) || !aligned4(kv_len, nullptr, nullptr) || !cache_aligned(p->cache, k_cache, v_cache))
         return DIT_ERR_ALIGNMENT;

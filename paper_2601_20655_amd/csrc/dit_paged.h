@@ -82,6 +82,8 @@ struct RowsArgs {
     double turn[kMostPairs];  // turns per unit of position, of every pair
 };
 hipError_t launch_rows(const RowsArgs& a, int D, hipStream_t s);
+// A token's wavefronts (one has four heads at least) are no more than those of a launch of 2^32 work items.
+bool rows_heads_fit(int H, int Hk, int Hv);
 bool rows_fit(int H, int Hk, int Hv, int D);  // the heads of a token, where the mean is over all of them
 
 // ---- attention over pages (dit_attn_paged.hip) ----

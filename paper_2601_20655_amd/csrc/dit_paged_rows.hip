@@ -307,7 +307,7 @@ hipError_t launch_rows_c(const RowsArgs& a, hipStream_t s) {
     const int W = w.all();
     // whole tokens a workgroup where their wavefronts have to meet; a launch has fewer than 2^32 work items
     const int tokens = NORM == RN_TOKEN ? (W >= 4 ? 1 : 4 / W) : 0;
-    const int64_t most = (0xffffffffLL / 1024 / W) * 4;
+    const int64_t most = tokens ? 0xffffffffLL / (64 * W * tokens) * tokens : 0xffffffffLL / 256 * 4 / W;  // (W: rows_heads_fit)
     for (int64_t t = 0; t < a.N; t += most) {
         const int64_t n = a.N - t < most ? a.N - t : most;
         RowsArgs b = a;
@@ -362,6 +362,7 @@ hipError_t launch_rows_d(const RowsArgs& a, hipStream_t s) {
 
 }  // namespace
 
+bool rows_heads_fit(int H, int Hk, int Hv) { return (int64_t)H + Hk + Hv <= 1 << 27; }
 bool rows_fit(int H, int Hk, int Hv, int D) { return row_waves(H, Hk, Hv, D, kMostRowChunks).all() <= 16; }
 
 hipError_t launch_rows(const RowsArgs& a, int D, hipStream_t s) {
