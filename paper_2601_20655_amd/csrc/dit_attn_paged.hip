@@ -298,6 +298,8 @@ __device__ __forceinline__ KeyRow row_of(const PageArgs& p, int entry, int key, 
 }
 
 // ---- query rows ----
+// Rounded to the cache's type where theirs is another: a product of the matrix cores has two operands of one 16-bit type, and a second part
+// (what the rounding leaves) would double the scores' products.
 __device__ __forceinline__ u32x4 load_q(const void* q, int64_t off, int type, int op) {
     if (type == (op == OP_F16 ? DIT_F16 : DIT_BF16)) return *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(q) + off);
     float x[8];
@@ -369,7 +371,8 @@ struct RowState {
     }
 };
 
-// 32 keys: scores, softmax, O += P V.  kf(f), vf(cb): their fragments.  MASKED: `there` (bit = the key's page is there) and the
+// 32 keys: scores, softmax, O += P V.  P is rounded to the cache's type, V's, as the matrix cores take it (what a second part of P would cost
+// is as many products again); its sums are of the unrounded ones.  kf(f), vf(cb): their fragments.  MASKED: `there` (bit = the key's page is there) and the
 // rows' ranges leave some out, and vt is where V's rows lie in LDS.
 template <int D, int OP, int QB, bool MASKED, class KF, class VF>
 __device__ __forceinline__ void block_step(RowState<D, QB>& st, const u32x4 (&Q)[QB][D / 32], KF&& kf, VF&& vf, const uint8_t* vt,
@@ -550,7 +553,8 @@ __device__ __forceinline__ void key_tiles_of(const PagedAttnArgs& a, const Unit&
 // before it multiplies.  Two workgroups of 4 wavefronts a compute unit, or one of 8 (where there are few: half as many keys one
 // after the other), keep up to 128 KiB on their way.  Their results are joined in LDS.  Measured, one new token a request: 40 heads with
 // keys of their own x 32,760 keys 114 us = 5.9 TB/s, 32 requests of 16 to 8,190 keys x 8 key heads 104 us = 5.2 TB/s, 8 key heads x 257 keys
-// 9.9 (counts, page, rows, products, join and store one after the other; 11.6 where one wavefront joined and stored).
+// 9.9 (counts, page, rows, products, join and store one after the other; 11.6 where one wavefront joined and stored).  Of 128 channels the
+// 32-row form fills all 256 vector registers and spills 35 to 45 (16 rows: 181 to 200, none).
 template <int D, int NW>
 constexpr int few_lds() { return NW * (Rows<D>::k_bytes(32) + Rows<D>::v_bytes(32)); }
 
