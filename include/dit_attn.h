@@ -545,9 +545,9 @@ dit_status dit_linear_quant_forward(const int8_t *x, const float *x_scale, const
  * the same; else it may overlap neither input.  No workspace.
  * Errors: NULL p, q and k both NULL, an output that is NULL where its input is not (or the other way round), N < 0, heads that
  * are not 1 or more where there are rows and 0 where there are none, a bad dtype, split, rope_base or norm, nonzero flags, rows
- * that overlap -> DIT_ERR_INVALID_ARG; D other than 64 or 128, more than 2^27 heads in all, DIT_NORM_TOKEN with more heads than 512 of 128 channels or 1,024
- * of 64 (those of q, k and v together, each rounded up to a multiple of 32 or 64) -> DIT_ERR_UNSUPPORTED; a base pointer or
- * stride that breaks 16-byte row alignment (4 bytes for pos) -> DIT_ERR_ALIGNMENT.  N = 0 is no error and does nothing.
+ * that overlap -> DIT_ERR_INVALID_ARG; D other than 64 or 128, more than 2^27 heads in all (v's among them), DIT_NORM_TOKEN with
+ * more heads than 512 of 128 channels or 1,024 of 64 (those of q, k and v together, each rounded up to a multiple of 32 or 64) ->
+ * DIT_ERR_UNSUPPORTED; a base pointer or stride that breaks 16-byte row alignment (4 bytes for pos) -> DIT_ERR_ALIGNMENT.  N = 0 is no error and does nothing.
  */
 typedef struct {
     int32_t N;             /* tokens */

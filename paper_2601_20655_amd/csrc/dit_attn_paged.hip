@@ -371,9 +371,9 @@ struct RowState {
     }
 };
 
-// 32 keys: scores, softmax, O += P V.  P is rounded to the cache's type, V's, as the matrix cores take it (what a second part of P would cost
-// is as many products again); its sums are of the unrounded ones.  kf(f), vf(cb): their fragments.  MASKED: `there` (bit = the key's page is there) and the
-// rows' ranges leave some out, and vt is where V's rows lie in LDS.
+// 32 keys: scores, softmax, O += P V.  P is rounded to the cache's type, V's, as the matrix cores take it (what a second part of P
+// would cost is as many products again); its sums are of the unrounded ones.  kf(f), vf(cb): their fragments.  MASKED: `there` (bit
+// = the key's page is there) and the rows' ranges leave some out, and vt is where V's rows lie in LDS.
 template <int D, int OP, int QB, bool MASKED, class KF, class VF>
 __device__ __forceinline__ void block_step(RowState<D, QB>& st, const u32x4 (&Q)[QB][D / 32], KF&& kf, VF&& vf, const uint8_t* vt,
                                            int key0, uint32_t there, float scale_log2, int i, int g) {
@@ -423,7 +423,7 @@ __device__ __forceinline__ void block_step(RowState<D, QB>& st, const u32x4 (&Q)
                 for (int r = 0; r < 4; ++r) st.O[q][cb][r] *= alpha;
             st.m[q] = mx;
         }
-        // (s - m) c as one fma(s, c, -m c).  -m c is rounded: by 2^-13 at most below 2^12; beyond, where it would be by more
+        // (s - m) c (+ bits) as one fma(s, c, -m c).  -m c is rounded: by 2^-13 at most below 2^12; beyond, where it would be by more
         // than an exponent holds, the difference is taken first.
         constexpr float bits = prob_bits<OP>(true);
         float off = fmaf(-mx, scale_log2, bits);
@@ -498,8 +498,8 @@ __device__ __forceinline__ void load_rows(const PagedAttnArgs& a, const Unit& u,
     }
 }
 
-// Channel blocks cb0 .. of row `row` out: normalised, or (a tile in pieces) as they are with their maximum (of the products, not scaled) and sum.  l: summed over the
-// row's lanes.  at_tile: the row's place in its tile.  bits: as of prob_bits.
+// Channel blocks cb0 .. of row `row` out: normalised, or (a tile in pieces) as they are with their maximum (of the products, not
+// scaled) and sum.  l: summed over the row's lanes.  at_tile: the row's place in its tile.  bits: as of prob_bits.
 template <int N>
 __device__ __forceinline__ void store_blocks(const PagedAttnArgs& a, const Unit& u, int hk, int D, int rows_of_tile, int at_tile, int64_t row,
                                              int g, int cb0, const f32x4 (&O)[N], float m, float l, int bits) {
@@ -1106,7 +1106,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attn_paged_big_kernel(const PagedA
             const int ln = opaque_lane(), i = ln & 15, g = ln >> 4;
             if (far) take_maxima(S);
 #pragma unroll
-            for (int q = 0; q < QB; ++q) off[q] = fminf(off[q], -kNoScore);  // (a row without a score: all of its exponents are to be -infinity)
+            for (int q = 0; q < QB; ++q) off[q] = fminf(off[q], -kNoScore);  // (a row without a score: all exponents are to be -infinity)
             uint32_t P[QB][4];
 #pragma unroll
             for (int x = 0; x < NCH; ++x) exp_slice(S, x);
